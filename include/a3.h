@@ -380,6 +380,94 @@ a3_status a3_rope_realign_q8(const a3_layout *layout, const void *cache_q8, void
 a3_status a3_chunk_cache_load_q8(const a3_layout *layout, const int *chunk_start_host, const int *chunk_len_host,
                                  int n_chunks, const void *const *host_q8, void *cache_q8, void *stream);
 
+/* ---- generating on the fused cache -----------------------------------------------------------------------------
+ *
+ * After the prompt every request grows by one token a step.  Its K and V live in pages of page_size tokens that lie
+ * anywhere in a pool; page_table[r, j] is the page of the request's tokens j * page_size .. (j + 1) * page_size - 1
+ * ("slots": a token's index in its request's cache; after an eviction that is not its position).  One a3_pages is one
+ * layer's cache; the layers of a stack may share page_table and rope_cs.
+ *   A3_PAGES_PLAIN  one page of one KV head is [page_size, head_dim] elements of `dtype`
+ *   A3_PAGES_Q8     [page_size, head_dim] int8 codes, then [page_size] float32 scales: x = code * scale per token and
+ *                   KV head (the rule of a3_quantize_q8)
+ * and a pool is [n_pages, n_kv_heads] of those: the tokens of one head, which one workgroup reads, are one run of memory.
+ *
+ * Supported: head_dim 64 or 128, up to 16 query heads per KV head, page_size a power of two from 32 to 1024, both dtypes
+ * with both formats; pools of any size.  Device arrays cannot be checked on the host, so the kernels check them: a page
+ * number outside [0, n_pages), a request outside [0, n_req), a slot outside the table and a position outside rope_cs are
+ * never followed (see each call).  Nothing is assumed about what a page holds behind a request's last token. */
+typedef enum { A3_PAGES_PLAIN = 0, A3_PAGES_Q8 = 1 } a3_page_format;
+
+typedef struct a3_pages {
+  int dtype;              /* a3_dtype of q, k, v rows and outputs */
+  int format;             /* a3_page_format */
+  int n_q_heads;
+  int n_kv_heads;
+  int head_dim;
+  int rope_layout;        /* a3_rope */
+  double rope_base;
+  float sm_scale;         /* softmax scale; 0 means 1/sqrt(head_dim) */
+  int page_size;
+  int n_pages;            /* pages in each pool */
+  int n_req;              /* rows of the page table */
+  int max_pages;          /* columns of the page table */
+  int n_pos;              /* rows of rope_cs */
+  void *k_pool;           /* [n_pages] of a3_page_bytes(), 16-byte aligned */
+  void *v_pool;
+  const int *page_table;  /* device int32 [n_req, max_pages] */
+  float *rope_cs;         /* device [n_pos, head_dim/2, 2] (cos, sin) of p * theta_i: a3_pages_prepare fills it */
+} a3_pages;
+
+/* Bytes of one page of one pool (all KV heads).  Host only; 0 on a bad argument. */
+size_t a3_page_bytes(const a3_pages *pages);
+
+/* Fills rope_cs (angles formed and evaluated in double precision, stored as float, as a3_layout_prepare does). */
+a3_status a3_pages_prepare(const a3_pages *pages, void *stream);
+
+/* Writes K and V of row i, of request r = row_req[i] (NULL: i), to slot row_slot[i]; with row_pos the key is turned to
+ * position row_pos[i] first, and with q the query too (q_out[i] = R(row_pos[i]) q[i]; q_out may be q).  row_pos NULL: keys
+ * stand at their positions already (a prompt's fused cache: row_req = layout->tok_req, row_slot = layout->tok_pos), q must be
+ * NULL.  k, v: [n_rows, n_kv_heads, head_dim]; q, q_out: [n_rows, n_q_heads, head_dim]; index arrays: device int32 [n_rows].
+ * A row whose request, slot, page or position does not exist is skipped: nothing of it is written, q_out included (a padded
+ * batch marks its rows with request or slot -1).  No two rows may name the same slot of the same request, no page may belong
+ * to two requests.  Turned in float and rounded once; A3_PAGES_Q8: turned in double, so that the codes are those of the exact
+ * values (finite values). */
+a3_status a3_paged_append(const a3_pages *pages, const void *k, const void *v, const int *row_req, const int *row_slot,
+                          const int *row_pos, int n_rows, const void *q, void *q_out, void *stream);
+
+/* Attention of single tokens: out[i, hq] = sum_u softmax_u(q[i, hq] . K[r, u, hq/G] * sm_scale) V[r, u, hq/G] over the slots
+ * u < row_len[i] of request r = row_req[i] (NULL: i).  q, out: [n_rows, n_q_heads, head_dim], may be the same buffer; row_len:
+ * device int32 [n_rows].  Rows may name the same request (with lengths of their own).  A row that sees nothing (length
+ * <= 0) gets zeros; a length beyond the table is cut to it; the slots of a page that does not exist count as not seen; a row
+ * whose request does not exist is left as it was.  Which bytes lie behind row_len in a page does not matter, NaN included.
+ * Softmax statistics, weights' sums and products in float.  How the sums of a row are cut depends on the lengths of all rows:
+ * a row may differ in its last bits between calls with other lengths, never between calls with the same.
+ * ws: a3_paged_attention_ws_bytes(pages, n_rows) bytes, 16-byte aligned, contents of no concern before or after; one buffer
+ * serves one call at a time. */
+size_t a3_paged_attention_ws_bytes(const a3_pages *pages, int n_rows);
+a3_status a3_paged_attention(const a3_pages *pages, const void *q, const int *row_req, const int *row_len, int n_rows,
+                             void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* logits[i, v] = sum_c hidden[row_idx[i], c] * w[v, c], float, row i at logits + i * ld.  hidden: [total_tokens, hidden] in the
+ * layout's dtype (the final-normed rows a3_block_tail leaves); row_idx: device int32 [n_rows], NULL = rows 0 .. n_rows-1, a row
+ * may be named more than once; w: [vocab, hidden], 16-byte aligned; ld >= vocab.  Any vocab; 4-byte aligned logits. */
+a3_status a3_lm_head(const a3_layout *layout, const void *hidden, const int *row_idx, int n_rows, const void *w, int vocab,
+                     float *logits, long long ld, void *stream);
+
+/* Log probabilities of rows of logits.  Row i is logits + i * ld (elements of `dtype`, an a3_dtype; ld >= vocab, any vocab and
+ * ld; the base 16-byte aligned).  With m = max_v x_v and Z = sum_v e^(x_v - m):
+ *   logprob[i, j]      x_t - m - log Z of t = tokens[i, j], j < n_given; -inf where t is outside [0, vocab)
+ *   entropy[i]         log Z - sum_v e^(x_v - m) (x_v - m) / Z      (a logit of -inf adds nothing)
+ *   top_idx[i, j]      the n_top largest logits, largest first, equal ones by the lower index (-0 equals 0; NaN comes last)
+ *   top_logprob[i, j]  their log probabilities
+ * A row of nothing but -inf, or with a NaN or +inf, has no distribution: its logprob, entropy and top_logprob are NaN.
+ * tokens: device int32 [n_rows, n_given]; logprob, entropy, top_logprob: float; top_idx: int32.  entropy may be NULL; tokens and
+ * logprob are not looked at for n_given = 0, the top outputs for n_top = 0.  0 <= n_top <= min(vocab, 64).
+ * ws: a3_token_logprobs_ws_bytes() bytes, 16-byte aligned, contents of no concern before or after. */
+size_t a3_token_logprobs_ws_bytes(int n_rows, int vocab, int n_top);
+a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows, int vocab, long long ld, const int *tokens, int n_given,
+                            int n_top, float *logprob, float *entropy, int *top_idx, float *top_logprob, void *ws,
+                            size_t ws_bytes, void *stream);
+
 /* ---- tuning values (for tests and measurements; the defaults are what the library picks by itself) -----------
  * Process-wide integers, read when a call is made; value < 0 restores the library's own choice.  Names:
  *   "attn_wgs"        workgroups (shares of the work) per KV head in a3_fused_attention, 1 .. 1024

@@ -19,13 +19,16 @@ A3_OK, A3_ERR_INVALID_ARG, A3_ERR_UNSUPPORTED, A3_ERR_WORKSPACE, A3_ERR_HIP, A3_
 A3_F32, A3_BF16 = 0, 1
 A3_ROPE_INTERLEAVED, A3_ROPE_HALF = 0, 1
 A3_POOL_MAX, A3_POOL_AVG = 0, 1
+A3_PAGES_PLAIN, A3_PAGES_Q8 = 0, 1
 
 EXPORTS = ["a3_workspace_bytes", "a3_layout_prepare", "a3_rope_realign", "a3_question_scores", "a3_question_scores_noalloc", "a3_realign_scores", "a3_topk_select", "a3_topk_select_plan",
            "a3_selected_qkv_proj", "a3_selected_qkv_proj_scatter", "a3_kv_scatter", "a3_fused_attention", "a3_attention_plan", "a3_fused_attention_planned", "a3_fused_attention_planned_events", "a3_active_rows",
            "a3_block_tail_ws_bytes", "a3_block_tail", "a3_rms_norm", "a3_question_scores_causal", "a3_window_votes",
            "a3_evict_ws_bytes", "a3_evict_select", "a3_evict_compact", "a3_value_deviation_scores",
            "a3_select_chunk_edges", "a3_chunk_cache_load", "a3_rope_realign_q8", "a3_q8_row_bytes", "a3_quantize_q8",
-           "a3_chunk_cache_load_q8", "a3_chunk_file_read", "a3_set_tuning", "a3_recompute_count", "a3_chunk_edge_sel_start", "a3_strerror", "a3_last_error", "a3_version"]
+           "a3_chunk_cache_load_q8", "a3_chunk_file_read", "a3_page_bytes", "a3_pages_prepare", "a3_paged_append",
+           "a3_paged_attention_ws_bytes", "a3_paged_attention", "a3_lm_head", "a3_token_logprobs_ws_bytes", "a3_token_logprobs",
+           "a3_set_tuning", "a3_recompute_count", "a3_chunk_edge_sel_start", "a3_strerror", "a3_last_error", "a3_version"]
 
 
 class A3Error(RuntimeError):
@@ -50,6 +53,15 @@ class a3_layout(C.Structure):
 class a3_block_weights(C.Structure):
     _fields_ = [("wo", C.c_void_p), ("g_post", C.c_void_p), ("w_gate", C.c_void_p), ("w_up", C.c_void_p),
                 ("w_down", C.c_void_p), ("g_next", C.c_void_p), ("ffn", C.c_int), ("eps", C.c_float)]
+
+
+class a3_pages(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("format", C.c_int), ("n_q_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+        ("rope_layout", C.c_int), ("rope_base", C.c_double), ("sm_scale", C.c_float), ("page_size", C.c_int),
+        ("n_pages", C.c_int), ("n_req", C.c_int), ("max_pages", C.c_int), ("n_pos", C.c_int),
+        ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("page_table", C.c_void_p), ("rope_cs", C.c_void_p),
+    ]
 
 
 _lib = None
@@ -126,6 +138,20 @@ def lib() -> C.CDLL:
     L.a3_chunk_edge_sel_start.argtypes = [I, C.POINTER(C.c_int), C.POINTER(C.c_int), I, C.POINTER(C.c_int),
                                           C.POINTER(C.c_int), I, I, C.POINTER(C.c_int)]
     L.a3_chunk_edge_sel_start.restype = I
+    G = C.POINTER(a3_pages)
+    L.a3_page_bytes.argtypes = [G]
+    L.a3_page_bytes.restype = C.c_size_t
+    L.a3_pages_prepare.argtypes = [G, V]
+    L.a3_paged_append.argtypes = [G, V, V, V, V, V, I, V, V, V]
+    L.a3_paged_attention_ws_bytes.argtypes = [G, I]
+    L.a3_paged_attention_ws_bytes.restype = C.c_size_t
+    L.a3_paged_attention.argtypes = [G, V, V, V, I, V, V, C.c_size_t, V]
+    L.a3_lm_head.argtypes = [P, V, V, I, V, I, V, C.c_longlong, V]
+    L.a3_token_logprobs_ws_bytes.argtypes = [I, I, I]
+    L.a3_token_logprobs_ws_bytes.restype = C.c_size_t
+    L.a3_token_logprobs.argtypes = [I, V, I, I, C.c_longlong, V, I, I, V, V, V, V, V, C.c_size_t, V]
+    for name in ("a3_pages_prepare", "a3_paged_append", "a3_paged_attention", "a3_lm_head", "a3_token_logprobs"):
+        getattr(L, name).restype = I
     L.a3_set_tuning.argtypes = [C.c_char_p, I]
     L.a3_set_tuning.restype = I
     L.a3_strerror.restype = C.c_char_p
@@ -222,6 +248,13 @@ class Layout:
                    ctx_len=w.ctx_len, q_len=w.q_lens, chunk_start=w.chunk_start, chunk_len=w.chunk_len,
                    chunk_delta=w.chunk_delta, device=device, **kw)
 
+    @classmethod
+    def decode(cls, *, n_req: int, **kw) -> "Layout":
+        """The layout of one decoding step: one row per request, nothing else.  Every row's position in it is 0, so
+        a3_selected_qkv_proj leaves Q and K as projected; a3_paged_append turns them to their positions."""
+        return cls(seg_start=np.arange(n_req + 1), ctx_len=np.zeros(n_req), q_len=np.ones(n_req), chunk_start=[], chunk_len=[],
+                   chunk_delta=[], rope_layout=kw.pop("rope_layout", A3_ROPE_INTERLEAVED), **kw)
+
     @property
     def ref(self):
         return C.byref(self.struct)
@@ -229,6 +262,75 @@ class Layout:
     def workspace(self, max_active_rows: int) -> torch.Tensor:
         n = a3_workspace_bytes(self, max_active_rows)
         return torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
+
+
+class Pages:
+    """One layer's paged K/V cache: two pools, the page table and the position table, and the a3_pages struct that points
+    at them.  ``page_table`` [n_req, max_pages] int32 is the caller's (written as requests grow); pools are allocated unless
+    given.  Pool shapes: [n_pages, Hkv, page_size, d] in the rows' type; 8-bit pages (``q8``): int8 [n_pages, Hkv,
+    page_size * (d + 4)], codes and then float scales."""
+
+    def __init__(self, *, dtype: str, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
+                 page_table: torch.Tensor, rope_base: float, n_pos: int, rope_layout: int = A3_ROPE_INTERLEAVED, q8: bool = False,
+                 sm_scale: float = 0.0, k_pool: Optional[torch.Tensor] = None, v_pool: Optional[torch.Tensor] = None,
+                 rope_cs: Optional[torch.Tensor] = None, stream=None):
+        dev = page_table.device
+        if page_table.dtype != torch.int32 or page_table.dim() != 2:
+            raise ValueError("Pages: page_table is an int32 tensor [n_req, max_pages]")
+        shape = (n_pages, n_kv_heads, page_size * (head_dim + 4)) if q8 else (n_pages, n_kv_heads, page_size, head_dim)
+        dt = torch.int8 if q8 else torch_dtype(dtype)
+        self.dtype, self.q8, self.device, self.page_table = dtype, q8, dev, page_table
+        self.k_pool, self.v_pool = (torch.empty(shape, dtype=dt, device=dev) if p is None else p for p in (k_pool, v_pool))
+        for p in (self.k_pool, self.v_pool):
+            if tuple(p.shape) != shape or p.dtype != dt or p.device != dev:
+                raise ValueError(f"Pages: a pool is {shape} of {dt} on {dev}, got {tuple(p.shape)} of {p.dtype} on {p.device}")
+        fresh = rope_cs is None
+        self.rope_cs = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=dev) if fresh else rope_cs
+        if tuple(self.rope_cs.shape) != (n_pos, head_dim // 2, 2) or self.rope_cs.dtype != torch.float32 or self.rope_cs.device != dev:
+            raise ValueError(f"Pages: rope_cs is float32 {(n_pos, head_dim // 2, 2)} on {dev}")
+        s = a3_pages()
+        s.dtype, s.format = {"f32": A3_F32, "bf16": A3_BF16}[dtype], A3_PAGES_Q8 if q8 else A3_PAGES_PLAIN
+        s.n_q_heads, s.n_kv_heads, s.head_dim = n_q_heads, n_kv_heads, head_dim
+        s.rope_layout, s.rope_base, s.sm_scale = rope_layout, rope_base, sm_scale
+        s.page_size, s.n_pages, s.n_pos = page_size, n_pages, n_pos
+        s.n_req, s.max_pages = page_table.shape
+        s.k_pool, s.v_pool, s.page_table, s.rope_cs = _ptr(self.k_pool), _ptr(self.v_pool), _ptr(page_table), _ptr(self.rope_cs)
+        self.struct = s
+        if fresh:
+            a3_pages_prepare(self, stream)
+
+    def sibling(self) -> "Pages":
+        """Another layer's cache: pools of its own, the same page table and position table."""
+        s = self.struct
+        return Pages(dtype=self.dtype, n_q_heads=s.n_q_heads, n_kv_heads=s.n_kv_heads, head_dim=s.head_dim, page_size=s.page_size,
+                     n_pages=s.n_pages, page_table=self.page_table, rope_base=s.rope_base, n_pos=s.n_pos, rope_layout=s.rope_layout,
+                     q8=self.q8, sm_scale=s.sm_scale, rope_cs=self.rope_cs)
+
+    @property
+    def ref(self):
+        return C.byref(self.struct)
+
+    def workspace(self, n_rows: int) -> torch.Tensor:
+        return torch.empty(max(a3_paged_attention_ws_bytes(self, n_rows), 256), dtype=torch.uint8, device=self.device)
+
+
+class TokenLogprobs:
+    """What a3_token_logprobs writes, and its workspace, allocated once for up to ``n_rows`` rows."""
+
+    def __init__(self, n_rows: int, vocab: int, n_given: int, n_top: int, device="cuda"):
+        new = lambda *s, dtype=torch.float32: torch.empty(s, dtype=dtype, device=device)
+        self.n_given, self.n_top = n_given, n_top
+        self.logprob, self.entropy = new(n_rows, n_given), new(n_rows)
+        self.top_idx, self.top_logprob = new(n_rows, n_top, dtype=torch.int32), new(n_rows, n_top)
+        self.ws = new(max(int(lib().a3_token_logprobs_ws_bytes(n_rows, vocab, n_top)), 256), dtype=torch.uint8)
+
+    def rows(self, first: int, end: int) -> "TokenLogprobs":
+        """Rows first .. end - 1 as outputs of their own, with the same workspace."""
+        part = object.__new__(TokenLogprobs)
+        part.n_given, part.n_top, part.ws = self.n_given, self.n_top, self.ws
+        part.logprob, part.entropy = self.logprob[first:end], self.entropy[first:end]
+        part.top_idx, part.top_logprob = self.top_idx[first:end], self.top_logprob[first:end]
+        return part
 
 
 # ---- entry points (same names as the C ABI) -----------------------------------------------------
@@ -475,3 +577,80 @@ def a3_chunk_file_read(fds, file_offset, n_bytes, host_dst, n_threads: int = 4) 
                                     (C.c_size_t * n)(*[int(b) for b in n_bytes]),
                                     (C.c_void_p * n)(*[t.data_ptr() if t is not None else None for t in host_dst]),
                                     int(n_threads)), "a3_chunk_file_read")
+
+
+# ---- generating on the fused cache -------------------------------------------------------------------
+
+def a3_page_bytes(pages: Pages) -> int:
+    return int(lib().a3_page_bytes(pages.ref))
+
+
+def a3_pages_prepare(pages: Pages, stream=None) -> None:
+    _check(lib().a3_pages_prepare(pages.ref, _stream(stream)), "a3_pages_prepare")
+
+
+def _rows(where: torch.device, n_rows: int, dtype: torch.dtype, elems: int, **tensors) -> None:
+    """Refuses tensors that do not hold ``n_rows`` rows of ``elems`` elements of a type on the device the call runs on."""
+    if where.type != "cuda" or where.index != torch.cuda.current_device():
+        raise ValueError(f"the call's tensors are on {where}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, t in tensors.items():
+        if t is not None and not (t.device == where and t.dtype == dtype and t.dim() and t.shape[0] >= n_rows
+                                  and t.numel() == t.shape[0] * elems):
+            raise ValueError(f"{name}: {n_rows} rows of {elems} {dtype} on {where} are needed, got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def a3_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row_req: Optional[torch.Tensor], row_slot: torch.Tensor,
+                    row_pos: Optional[torch.Tensor], n_rows: int, q: Optional[torch.Tensor] = None,
+                    q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    s, dt = pages.struct, torch_dtype(pages.dtype)
+    _rows(pages.device, n_rows, dt, s.n_kv_heads * s.head_dim, k=k, v=v)
+    _rows(pages.device, n_rows, dt, s.n_q_heads * s.head_dim, q=q, q_out=q_out)
+    _rows(pages.device, n_rows, torch.int32, 1, row_req=row_req, row_slot=row_slot, row_pos=row_pos)
+    _check(lib().a3_paged_append(pages.ref, _ptr(k), _ptr(v), _ptr(row_req), _ptr(row_slot), _ptr(row_pos), int(n_rows), _ptr(q),
+                                 _ptr(q_out), _stream(stream)), "a3_paged_append")
+
+
+def a3_paged_attention_ws_bytes(pages: Pages, n_rows: int) -> int:
+    return int(lib().a3_paged_attention_ws_bytes(pages.ref, int(n_rows)))
+
+
+def a3_paged_attention(pages: Pages, q: torch.Tensor, row_req: Optional[torch.Tensor], row_len: torch.Tensor, n_rows: int,
+                       out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    s = pages.struct
+    _rows(pages.device, n_rows, torch_dtype(pages.dtype), s.n_q_heads * s.head_dim, q=q, out=out)
+    _rows(pages.device, n_rows, torch.int32, 1, row_req=row_req, row_len=row_len)
+    _rows(pages.device, 0, torch.uint8, 1, ws=ws)
+    _check(lib().a3_paged_attention(pages.ref, _ptr(q), _ptr(row_req), _ptr(row_len), int(n_rows), _ptr(out), _ptr(ws),
+                                    ws.numel() if ws is not None else 0, _stream(stream)), "a3_paged_attention")
+
+
+def a3_lm_head(layout: Layout, hidden: torch.Tensor, row_idx: Optional[torch.Tensor], n_rows: int, w: torch.Tensor,
+               logits: torch.Tensor, stream=None) -> None:
+    """``w`` [vocab, hidden]; ``logits`` float32 [>= n_rows, vocab], rows may be further apart than vocab."""
+    dt, h = torch_dtype(layout.dtype), layout.struct.hidden
+    _rows(hidden.device, 0 if row_idx is not None else n_rows, dt, h, hidden=hidden)
+    _rows(hidden.device, 0, dt, h, w=w)
+    _rows(hidden.device, n_rows, torch.int32, 1, row_idx=row_idx)
+    _rows(hidden.device, n_rows, torch.float32, w.shape[0], logits=logits)
+    if logits.dim() != 2 or logits.stride(1) != 1 or logits.stride(0) < logits.shape[1]:
+        raise ValueError("a3_lm_head: logits are rows of consecutive elements")
+    _check(lib().a3_lm_head(layout.ref, _ptr(hidden), _ptr(row_idx), int(n_rows), _ptr(w), int(w.shape[0]), logits.data_ptr(),
+                            logits.stride(0) if logits.shape[0] > 1 else w.shape[0], _stream(stream)), "a3_lm_head")
+
+
+def a3_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], out: TokenLogprobs, stream=None) -> TokenLogprobs:
+    """``logits`` [n_rows, vocab] float32 or bfloat16, rows may be further apart than vocab; ``tokens`` int32
+    [n_rows, out.n_given].  Writes the first n_rows rows of ``out`` and returns it."""
+    n_rows, vocab = logits.shape
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1 or (n_rows > 1 and logits.stride(0) < vocab):
+        raise ValueError("a3_token_logprobs: logits are float32 or bfloat16 rows of consecutive elements")
+    if (tokens is None) != (out.n_given == 0):
+        raise ValueError(f"a3_token_logprobs: tokens are int32 [{n_rows}, {out.n_given}], None for 0 given")
+    where = logits.device
+    _rows(where, n_rows, torch.int32, out.n_given, tokens=tokens)
+    _rows(where, n_rows, torch.float32, 1, entropy=out.entropy)
+    _check(lib().a3_token_logprobs(A3_F32 if logits.dtype == torch.float32 else A3_BF16, logits.data_ptr(), n_rows, vocab,
+                                   logits.stride(0) if n_rows > 1 else vocab, _ptr(tokens), out.n_given, out.n_top,
+                                   _ptr(out.logprob), _ptr(out.entropy), _ptr(out.top_idx), _ptr(out.top_logprob), _ptr(out.ws),
+                                   out.ws.numel(), _stream(stream)), "a3_token_logprobs")
+    return out

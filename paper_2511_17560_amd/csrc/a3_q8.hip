@@ -6,12 +6,11 @@
 // expands the record: the 8-bit data are read once, the realigned keys and the values written once in the
 // storage type.  HBM-bound: 1 byte + 4/d bytes in, 2 (or 4) bytes out per element.
 #include "a3_internal.h"
+#include "a3_q8.h"
 
 namespace {
 
 constexpr int kBlock = 256;
-
-typedef signed char i8x8 __attribute__((ext_vector_type(8)));
 
 __host__ __device__ inline size_t q8_row_bytes(int n_kv_heads, int head_dim) {
   return (size_t)n_kv_heads * (2 * head_dim + 8);
@@ -84,44 +83,15 @@ expand_q8_kernel(const signed char *__restrict__ rows, T *__restrict__ k_out, T 
   }
 }
 
-// The quantiser (run once, when a chunk's caches are produced).  One lane: 16 consecutive coordinates of the
-// key and of the value; the head_dim / 16 lanes of a (row, head) are neighbours in a wave and share the maxima.
-// The scale is the float32 rounding of max|x| / 127 taken in float64 and the code the float64 quotient rounded
-// half to even, so that the integer decision is the same as in a float64 reference.  That division is spared
-// nearly always: n = x * (1 / scale) rounded is at most a step off, and x - n * scale formed in one rounding
-// says whether n is the nearest whole number (rounding is monotone and scale / 2 is a float, so a rounded
-// remainder below scale / 2 is a true one below it).  Only a remainder that is not below (a tie, a quotient
-// within 1e-5 of one, NaN) and scales whose reciprocal a float does not hold take the division.
-// Bound by HBM now: 16448 rows of 8 KV heads (102 MB in and out) 30.4 -> 20.3 us, 5.0 TB/s; a copy reaches 5.2 - 5.35.
-typedef signed char i8x16 __attribute__((ext_vector_type(16), aligned(8)));
-
-__device__ __forceinline__ float quotient_code(float v, float s) {
-  const double r = s > 0.f ? rint((double)v / (double)s) : 0.0;
-  return (float)fmin(fmax(r, -127.0), 127.0);
-}
-
 __device__ __forceinline__ void quantize_run(const float (&v)[16], signed char *__restrict__ dst, float *scale_out,
                                              int per_head, int c) {
   float amax = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(v[e]));
   for (int m = 1; m < per_head; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
-  const float s = (float)((double)amax / 127.0);
+  const float s = q8_scale((double)amax);
   if (c == 0) *scale_out = s;
-  const bool normal = s > 1e-30f && s < 1e30f;
-  const float inv = normal ? __builtin_amdgcn_rcpf(s) : 0.f, half = normal ? 0.5f * s : -1.f;
-  constexpr float kMagic = 12582912.f;                         // 1.5 * 2^23: the sum's low bits are the rounded number
-  uint32_t code[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    float m = fmaf(v[e], inv, kMagic);
-    if (!(fabsf(fmaf(kMagic - m, s, v[e])) < half)) m = kMagic + quotient_code(v[e], s);
-    code[e] = __float_as_uint(m);
-  }
-  i8x16 q;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) q[e] = (signed char)code[e];
-  *reinterpret_cast<i8x16 *>(dst) = q;
+  *reinterpret_cast<i8x16 *>(dst) = q8_codes(v, s);
 }
 
 template <typename T>
@@ -135,6 +105,9 @@ __device__ __forceinline__ void load_run(const T *__restrict__ src, float (&v)[1
   }
 }
 
+// The quantiser (run once, when a chunk's caches are produced).  One lane: 16 consecutive coordinates of the
+// key and of the value; the head_dim / 16 lanes of a (row, head) are neighbours in a wave and share the maxima.
+// Bound by HBM now: 16448 rows of 8 KV heads (102 MB in and out) 30.4 -> 20.3 us, 5.0 TB/s; a copy reaches 5.2 - 5.35.
 template <typename T>
 __global__ void __launch_bounds__(kBlock)
 quantize_q8_kernel(const T *__restrict__ k, const T *__restrict__ v, signed char *__restrict__ rows, long total,

@@ -6,6 +6,7 @@ front of Eq. 3, and Eq. 3-5).  Call sequencing and buffer allocation only; all a
                    Q of the rows [Re, Q] -> attention (Eq. 4) -> H(.)
     layers >= 2    realign the layer's chunk cache (Eq. 2); Q/K/V of the rows [Re, Q] from X_l = H(O_{l-1}),
                    K/V stored into the cache (Eq. 5); attention; H(.)
+    afterwards     one token per request and step: every layer's fused cache goes on as pages that grow (decode_stack)
 """
 from __future__ import annotations
 
@@ -17,9 +18,13 @@ import torch
 from . import api
 
 
+def _bias(lw):
+    return dict(bq=lw.get("bq"), bk=lw.get("bk"), bv=lw.get("bv"))
+
+
 def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor,
                resid: torch.Tensor, k_cat: List[torch.Tensor], v_cat: List[torch.Tensor], sel_start: np.ndarray,
-               q_rows: np.ndarray, stream=None, keep: bool = False, cache_stream=None) -> dict:
+               q_rows: np.ndarray, stream=None, keep: bool = False, cache_stream=None, pages=None) -> dict:
     """``resid`` [T, h] holds the embedding output and is overwritten by the residual stream (all rows after
     block 0, the active rows afterwards).  ``k_cat[l]`` / ``v_cat[l]`` are the chunk caches of layer l >= 2
     (entries 0 and 1 are ignored); ``v_cat[l]`` is updated in place.  Every layer dict holds wq, wk, wv, wo,
@@ -27,6 +32,8 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     With ``cache_stream`` (a loader.ChunkCacheStream) the caches are not resident: layer l's blocks are copied
     from host memory into a ring of device buffers while the layers before it compute, and ``k_cat`` / ``v_cat``
     are ignored; its blocks may be 8-bit (position recovery and dequantisation then run in one kernel).
+    ``pages`` (one api.Pages per layer, a request of theirs for each of the layout's) receives every layer's fused cache,
+    token p of a request in slot p, so that decode_stack can go on.
     Returns dict(sel_idx, act_idx, n_act, scores, resid, hidden): ``hidden`` [T, h] holds the final-normed
     output at the active rows.  With ``keep`` every layer's attention output, caches, residual stream and the
     hidden states handed to the next layer are kept too (``per_layer[l]``: k, v, out, resid, x_next; whole arrays
@@ -54,8 +61,9 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
         api.a3_block_tail(layout, out, idx, n, lw["wo"], lw["g_post"], lw["w_gate"], lw["w_up"], lw["w_down"],
                           g_next(l), eps, resid, x, ws_tail, stream=stream)
 
-    def bias(lw):
-        return dict(bq=lw.get("bq"), bk=lw.get("bk"), bv=lw.get("bv"))
+    def to_pages(l, k, v):
+        if pages is not None:
+            api.a3_paged_append(pages[l], k, v, layout.tok_req, layout.tok_pos, None, T, stream=stream)
 
     if cache_stream is not None:
         for l in range(2, min(2 + cache_stream.depth, n_layers)):
@@ -70,8 +78,9 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     q_all = torch.empty((T, Hq, d), dtype=dt, device=dev)
     out_all = torch.empty((T, Hq, d), dtype=dt, device=dev)
     api.a3_selected_qkv_proj_scatter(layout, x, None, T, lw["wq"], lw["wk"], lw["wv"], q_out=q_all, k_fused=k_l,
-                                     v_fused=v_l, stream=stream, **bias(lw))
+                                     v_fused=v_l, stream=stream, **_bias(lw))
     api.a3_fused_attention(layout, q_all, all_idx, T, k_l, v_l, out_all, ws_attn, stream=stream)
+    to_pages(0, k_l, v_l)
     tail(0, out_all, None, T)
     if keep:
         kept.append(dict(k=k_l.clone(), v=v_l.clone(), out=out_all.clone(), resid=resid.clone(), x_next=x.clone()))
@@ -88,7 +97,7 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     q_act = torch.empty((max(n_act, 1), Hq, d), dtype=dt, device=dev)
     out = out_all[:max(n_act, 1)]
     api.a3_selected_qkv_proj_scatter(layout, x, None, T, None, lw["wk"], lw["wv"], k_fused=k_l, v_fused=v_l,
-                                     stream=stream, **bias(lw))
+                                     stream=stream, **_bias(lw))
     api.a3_selected_qkv_proj(layout, x, q_rows_d, nq, lw["wq"], None, None, bq=lw.get("bq"), q_out=q_question,
                              stream=stream)
     api.a3_question_scores(layout, q_question, k_l, scores, ws_attn, stream=stream)
@@ -98,6 +107,7 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     api.a3_selected_qkv_proj(layout, x, act_idx, n_act, lw["wq"], None, None, bq=lw.get("bq"), q_out=q_act,
                              stream=stream)
     api.a3_fused_attention_planned(layout, q_act, act_idx, n_act, k_l, v_l, out, ws_attn, stream=stream)
+    to_pages(1, k_l, v_l)
     tail(1, out, act_idx, n_act)
     act_long = act_idx[:n_act].long()
     if keep:
@@ -116,8 +126,9 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
             k_c, v_c = (k_cat[l], v_cat[l]) if cache_stream is None else cache_stream.acquire(l, stream)
             api.a3_rope_realign(layout, k_c, k_l, stream=stream)
         api.a3_selected_qkv_proj_scatter(layout, x, act_idx, n_act, lw["wq"], lw["wk"], lw["wv"], q_out=q_act,
-                                         k_fused=k_l, v_fused=v_c, stream=stream, **bias(lw))
+                                         k_fused=k_l, v_fused=v_c, stream=stream, **_bias(lw))
         api.a3_fused_attention_planned(layout, q_act, act_idx, n_act, k_l, v_c, out, ws_attn, stream=stream)
+        to_pages(l, k_l, v_c)
         if keep:
             kept.append(dict(k=k_l.clone(), v=v_c.clone(), out=out[:n_act].clone()))
         if cache_stream is not None and not cache_stream.q8:
@@ -131,10 +142,11 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
 
 
 def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor,
-                  resid: torch.Tensor, stream=None, keep_kv: bool = False) -> dict:
+                  resid: torch.Tensor, stream=None, keep_kv: bool = False, pages=None) -> dict:
     """Every block on every row: the plain prefill the schedule above is measured against (and, run on one
     chunk alone, the precompute of Eq. 1 that produces a chunk's per-layer K/V).  ``resid`` [T, h] holds the
-    embedding output and is overwritten.  Returns dict(resid, hidden, k=[...], v=[...] if keep_kv)."""
+    embedding output and is overwritten.  ``pages`` as in fuse_stack.  Returns dict(resid, hidden, k=[...], v=[...] if
+    keep_kv)."""
     dev, dt = layout.device, api.torch_dtype(layout.dtype)
     T, h = layout.total_tokens, shape.hidden
     Hq, Hkv, d = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
@@ -154,10 +166,11 @@ def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Te
     for l, lw in enumerate(layers):
         if keep_kv and l > 0:
             k_l, v_l = torch.empty_like(k_l), torch.empty_like(v_l)
-        api.a3_selected_qkv_proj_scatter(layout, x, None, T, lw["wq"], lw["wk"], lw["wv"], bq=lw.get("bq"),
-                                         bk=lw.get("bk"), bv=lw.get("bv"), q_out=q_all, k_fused=k_l, v_fused=v_l,
-                                         stream=stream)
+        api.a3_selected_qkv_proj_scatter(layout, x, None, T, lw["wq"], lw["wk"], lw["wv"], q_out=q_all, k_fused=k_l,
+                                         v_fused=v_l, stream=stream, **_bias(lw))
         api.a3_fused_attention(layout, q_all, all_idx, T, k_l, v_l, out_all, ws_attn, stream=stream)
+        if pages is not None:
+            api.a3_paged_append(pages[l], k_l, v_l, layout.tok_req, layout.tok_pos, None, T, stream=stream)
         g_next = layers[l + 1]["g_in"] if l + 1 < n_layers else g_final
         api.a3_block_tail(layout, out_all, None, T, lw["wo"], lw["g_post"], lw["w_gate"], lw["w_up"], lw["w_down"],
                           g_next, eps, resid, x, ws_tail, stream=stream)
@@ -165,3 +178,59 @@ def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Te
             ks.append(k_l)
             vs.append(v_l)
     return dict(resid=resid, hidden=x, k=ks, v=vs)
+
+
+class DecodeBuffers:
+    """What one decoding step of up to ``layout.n_req`` rows writes, allocated once (a captured graph keeps using them).
+    ``layout`` is an api.Layout.decode; ``pages`` one api.Pages per layer; ``vocab`` > 0 asks for logits too."""
+
+    def __init__(self, layout: api.Layout, shape, ffn: int, pages: Sequence[api.Pages], vocab: int = 0):
+        dev, dt, n = layout.device, api.torch_dtype(layout.dtype), layout.n_req
+        new = lambda *s: torch.empty(s, dtype=dt, device=dev)
+        self.x = new(n, shape.hidden)
+        self.q, self.out = new(n, shape.n_q_heads, shape.head_dim), new(n, shape.n_q_heads, shape.head_dim)
+        self.k, self.v = new(n, shape.n_kv_heads, shape.head_dim), new(n, shape.n_kv_heads, shape.head_dim)
+        self.ws_attn = pages[0].workspace(n)
+        self.ws_tail = torch.empty(max(api.a3_block_tail_ws_bytes(layout, ffn, n), 256), dtype=torch.uint8, device=dev)
+        self.logits = torch.empty((n, vocab), dtype=torch.float32, device=dev) if vocab else None
+
+
+def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor,
+                 resid: torch.Tensor, pages: Sequence[api.Pages], row_slot: torch.Tensor, row_pos: torch.Tensor,
+                 row_len: torch.Tensor, bufs: DecodeBuffers, row_req=None, w_vocab=None, stream=None) -> dict:
+    """One new token per row through every block.  ``resid`` [n_req, h] holds the tokens' embeddings and is overwritten by
+    the residual stream.  Row i belongs to request ``row_req[i]`` of the pages (None: i); its K and V go to slot
+    ``row_slot[i]``, turned to position ``row_pos[i]``, and it sees the slots below ``row_len[i]`` (its own included: row_slot +
+    1).  All four are device int32, so that a captured step is replayed with the next values in them; a row whose request
+    is -1 is padding: no cache row is written for it and its outputs mean nothing.  ``w_vocab`` [vocab, h]: logits of every
+    row too.  Returns dict(hidden, resid, logits)."""
+    n, eps, b = layout.n_req, float(shape.rms_eps), bufs
+    api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
+    for l, lw in enumerate(layers):
+        api.a3_selected_qkv_proj(layout, b.x, None, n, lw["wq"], lw["wk"], lw["wv"], q_out=b.q, k_out=b.k, v_out=b.v,
+                                 stream=stream, **_bias(lw))
+        api.a3_paged_append(pages[l], b.k, b.v, row_req, row_slot, row_pos, n, q=b.q, q_out=b.q, stream=stream)
+        api.a3_paged_attention(pages[l], b.q, row_req, row_len, n, b.out, b.ws_attn, stream=stream)
+        g_next = layers[l + 1]["g_in"] if l + 1 < len(layers) else g_final
+        api.a3_block_tail(layout, b.out, None, n, lw["wo"], lw["g_post"], lw["w_gate"], lw["w_up"], lw["w_down"], g_next, eps,
+                          resid, b.x, b.ws_tail, stream=stream)
+    if w_vocab is not None:
+        api.a3_lm_head(layout, b.x, None, n, w_vocab, b.logits, stream=stream)
+    return dict(hidden=b.x, resid=resid, logits=b.logits if w_vocab is not None else None)
+
+
+def score_tokens(layout: api.Layout, hidden: torch.Tensor, row_idx, n_rows: int, w_vocab: torch.Tensor, tokens,
+                 out: api.TokenLogprobs, rows_at_once: int = 1024, stream=None) -> api.TokenLogprobs:
+    """Log probabilities of given tokens (and entropy, alternatives) behind rows of final-normed hidden states, as fuse_stack,
+    prefill_stack and decode_stack return them: ``tokens`` int32 [n_rows, out.n_given] beside the packed rows ``row_idx`` (None:
+    the first n_rows).  The logits of ``rows_at_once`` rows at a time are formed and read (1024 rows of 128256: 0.5 GB)."""
+    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):      # the logits live and die on it
+        logits = torch.empty((min(max(n_rows, 1), rows_at_once), w_vocab.shape[0]), dtype=torch.float32, device=hidden.device)
+        for i in range(0, n_rows, rows_at_once):
+            m = min(rows_at_once, n_rows - i)
+            if row_idx is None:
+                api.a3_lm_head(layout, hidden[i:i + m], None, m, w_vocab, logits[:m])
+            else:
+                api.a3_lm_head(layout, hidden, row_idx[i:i + m], m, w_vocab, logits[:m])
+            api.a3_token_logprobs(logits[:m], None if tokens is None else tokens[i:i + m], out.rows(i, i + m))
+    return out

@@ -1,0 +1,213 @@
+"""Generating on the fused cache as a run: prompt -> pages -> decoding steps -> log probabilities, against the float64 stack oracle.
+
+Tolerances: those of the stack's tests for the same number of blocks (tests/test_gpu_stack.py): fp32 1e-4, bf16 2e-2 of the
+tensor's largest value; a decoding step stores one tensor more per block than the prefill (Q and K before they are turned)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import generate_oracle as gen
+from oracle import stack_oracle as st
+import a3_synth as synth
+from paper_2511_17560_amd import api, stack
+from gpu_util import idev, max_abs_rel, to_dev, to_host
+from paged_util import get, make_pages
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = {"f32": synth.ModelShape("gen-f32", "f32", 256, 8, 2, 64, 1e4, synth.ROPE_INTERLEAVED, ffn=384),
+          "bf16": synth.ModelShape("gen-bf16", "bf16", 512, 8, 2, 128, 5e5, synth.ROPE_HALF, ffn=768)}
+
+
+def _setup(dtype, lens, n_layers=3, seed=3, **kw):
+    """A batch of prompts, each one chunk and a question, with stack weights, and pages for 40 more tokens."""
+    shape = SHAPES[dtype]
+    w = synth.custom(shape, [[n - 4] if n > 4 else [] for n in lens], [min(4, n) for n in lens], seed=seed, **kw)
+    sw = synth.draw_stack_weights(w, n_layers)
+    layers = [{k: to_dev(v, dtype) for k, v in lw.items()} for lw in sw["layers"]]
+    return shape, w, sw, layers
+
+
+def _pages(shape, lens, n_layers, q8=False, seed=0):
+    p = make_pages([n + 40 for n in lens], dtype=shape.dtype, Hq=shape.n_q_heads, Hkv=shape.n_kv_heads, d=shape.head_dim, page=32,
+                   base=shape.rope_base, layout=shape.rope_layout, q8=q8, seed=seed)
+    pages = [p] + [p.sibling() for _ in range(n_layers - 1)]
+    for s in pages[1:]:
+        s.k_pool.copy_(p.k_pool)
+        s.v_pool.copy_(p.v_pool)
+    return pages
+
+
+def _oracle(shape, sw, embeddings):
+    """Every block on every row of whole texts: hidden states [sum lens, h]."""
+    lens = [len(e) for e in embeddings]
+    layers = [{k: v.astype(np.float64) for k, v in lw.items()} for lw in sw["layers"]]
+    sd = dict(n_q_heads=shape.n_q_heads, n_kv_heads=shape.n_kv_heads, head_dim=shape.head_dim, base=shape.rope_base, layout=shape.rope_layout,
+              sm_scale=shape.head_dim ** -0.5, eps=shape.rms_eps)
+    pos = np.concatenate([np.arange(n) for n in lens])
+    r = st.full_prefill_stack(np.concatenate(embeddings), pos, np.concatenate([[0], np.cumsum(lens)]), layers, sw["g_final"].astype(np.float64),
+                              sd, shape.dtype)
+    return np.split(r["hidden"], np.cumsum(lens)[:-1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompt_then_tokens(dtype):
+    """A prefill, then five decoding steps of the batch, is the prefill of the longer texts; and their log probabilities."""
+    lens, steps, tol = [70, 1, 33, 5], 5, 1e-4 if dtype == "f32" else 2e-2
+    shape, w, sw, layers = _setup(dtype, lens)
+    rng = np.random.default_rng(1)
+    new = synth.round_to_storage(rng.standard_normal((steps, len(lens), shape.hidden), dtype=np.float32), dtype)
+    lay, pages, g = api.Layout.from_workload(w), _pages(shape, lens, 3), to_dev(sw["g_final"], dtype)
+    pre = stack.prefill_stack(lay, shape, layers, g, to_dev(sw["resid0"], dtype), pages=pages)
+    dlay = api.Layout.decode(dtype=dtype, n_q_heads=shape.n_q_heads, n_kv_heads=shape.n_kv_heads, head_dim=shape.head_dim, hidden=shape.hidden,
+                             rope_base=shape.rope_base, n_req=len(lens))
+    vocab = 501
+    w_vocab = synth.round_to_storage(0.1 * rng.standard_normal((vocab, shape.hidden), dtype=np.float32), dtype)
+    wv = to_dev(w_vocab, dtype)
+    bufs = stack.DecodeBuffers(dlay, shape, shape.ffn, pages, vocab)
+    slot = idev(lens)
+    length = slot + 1
+    hidden, logits = [], []
+    for t in range(steps):
+        r = stack.decode_stack(dlay, shape, layers, g, to_dev(new[t], dtype), pages, slot, slot, length, bufs, w_vocab=wv)
+        slot += 1
+        length += 1
+        hidden.append(to_host(r["hidden"]))
+        logits.append(to_host(r["logits"]))
+    texts = [np.concatenate([sw["resid0"][a:a + n], new[:, i]]).astype(np.float64) for i, (a, n) in enumerate(zip(w.seg_start, lens))]
+    want = _oracle(shape, sw, texts)
+    for i, n in enumerate(lens):
+        assert max_abs_rel(to_host(pre["hidden"])[w.seg_start[i]:w.seg_start[i] + n], want[i][:n]) <= tol
+        assert max_abs_rel(np.stack([h[i] for h in hidden]), want[i][n:]) <= tol
+        assert max_abs_rel(np.stack([l[i] for l in logits]), want[i][n:] @ w_vocab.T.astype(np.float64)) <= tol
+    # rating tokens behind the prompt's rows: in one piece and in pieces of 30 rows, the same
+    T = w.total_tokens
+    tokens = idev(rng.integers(0, vocab, (T, 2)))
+    whole = stack.score_tokens(lay, pre["hidden"], None, T, wv, tokens, api.TokenLogprobs(T, vocab, 2, 4))
+    x = to_host(pre["hidden"]) @ w_vocab.T.astype(np.float64)
+    lp = gen.log_probs(x)
+    assert np.abs(to_host(whole.logprob) - gen.given(lp, tokens.cpu().numpy())).max() <= 1e-4
+    assert np.abs(to_host(whole.entropy) - gen.entropy(lp)).max() <= 1e-4
+    assert np.mean(whole.top_idx.cpu().numpy() != gen.top(x, 4)) < 0.01            # (near ties may change places)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for idx in (None, torch.arange(T, dtype=torch.int32, device="cuda")):
+        part = stack.score_tokens(lay, pre["hidden"], idx, T, wv, tokens, api.TokenLogprobs(T, vocab, 2, 4), rows_at_once=30, stream=side)
+        side.synchronize()
+        assert np.abs(to_host(part.logprob) - to_host(whole.logprob)).max() <= 1e-5
+        assert np.mean((part.top_idx != whole.top_idx).cpu().numpy()) < 0.01
+
+
+def test_fused_prompt_goes_on_as_pages():
+    """fuse_stack hands every layer's fused cache on, 8-bit and not; its own results are what they are without pages."""
+    dtype, n_layers = "bf16", 4
+    shape = SHAPES[dtype]
+    w = synth.custom(shape, [[60, 40], [50, 33]], [9, 6], ratio=(15, 100), seed=5)
+    sw = synth.draw_stack_weights(w, n_layers)
+    layers = [{k: to_dev(v, dtype) for k, v in lw.items()} for lw in sw["layers"]]
+    lay, T = api.Layout.from_workload(w), w.total_tokens
+    rng = np.random.default_rng(2)
+    caches = [[None, None] + [synth.round_to_storage(rng.standard_normal((T, 2, 128), dtype=np.float32), dtype) for _ in range(n_layers - 2)] for _ in "kv"]
+
+    def fuse(pages):
+        k, v = ([None if c is None else to_dev(c, dtype) for c in cs] for cs in caches)
+        return stack.fuse_stack(lay, shape, layers, to_dev(sw["g_final"], dtype), to_dev(sw["resid0"], dtype), k, v, w.sel_start, w.question_rows(),
+                                keep=True, pages=pages)
+
+    lens = np.diff(w.seg_start).tolist()
+    plain = fuse(None)
+    for q8_pages in (False, True):
+        pages = _pages(shape, lens, n_layers, q8=q8_pages)
+        got = fuse(pages)
+        torch.cuda.synchronize()
+        rows = plain["act_idx"].long()
+        assert torch.equal(got["act_idx"], plain["act_idx"]) and torch.equal(got["hidden"][rows], plain["hidden"][rows])
+        for l in range(n_layers):
+            for r in range(2):
+                a, b = int(w.seg_start[r]), int(w.seg_start[r + 1])
+                for x, kept in zip(get(pages[l], r, 0, b - a), (got["per_layer"][l]["k"], got["per_layer"][l]["v"])):
+                    kept = to_host(kept)[a:b]
+                    if q8_pages:
+                        assert np.abs(x - kept).max() <= np.abs(kept).max() / 127 * 0.5 * 1.001
+                    else:
+                        assert np.array_equal(x, kept)
+
+
+def test_decoding_step_captured_with_a_padding_row():
+    """The step as one graph, replayed with the next slots, is the eager step; a padding row writes nothing into the cache."""
+    dtype, lens = "bf16", [40, 7, 90]
+    shape, w, sw, layers = _setup(dtype, lens)
+    lay, g = api.Layout.from_workload(w), to_dev(sw["g_final"], dtype)
+    dlay = api.Layout.decode(dtype=dtype, n_q_heads=shape.n_q_heads, n_kv_heads=shape.n_kv_heads, head_dim=shape.head_dim, hidden=shape.hidden,
+                             rope_base=shape.rope_base, n_req=4)
+    rng = np.random.default_rng(7)
+    new = to_dev(synth.round_to_storage(rng.standard_normal((4, 4, shape.hidden), dtype=np.float32), dtype), dtype)
+    req = idev([0, 1, -1, 2])
+    runs = []
+    for captured in (False, True):
+        pages = _pages(shape, lens, 3)
+        stack.prefill_stack(lay, shape, layers, g, to_dev(sw["resid0"], dtype), pages=pages)
+        bufs = stack.DecodeBuffers(dlay, shape, shape.ffn, pages)
+        bufs.out.zero_()
+        slot, length, resid = idev([40, 7, 3, 90]), idev([41, 8, 4, 91]), torch.empty_like(new[0])
+        step = lambda: stack.decode_stack(dlay, shape, layers, g, resid, pages, slot, slot, length, bufs, row_req=req)
+        graph = None
+        if captured:
+            saved = [(p.k_pool.clone(), p.v_pool.clone()) for p in pages]
+            resid.copy_(new[0])
+            step()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+            for p, (k, v) in zip(pages, saved):
+                p.k_pool.copy_(k)
+                p.v_pool.copy_(v)
+        out = []
+        for t in range(4):
+            resid.copy_(new[t])
+            graph.replay() if captured else step()
+            torch.cuda.synchronize()
+            out.append(bufs.x[[0, 1, 3]].clone())
+            slot += 1
+            length += 1
+        runs.append((torch.stack(out), [torch.cat([p.k_pool, p.v_pool]).nan_to_num(12345.0) for p in pages]))
+    assert torch.equal(runs[0][0], runs[1][0])
+    assert all(torch.equal(a, b) for a, b in zip(runs[0][1], runs[1][1]))
+    # request 1 had slots 7 .. 10 written and not slot 3 of the padding row's number
+    k, _ = get(pages[0], 1, 0, 11)
+    assert np.isfinite(k).all() and np.isnan(get(pages[0], 1, 11, 12)[0]).all()
+
+
+def test_evicted_cache_goes_on():
+    """Votes, retention and compaction, then the retained rows as pages (slots are not positions), a new token and its attention."""
+    shape = synth.ModelShape("evict", "bf16", 256, 8, 2, 128, 1e4)
+    w = synth.custom(shape, [[100, 80], [90]], [8, 5], seed=11)
+    lay, T = api.Layout.from_workload(w), w.total_tokens
+    rng = np.random.default_rng(12)
+    val = lambda *s: synth.round_to_storage(rng.standard_normal(s, dtype=np.float32), "bf16")
+    k, v, qq = val(T, 2, 128), val(T, 2, 128), val(13, 8, 128)
+    keep = np.array([0, 64, 64 + 40])
+    kd, vd = to_dev(k, "bf16"), to_dev(v, "bf16")
+    votes, kept = torch.zeros((2, T), device="cuda"), torch.zeros((2, 104), dtype=torch.int32, device="cuda")
+    api.a3_window_votes(lay, to_dev(qq, "bf16"), kd, votes, lay.workspace(0))
+    api.a3_evict_select(lay, votes, idev([4, 4]), idev(keep), 104, kept)
+    k_out, v_out = (torch.empty((104, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    api.a3_evict_compact(lay, kd, vd, kept, 104, k_out, v_out)
+    p = make_pages([65, 41], page=32, n_pos=200, Hq=8, Hkv=2)
+    req, slot = idev(np.repeat([0, 1], [64, 40])), idev(np.concatenate([np.arange(64), np.arange(40)]))
+    api.a3_paged_append(p, k_out, v_out, req, slot, None, 104)
+    nk, nv, nq = val(2, 2, 128), val(2, 2, 128), val(2, 8, 128)
+    qd, pos = to_dev(nq, "bf16"), np.diff(w.seg_start)
+    api.a3_paged_append(p, to_dev(nk, "bf16"), to_dev(nv, "bf16"), None, idev([64, 40]), idev(pos), 2, q=qd, q_out=qd)
+    out = torch.empty_like(qd)
+    api.a3_paged_attention(p, qd, None, idev([65, 41]), 2, out, p.workspace(2))
+    torch.cuda.synchronize()
+    idx, q = kept.cpu().numpy(), gen.turn(nq, pos, 1e4, 0, "bf16")
+    turned = gen.turn(nk, pos, 1e4, 0, "bf16")
+    for r in range(2):
+        rows = idx[:, keep[r]:keep[r + 1]]
+        kk = np.concatenate([np.stack([k[rows[h], h] for h in range(2)], 1), turned[r:r + 1]])
+        vv = np.concatenate([np.stack([v[rows[h], h] for h in range(2)], 1), nv[r:r + 1]])
+        want = gen.attend(q[r], kk, vv, 128 ** -0.5)
+        assert np.abs(to_host(out)[r] - want).max() <= (2.0 ** -8 * 2 + 1e-3) * np.abs(vv).max()

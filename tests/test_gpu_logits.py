@@ -1,0 +1,183 @@
+"""The product with the vocabulary's weights and log probabilities, against float64.
+
+Tolerances.  Logits: bf16 products are exact in float32 and their sum of h terms is off by at most h * 2^-24 sum |x w|; roundings are
+independent, and 8 sqrt(h) 2^-24 sum |x w| leaves eight deviations.  Log probabilities: x - m is off by 2^-24 |x - m|, the sum Z of
+positive terms by the float32 exponentials' error (2 units and the argument's rounding times |x - m|) and its summation (a few
+hundred terms a lane): relative 2^-24 * (|x - m| + 64), which log Z and the entropy's quotient carry over.  With |x - m| < 64 here:
+1e-5 of (1 + |value|)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import generate_oracle as gen
+from paper_2511_17560_amd import api
+from gpu_util import idev, to_dev, to_host
+import a3_synth as synth
+
+pytestmark = pytest.mark.gpu
+
+
+def _layout(dtype, h, T):
+    return api.Layout.decode(dtype=dtype, n_q_heads=2, n_kv_heads=1, head_dim=128 if dtype == "bf16" else 64, hidden=h, rope_base=1e4, n_req=T)
+
+
+def _values(rng, dtype, *shape):
+    return synth.round_to_storage(rng.standard_normal(shape, dtype=np.float32), dtype).astype(np.float64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h,vocab,n", [(64, 1, 1), (512, 17, 3), (128, 1000, 1), (192, 4099, 5), (512, 2048, 16), (1024, 513, 17), (256, 777, 64),
+                                       (320, 1025, 65), (256, 640, 130), (128, 260, 300), (4096, 600, 2), (3584, 100, 33)])
+def test_lm_head(dtype, h, vocab, n):
+    rng = np.random.default_rng(vocab + n)
+    T = n + 3
+    lay, x, w = _layout(dtype, h, T), _values(rng, dtype, T, h), _values(rng, dtype, vocab, h)
+    idx = rng.integers(0, T, n)
+    wide = torch.full((n, vocab + 5), 7.0, device="cuda")           # rows further apart than vocab: the rest stays
+    for row_idx, logits in ((None, torch.full((n, vocab), 7.0, device="cuda")), (idx, wide[:, :vocab])):
+        rows = np.arange(n) if row_idx is None else row_idx
+        xd, wd = to_dev(x, dtype), to_dev(w, dtype)
+        _call_lm_head(lay, xd, row_idx, n, wd, logits)
+        torch.cuda.synchronize()
+        want, size = x[rows] @ w.T, np.abs(x[rows]) @ np.abs(w).T
+        assert np.all(np.abs(to_host(logits) - want) <= 8 * np.sqrt(h) * 2.0 ** -24 * size)
+    assert bool((wide[:, vocab:] == 7.0).all())
+
+
+def _call_lm_head(lay, x, row_idx, n, w, logits):
+    api.a3_lm_head(lay, x, None if row_idx is None else idev(row_idx), n, w, logits)
+
+
+def test_lm_head_rows_do_not_mix():
+    """NaN and infinities in one row stay in its logits; a NaN weight row stays in its column."""
+    rng = np.random.default_rng(1)
+    h, vocab, n = 256, 300, 20
+    lay, x, w = _layout("bf16", h, n), _values(rng, "bf16", n, h), _values(rng, "bf16", vocab, h)
+    xb, wb = x.copy(), w.copy()
+    xb[3, 7], wb[299, 0] = np.nan, np.nan
+    logits = torch.empty((n, vocab), device="cuda")
+    _call_lm_head(lay, to_dev(xb, "bf16"), None, n, to_dev(wb, "bf16"), logits)
+    torch.cuda.synchronize()
+    got, ok = to_host(logits), np.ones((n, vocab), bool)
+    ok[3], ok[:, 299] = False, False
+    assert np.isnan(got[~ok]).all() and np.abs(got[ok] - (x @ w.T)[ok]).max() < 1e-3
+
+
+def _logprobs(x, tokens, n_top, ld=None, dtype="f32"):
+    n, vocab = x.shape
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    wide = torch.full((n, ld or vocab), float("nan"), dtype=t, device="cuda")
+    wide[:, :vocab] = torch.from_numpy(x).to(t).cuda()
+    tok = None if tokens is None else idev(tokens)
+    out = api.TokenLogprobs(n, vocab, 0 if tokens is None else tok.shape[1], n_top)
+    for o in (out.logprob, out.entropy, out.top_logprob):
+        o.fill_(77.0)
+    out.ws.fill_(255)
+    api.a3_token_logprobs(wide[:, :vocab], tok, out)
+    torch.cuda.synchronize()
+    return out, wide[:, :vocab].double().cpu().numpy()
+
+
+def _close(got, want):
+    got, want = to_host(got), np.asarray(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf])
+    ok = np.isfinite(want)
+    assert np.all(np.abs(got[ok] - want[ok]) <= 1e-5 * (1 + np.abs(want[ok]))), np.abs(got[ok] - want[ok]).max()
+
+
+def _check(x, tokens, n_top, **kw):
+    out, x = _logprobs(x, tokens, n_top, **kw)
+    lp = gen.log_probs(x)
+    _close(out.entropy, gen.entropy(lp))
+    if tokens is not None:
+        _close(out.logprob, gen.given(lp, tokens))
+    if n_top:
+        idx = gen.top(x, n_top)
+        assert np.array_equal(out.top_idx.cpu().numpy(), idx)
+        _close(out.top_logprob, np.take_along_axis(lp, idx, -1))
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,ld,n_top", [(1, 1, 1, 1), (1, 2, 9, 2), (3, 63, 63, 5), (2, 64, 64, 64), (5, 65, 67, 64), (1, 1000, 1000, 20),
+                                              (7, 4099, 4099, 20), (2, 8191, 8195, 1), (3, 8193, 8193, 33), (1, 128256, 128256, 20),
+                                              (2, 152065, 152065, 64), (600, 777, 778, 3), (1, 70001, 70001, 0)])
+def test_logprobs(dtype, n, vocab, ld, n_top):
+    rng = np.random.default_rng(n + vocab)
+    x = rng.standard_normal((n, vocab)) * 3
+    tokens = rng.integers(0, vocab, (n, 3))
+    _check(x, tokens, n_top, ld=ld, dtype=dtype)
+
+
+@pytest.mark.parametrize("vocab", [500, 9001, 128256])
+def test_ties_and_order(vocab):
+    """Equal logits by the lower index: constant rows, two values, rows in ascending and in descending order, -0 beside 0."""
+    rng = np.random.default_rng(3)
+    rows = [np.zeros(vocab), rng.integers(0, 2, vocab).astype(float), np.arange(vocab) / vocab, -np.arange(vocab) / vocab,
+            np.where(np.arange(vocab) % 2, 0.0, -0.0), np.where(np.arange(vocab) == vocab - 1, 1.0, -5.0),
+            np.where(np.arange(vocab) % 64 == 5, 2.0, -1.0), np.where(np.arange(vocab) // 64 == 3, 2.0 + np.arange(vocab) % 64 / 64, -1.0)]
+    x = np.stack(rows).astype(np.float32).astype(np.float64)
+    for n_top in (1, 20, 64):
+        _check(x, None, n_top)
+        _check(x, None, n_top, dtype="bf16")
+
+
+def test_masked_and_broken_rows():
+    """-inf logits: probability 0, last among the alternatives; the lowest finite value; NaN, +inf or nothing at all: no distribution."""
+    rng = np.random.default_rng(4)
+    V, low = 5000, float(np.finfo(np.float32).min)
+    x = rng.standard_normal((9, V))
+    x[0, 10:] = -np.inf
+    x[1] = -np.inf
+    x[2, 77] = np.nan
+    x[3, 78] = np.inf
+    x[4] = -np.inf
+    x[4, 4321] = 3.0
+    x[5, 1:] = low
+    x[6] = low
+    x[7] = np.nan
+    x[8, ::2] = -np.inf
+    tokens = np.tile([[5, 10, 4321, -1, V, 2 ** 31 - 1]], (9, 1))
+    out = _check(x, tokens, 16)
+    assert to_host(out.logprob)[4, 2] == 0.0 and to_host(out.entropy)[4] == 0.0
+
+
+def test_entropy_may_be_left_out_and_rows_may_be_none():
+    L = api.lib()
+    x = torch.randn(2, 100, device="cuda")
+    tok, lp, ws = idev([[3], [4]]), torch.full((2, 1), 7.0, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    assert L.a3_token_logprobs(api.A3_F32, x.data_ptr(), 2, 100, 100, tok.data_ptr(), 1, 0, lp.data_ptr(), None, None, None, ws.data_ptr(),
+                               ws.numel(), st) == api.A3_OK
+    torch.cuda.synchronize()
+    _close(lp, gen.given(gen.log_probs(x.double().cpu().numpy()), [[3], [4]]))
+
+
+def test_captured_logits_and_logprobs():
+    rng = np.random.default_rng(6)
+    lay, h, V, n = _layout("bf16", 512, 8), 512, 3001, 5
+    xs = [_values(rng, "bf16", 8, h) for _ in range(3)]
+    w, xd = to_dev(_values(rng, "bf16", V, h), "bf16"), to_dev(xs[0], "bf16")
+    logits, tok, out = torch.empty((n, V), device="cuda"), idev(rng.integers(0, V, (n, 2))), api.TokenLogprobs(n, V, 2, 5)
+
+    def step():
+        api.a3_lm_head(lay, xd, None, n, w, logits)
+        api.a3_token_logprobs(logits, tok, out)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for x in xs + xs[:1]:
+        xd.copy_(to_dev(x, "bf16"))
+        step()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (logits, out.logprob, out.entropy, out.top_idx, out.top_logprob)]
+        for t in (logits, out.logprob, out.entropy, out.top_idx, out.top_logprob):
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (logits, out.logprob, out.entropy, out.top_idx, out.top_logprob)))
