@@ -152,81 +152,477 @@ paged_append_kernel(append_args a) {
 // ---------------------------------------------------------------------------------------
 // attention of single tokens
 // ---------------------------------------------------------------------------------------
-// One workgroup per (row, query head), 256 slots a step: every thread scores one slot, then sums one coordinate over the 256.
+// Eight codes as bf16 (whole numbers up to 127: exact, the high half of the float).
+__device__ __forceinline__ uint32_t pack_codes(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+__device__ __forceinline__ bf16x8 codes8(const uint32_t (&w)[2]) {
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] = pack_codes((float)(signed char)(w[i >> 1] >> 16 * (i & 1)), (float)(signed char)(w[i >> 1] >> (16 * (i & 1) + 8)));
+  return __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+}
+
+// A step of a workgroup is 4 SK slots of one (row, KV head), SK a wave: 32, or 16 with fp32 pages.  The steps of the call, rows first, then
+// KV heads, then slots, are cut into as many equal runs as there are workgroups, whatever the lengths are: every workgroup
+// forms the running sum of the rows' steps itself (lengths live on the device).  An item (row, KV head) that ends up whole in
+// one workgroup is finished there; of one that is cut, every workgroup leaves a piece in ws and a second kernel joins them.
+//
+// Matrix instructions, operands straight from memory to registers, no LDS: S^T = K Q^T puts the query heads of the KV head (16
+// columns, those past G zero) beside the slots (rows), and O^T = V^T P^T wants of a lane 8 consecutive slots of one coordinate.
+//   - which slot a row of S^T is, is free: row i of block b is slot 8 (i / 4) + 4 b + i % 4, so that the weights a lane (column
+//     l16, lane group lg) gets are those of slots 8 lg .. 8 lg + 7, the P^T operand as it stands
+//   - which coordinate a row of O^T is, is free too: row l16 of block c is coordinate E l16 + c, so that a lane loads E consecutive
+//     coordinates of its 8 slots (a row of the page in 16 lanes) and the V^T operands are a transposition inside the lane
+//   - the weights go in as a sum of two bf16 (three where rows are fp32): the matrix pipe is idle most of the time, and the
+//     only rounding of bf16 size is then the output's; each part but the last is cut off below the weight, so that none is
+//     zero or negative and an infinite value stays one
+//   - codes of 8-bit pages are whole numbers that bf16 holds; the scales join the logits and the weights
+// The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float): a
+// comparison a slab instead of a reduction over lanes.
 struct attend_args {
   pages_args p;
   const void *q;
   void *out;
   const int *row_req, *row_len;
-  int n_rows;
-  float scale;
+  int n_rows, shares;
+  float scale;             // of the logits, in units of log 2
+  float *part_o;           // [2 * shares, G, D] pieces: 2 w the one that began before workgroup w, 2 w + 1 the one that goes on after it
+  float2 *part_ml;         // [2 * shares, G] (maximum, sum)
+  int *part_seen;          // [2 * shares] whether the piece has a slot at all
+  int2 *cut;               // [shares] the item that goes on after workgroup w (-1: none), and its pieces
 };
 
 template <typename T, int D, bool Q8>
-__global__ void __launch_bounds__(256)
-paged_attention_kernel(attend_args a) {
-  __shared__ float qs[D], w[256], red[4], part[256];
-  const int row = blockIdx.x / a.p.Hq, hq = blockIdx.x % a.p.Hq, G = a.p.Hq / a.p.Hkv, h = hq / G, tid = threadIdx.x;
+struct attend_form {
+  static constexpr bool kF32 = sizeof(T) == 4 && !Q8;          // fp32 matrix instructions
+  static constexpr int SK = kF32 ? 16 : 32;                    // slots of a wave's slab
+  static constexpr int KB = SK / 16;                           // row blocks of S^T
+  static constexpr int kRow = Q8 ? D : D * (int)sizeof(T);     // bytes of a slot
+  static constexpr int NK = kRow / 64;                         // 16-byte loads of a lane and row block: bytes 64 s + 16 lg ..
+  static constexpr int NS = SK / 4;                            // slots whose weights a lane has
+  static constexpr int E = kF32 ? 4 : D / 16, NP = D / (16 * E);   // a lane's coordinates: 16 E j + E l16 .. + E - 1, j < NP
+  static constexpr int kVWords = E * kRow / D / 4;             // 32-bit words of one of them
+  static constexpr int kQParts = Q8 && sizeof(T) == 4 ? 3 : 1, kPParts = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int kStep = 4 * SK;
+};
+// slots of a step by a3_pages (host and device agree through this)
+constexpr int step_shift(int dtype, int format) { return dtype == A3_F32 && format == A3_PAGES_PLAIN ? 6 : 7; }
+
+__device__ __forceinline__ int steps_of(const attend_args &a, int row, int shift) {
   const int req = a.row_req ? a.row_req[row] : row;
-  if (req < 0 || req >= a.p.n_req) return;
-  const int len = min(a.row_len[row], a.p.slots), page_size = 1 << a.p.page_shift;
-  const size_t head_bytes = page_head_bytes(Q8 ? A3_PAGES_Q8 : A3_PAGES_PLAIN, sizeof(T), page_size, D);
-  const size_t qo = ((size_t)row * a.p.Hq + hq) * D;
-  if (tid < D) qs[tid] = (float)((const T *)a.q)[qo + tid];
+  if (req < 0 || req >= a.p.n_req) return 0;
+  const int len = min(a.row_len[row], a.p.slots);
+  return len <= 0 ? 1 : ((len - 1) >> shift) + 1;                // (a row that sees nothing has its zeros written)
+}
+
+template <typename T, int D, bool Q8>
+__global__ void __launch_bounds__(256, 2)
+paged_attention_kernel(attend_args a) {
+  using F = attend_form<T, D, Q8>;
+  constexpr int SK = F::SK, kShift = SK == 16 ? 6 : 7, kOS = D + 4;
+  static_assert(F::kStep == 1 << kShift, "step");
+  __shared__ int scan[6];
+  __shared__ float2 ml[4][16];
+  __shared__ __align__(16) float os[4][16][kOS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, lg = lane >> 4, G = a.p.Hq / a.p.Hkv, Hkv = a.p.Hkv;
+
+  // ---- this workgroup's run of steps -----------------------------------------------------------------------
+  int mine = 0;
+  for (int r = tid; r < a.n_rows; r += 256) mine += steps_of(a, r, kShift);
+  for (int o = 32; o; o >>= 1) mine += __shfl_xor(mine, o);
+  if (lane == 0) scan[wave] = mine;
   __syncthreads();
-  auto block_of = [&](char *pool, int slot) -> char * {
-    const int page = a.p.table[(size_t)req * a.p.max_pages + (slot >> a.p.page_shift)];
-    return page < 0 || page >= a.p.n_pages ? nullptr : pool + ((size_t)page * a.p.Hkv + h) * head_bytes;
+  const int total = (scan[0] + scan[1] + scan[2] + scan[3]) * Hkv;
+  const int each = (total + a.shares - 1) / a.shares, first = min((int)blockIdx.x * each, total), n_steps = min(each, total - first);
+  if (n_steps <= 0) {
+    if (tid == 0) a.cut[blockIdx.x] = make_int2(-1, 0);
+    return;
+  }
+  int before = 0;                                              // steps of the rows in front of a block of 256 rows
+  for (int r0 = 0;; r0 += 256) {
+    __syncthreads();
+    const int st = r0 + tid < a.n_rows ? steps_of(a, r0 + tid, kShift) : 0;
+    const int incl = a3_wave_prefix(st);
+    if (lane == 63) scan[wave] = incl;
+    __syncthreads();
+    int base = before;
+    for (int w = 0; w < wave; ++w) base += scan[w];
+    const int lo = (base + incl - st) * Hkv, hi = (base + incl) * Hkv;
+    before += scan[0] + scan[1] + scan[2] + scan[3];
+    if (first >= lo && first < hi) { scan[4] = r0 + tid; scan[5] = first - lo; }
+    if (before * Hkv > first) break;
+  }
+  __syncthreads();
+
+  // ---- where the workgroup stands: a step of a row's KV head (all scalar) ------------------------------------------
+  struct place { int row, head, step, steps, len, req; };
+  place now;
+  now.row = __builtin_amdgcn_readfirstlane(scan[4]);
+  const int inside = __builtin_amdgcn_readfirstlane(scan[5]);
+  auto enter = [&](place &p) {                                 // the row's own numbers
+    p.req = __builtin_amdgcn_readfirstlane(a.row_req ? a.row_req[p.row] : p.row);
+    p.len = __builtin_amdgcn_readfirstlane(max(0, min(a.row_len[p.row], a.p.slots)));
+    p.steps = __builtin_amdgcn_readfirstlane(steps_of(a, p.row, kShift));
   };
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  bool any = false;
-  for (int u0 = 0; u0 < len; u0 += 256) {
-    const int slot = u0 + tid;
-    float s = -INFINITY;
-    bool here = false;
-    if (slot < len) {
-      const char *b = block_of(a.p.k_pool, slot);
-      const int at = slot & (page_size - 1);
-      if (b) {
-        here = true;
-        s = 0.f;
-        for (int e = 0; e < D; ++e)
-          s += qs[e] * (Q8 ? (float)((const signed char *)b)[at * D + e] : (float)((const T *)b)[at * D + e]);
-        if (Q8) s *= ((const float *)(b + (size_t)page_size * D))[at];
-        s *= a.scale;
+  enter(now);
+  now.head = inside / now.steps;
+  now.step = inside - now.head * now.steps;
+  auto advance = [&](place &p) {
+    if (++p.step < p.steps) return;
+    p.step = 0;
+    if (++p.head < Hkv) return;
+    p.head = 0;
+    do {
+      if (++p.row >= a.n_rows) return;                         // (only behind the last step of all)
+      enter(p);
+    } while (p.steps == 0);
+  };
+
+  // ---- one slab of one wave in registers ------------------------------------------------------------------
+  struct slab {
+    uint4 k[F::KB][F::NK];
+    uint32_t v[F::NS][F::NP][F::kVWords];
+    f32x4 ks[Q8 ? 2 : 1], vs[Q8 ? 2 : 1];
+    int n;                                                     // slots of it that are seen (0: nothing was loaded)
+  };
+  const size_t head_bytes = page_head_bytes(Q8 ? A3_PAGES_Q8 : A3_PAGES_PLAIN, sizeof(T), 1 << a.p.page_shift, D);
+  uint32_t koff[F::KB], voff;
+#pragma unroll
+  for (int b = 0; b < F::KB; ++b) koff[b] = (SK == 16 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3)) * F::kRow + 16 * lg;
+  voff = (uint32_t)(F::NS * lg * F::kRow + F::kVWords * 4 * l16);
+  auto load = [&](slab &s, const place &p) {
+    const int slot = (p.step << kShift) + SK * wave;
+    s.n = p.len - slot;
+    if (s.n <= 0) { s.n = 0; return; }
+    const int page = __builtin_amdgcn_readfirstlane(a.p.table[(size_t)p.req * a.p.max_pages + (slot >> a.p.page_shift)]);
+    if (page < 0 || page >= a.p.n_pages) { s.n = 0; return; }
+    const size_t block = ((size_t)page * Hkv + p.head) * head_bytes;
+    const int at = slot & ((1 << a.p.page_shift) - 1);
+    const char *kb = a.p.k_pool + block + at * F::kRow, *vb = a.p.v_pool + block + at * F::kRow;
+#pragma unroll
+    for (int b = 0; b < F::KB; ++b)
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i) s.k[b][i] = *reinterpret_cast<const uint4 *>(kb + koff[b] + 64 * i);
+    if constexpr (Q8) {
+      const char *sc = a.p.k_pool + block + ((size_t)D << a.p.page_shift) + 4 * at + 32 * lg;
+      s.ks[0] = *reinterpret_cast<const f32x4 *>(sc);
+      s.ks[1] = *reinterpret_cast<const f32x4 *>(sc + 16);
+      sc += a.p.v_pool - a.p.k_pool;
+      s.vs[0] = *reinterpret_cast<const f32x4 *>(sc);
+      s.vs[1] = *reinterpret_cast<const f32x4 *>(sc + 16);
+    }
+#pragma unroll
+    for (int i = 0; i < F::NS; ++i)
+#pragma unroll
+      for (int j = 0; j < F::NP; ++j) {
+        typedef uint32_t words __attribute__((ext_vector_type(F::kVWords == 1 ? 1 : F::kVWords)));
+        const words w = *reinterpret_cast<const words *>(vb + voff + i * F::kRow + j * 64 * F::kVWords);
+#pragma unroll
+        for (int u = 0; u < F::kVWords; ++u) s.v[i][j][u] = w[u];
+      }
+  };
+
+  // ---- queries of the item: operand of S^T, 16 columns ----------------------------------------------------------------
+  constexpr int NQ = F::kF32 ? F::NK : D / 32;
+  f32x4 qf[F::kF32 ? NQ : 1];
+  bf16x8 qb[F::kF32 ? 1 : F::kQParts][F::kF32 ? 1 : NQ];
+  auto load_queries = [&](const place &p) {
+    const T *q = (const T *)a.q + ((size_t)p.row * a.p.Hq + p.head * G + min(l16, G - 1)) * D;
+    const bool on = l16 < G;
+    if constexpr (F::kF32) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(q + 16 * i + 4 * lg);
+        qf[i] = on ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const T *at = q + (Q8 ? 64 * (i >> 1) + 16 * lg + 8 * (i & 1) : 32 * i + 8 * lg);
+        if constexpr (sizeof(T) == 2) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8 *>(at), zero = {};
+          qb[0][i] = on ? x : zero;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {                        // x as the sum of three bf16
+            float x = on ? at[e] : 0.f;
+#pragma unroll
+            for (int k = 0; k < F::kQParts; ++k) {
+              const bf16_t h = a3_f2bf(x);
+              qb[k][i][e] = h;
+              x -= a3_bf2f(h);
+              if (!(fabsf(x) < INFINITY)) x = 0.f;             // an infinity has no remainder
+            }
+          }
+        }
       }
     }
-    any = __syncthreads_or(here) || any;
-    float mx = s;
-    for (int x = 32; x; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-    if ((tid & 63) == 0) red[tid >> 6] = mx;
-    __syncthreads();
-    mx = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    const float ref = mx == -INFINITY ? 0.f : mx, keep = expf(m - ref);
-    w[tid] = here ? expf(s - ref) : 0.f;
-    __syncthreads();
-    o *= keep;
-    l *= keep;
-    m = mx;
-    const int e = tid % D, lo = tid / D * D, n = min(256, len - u0);           // each group of D threads sums D of the 256 slots
-    for (int j = lo; j < min(n, lo + D); ++j) {
-      const char *b = block_of(a.p.v_pool, u0 + j);
-      const int at = (u0 + j) & (page_size - 1);
-      if (!b) continue;
-      const float v = Q8 ? (float)((const signed char *)b)[at * D + e] * ((const float *)(b + (size_t)page_size * D))[at]
-                         : (float)((const T *)b)[at * D + e];
-      o += w[j] * v;
-      l += w[j];
+  };
+
+  // ---- running state of the item --------------------------------------------------------------------------
+  f32x4 o[D / 16];
+  float m, l;
+  bool seen;
+  auto clear = [&]() {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+    seen = false;
+  };
+
+  auto compute = [&](slab &s) {
+    if (s.n == 0) return;
+    seen = true;
+    f32x4 acc[F::KB];
+#pragma unroll
+    for (int b = 0; b < F::KB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (F::kF32) {
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i) {
+        const f32x4 kf = __builtin_bit_cast(f32x4, s.k[0][i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[i][e], acc[0], 0, 0, 0);
+      }
+    } else if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int b = 0; b < F::KB; ++b) {
+            const uint32_t w[2] = {u ? s.k[b][i].z : s.k[b][i].x, u ? s.k[b][i].w : s.k[b][i].y};
+            const bf16x8 kf = codes8(w);
+#pragma unroll
+            for (int k = 0; k < F::kQParts; ++k) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[k][2 * i + u], acc[b], 0, 0, 0);
+          }
+    } else {
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i)
+#pragma unroll
+        for (int b = 0; b < F::KB; ++b)
+          acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, s.k[b][i]), qb[0][i], acc[b], 0, 0, 0);
     }
-    __syncthreads();
+    float w[F::NS];
+#pragma unroll
+    for (int i = 0; i < F::NS; ++i) {
+      w[i] = acc[i >> 2][i & 3] * a.scale;
+      if constexpr (Q8) w[i] *= s.ks[i >> 2][i & 3];
+    }
+    if (s.n < SK) {                                            // the row ends in this slab: whatever lies behind counts nothing
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i)
+        if (F::NS * lg + i >= s.n) {
+          w[i] = -INFINITY;
+          if constexpr (Q8) s.vs[i >> 2][i & 3] = 0.f;
+          else
+#pragma unroll
+            for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+              for (int u = 0; u < F::kVWords; ++u) s.v[i][j][u] = 0u;
+        }
+    }
+    float top = w[0];
+#pragma unroll
+    for (int i = 1; i < F::NS; ++i) top = fmaxf(top, w[i]);
+    if (__any(top > m + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float next = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[c] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < F::NS; ++i) {
+      w[i] = __builtin_amdgcn_exp2f(w[i] - ref);
+      l += w[i];
+      if constexpr (Q8) w[i] *= s.vs[i >> 2][i & 3];
+    }
+    if constexpr (F::kF32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+          o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, s.v[i][c >> 2][c & 3]), w[i], o[c], 0, 0, 0);
+    } else {
+      bf16x8 pf[F::kPParts];
+#pragma unroll
+      for (int k = 0; k < F::kPParts; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (k == F::kPParts - 1) { pf[k][i] = a3_f2bf(w[i]); continue; }
+          const uint32_t h = __builtin_elementwise_sub_sat(__float_as_uint(w[i]), 1u) & 0xffff0000u;
+          pf[k][i] = __builtin_bit_cast(bf16_t, (unsigned short)(h >> 16));
+          w[i] -= __uint_as_float(h);
+        }
+      bf16x8 vf[D / 16];
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        if constexpr (Q8) {
+          uint32_t x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = pack_codes((float)(signed char)(s.v[2 * i][0][c >> 2] >> 8 * (c & 3)), (float)(signed char)(s.v[2 * i + 1][0][c >> 2] >> 8 * (c & 3)));
+          vf[c] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+        } else {
+          uint32_t x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = __builtin_amdgcn_perm(s.v[2 * i + 1][0][c >> 1], s.v[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+          vf[c] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < F::kPParts; ++k)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], pf[k], o[c], 0, 0, 0);
+    }
+  };
+
+  // ---- an item, or this workgroup's part of one, is done: join the four waves -----------------------------------------------
+  auto finish = [&](const place &p, bool begins, bool ends) {
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (lg == 0) ml[wave][l16] = make_float2(m, l);
+    if (lane == 0) scan[wave] = seen;
+    A3_LDS_BARRIER();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][l16].x);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    if (l16 < G) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+          for (int c = 0; c < F::E; c += 4) {
+            const int b = j * F::E + c;
+            *reinterpret_cast<f32x4 *>(&os[wave][l16][16 * F::E * j + F::E * (4 * lg + r) + c]) =
+                f32x4{o[b][r], o[b + 1][r], o[b + 2][r], o[b + 3][r]} * f;
+          }
+    }
+    const bool any = scan[0] | scan[1] | scan[2] | scan[3];
+    A3_LDS_BARRIER();
+    const bool whole = begins && ends;
+    const int slot = 2 * blockIdx.x + (begins ? 1 : 0);
+    for (int e = tid; e < G * (D / 4); e += 256) {
+      const int g = e / (D / 4), d = 4 * (e % (D / 4));
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        sum += *reinterpret_cast<const f32x4 *>(&os[w][g][d]);
+        M = fmaxf(M, ml[w][g].x);
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w) L += ml[w][g].x == -INFINITY ? 0.f : ml[w][g].y * __builtin_amdgcn_exp2f(ml[w][g].x - M);
+      if (whole) {
+        typedef T vec4 __attribute__((ext_vector_type(4)));
+        vec4 y;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = (T)(any ? sum[u] / L : 0.f);
+        *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)p.row * a.p.Hq + p.head * G + g) * D + d) = y;
+      } else {
+        *reinterpret_cast<f32x4 *>(a.part_o + ((size_t)slot * G + g) * D + d) = sum;
+        if (d == 0) a.part_ml[(size_t)slot * G + g] = make_float2(M, L);
+      }
+    }
+    if (!whole && tid == 0) a.part_seen[slot] = any;
+    A3_LDS_BARRIER();
+  };
+
+  // ---- the run of steps: the next slab is on its way while one is worked on ------------------------------------------
+  slab sa, sb;
+  bool begins = now.step == 0;
+  load(sa, now);
+  load_queries(now);
+  clear();
+  place next = now;
+  int cut_item = -1, cut_pieces = 0;
+  auto step = [&](int i, slab &cur, slab &nxt) {
+    next = now;
+    const bool more = i + 1 < n_steps;
+    if (more) {
+      advance(next);
+      load(nxt, next);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    compute(cur);
+    const bool ends = now.step == now.steps - 1;
+    if (ends || !more) {
+      finish(now, begins, ends);
+      if (begins && !ends) {                                   // goes on in the workgroups behind: how many of them
+        cut_item = now.row * Hkv + now.head;
+        cut_pieces = 1 + (now.steps - 1 - now.step + each - 1) / each;
+      }
+      if (more) {
+        begins = true;
+        load_queries(next);
+        clear();
+      }
+    }
+    now = next;
+  };
+  for (int i = 0; i < n_steps; i += 2) {
+    step(i, sa, sb);
+    if (i + 1 < n_steps) step(i + 1, sb, sa);
   }
-  part[tid] = o;
-  w[tid] = l;
+  if (tid == 0) a.cut[blockIdx.x] = make_int2(cut_item, cut_pieces);
+}
+
+// Joins the pieces of the item that goes on after workgroup blockIdx.x, query head blockIdx.y of its KV head.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+paged_attention_join_kernel(attend_args a) {
+  constexpr int kGroups = 256 / D;
+  __shared__ float factor[1024], red[4], sum[256];
+  const int2 cut = a.cut[blockIdx.x];
+  if (cut.x < 0) return;
+  const int tid = threadIdx.x, g = blockIdx.y, G = a.p.Hq / a.p.Hkv, n = cut.y, w = blockIdx.x;
+  auto slot_of = [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); };
+  float M = -INFINITY;
+  bool seen = false;
+  for (int i = tid; i < n; i += 256) {
+    factor[i] = a.part_ml[(size_t)slot_of(i) * G + g].x;
+    M = fmaxf(M, factor[i]);
+    seen |= a.part_seen[slot_of(i)] != 0;
+  }
+  for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) red[tid >> 6] = M;
+  seen = __syncthreads_or(seen);
+  M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  float L = 0.f;
+  for (int i = tid; i < n; i += 256) {
+    const float f = factor[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(factor[i] - M);
+    factor[i] = f;
+    if (f != 0.f) L += f * a.part_ml[(size_t)slot_of(i) * G + g].y;
+  }
+  for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
+  __syncthreads();
+  if ((tid & 63) == 0) red[tid >> 6] = L;
+  __syncthreads();
+  L = (red[0] + red[1]) + (red[2] + red[3]);
+  const int d = tid % D;
+  float o = 0.f;
+#pragma unroll 4
+  for (int i = tid / D; i < n; i += kGroups) {
+    const float x = a.part_o[((size_t)slot_of(i) * G + g) * D + d];
+    if (factor[i] != 0.f) o += factor[i] * x;
+  }
+  sum[tid] = o;
   __syncthreads();
   if (tid >= D) return;
-  o = l = 0.f;
-  for (int j = tid; j < 256; j += D) { o += part[j]; l += w[j]; }
-  ((T *)a.out)[qo + tid] = (T)(any ? o / l : 0.f);
+  o = 0.f;
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) o += sum[tid + i * D];
+  ((T *)a.out)[((size_t)(cut.x / a.p.Hkv) * a.p.Hq + (cut.x % a.p.Hkv) * G + g) * D + tid] = (T)(seen ? o / L : 0.f);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -336,9 +732,31 @@ extern "C" a3_status a3_paged_append(const a3_pages *P, const void *k, const voi
   return A3_OK;
 }
 
+// Two workgroups on each of the 256 compute units, fewer where the page table has fewer steps than that.
+constexpr int kMaxShares = 512;
+static long long attend_steps(const a3_pages *P, int n_rows) {
+  const int shift = step_shift(P->dtype, P->format);
+  return (((long long)P->max_pages * P->page_size + (1 << shift) - 1) >> shift) * P->n_kv_heads * n_rows;
+}
+static int attend_shares(const a3_pages *P, int n_rows) {
+  const long long steps = attend_steps(P, n_rows);
+  return steps < kMaxShares ? (int)steps : kMaxShares;
+}
+// workspace of `shares` workgroups; base NULL: only its size
+static size_t attend_ws(const a3_pages *P, int shares, void *base, attend_args *a) {
+  const size_t G = P->n_q_heads / P->n_kv_heads, D = P->head_dim, n = (size_t)shares;
+  a3_ws_cursor cur(base, 0);
+  float *o = (float *)cur.take(2 * n * G * D * sizeof(float));
+  float2 *ml = (float2 *)cur.take(2 * n * G * sizeof(float2));
+  int *seen = (int *)cur.take(2 * n * sizeof(int));
+  int2 *cut = (int2 *)cur.take(n * sizeof(int2));
+  if (a) { a->part_o = o; a->part_ml = ml; a->part_seen = seen; a->cut = cut; }
+  return cur.off;
+}
+
 extern "C" size_t a3_paged_attention_ws_bytes(const a3_pages *P, int n_rows) {
   if (check_pages(P, "a3_paged_attention_ws_bytes", false) != A3_OK || n_rows < 0) return 0;
-  return 256;
+  return attend_ws(P, attend_shares(P, n_rows > 0 ? n_rows : 1), nullptr, nullptr);
 }
 
 extern "C" a3_status a3_paged_attention(const a3_pages *P, const void *q, const int *row_req, const int *row_len, int n_rows,
@@ -351,14 +769,18 @@ extern "C" a3_status a3_paged_attention(const a3_pages *P, const void *q, const 
   A3_REQUIRE(row_req || n_rows <= P->n_req, A3_ERR_INVALID_ARG, "a3_paged_attention: %d rows without row_req for %d requests", n_rows,
              P->n_req);
   A3_REQUIRE(a3_aligned16(q) && a3_aligned16(out), A3_ERR_INVALID_ARG, "a3_paged_attention: tensors must be 16-byte aligned");
-  A3_REQUIRE((long long)n_rows * P->n_q_heads < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_paged_attention: too many rows");
-  const size_t need = a3_paged_attention_ws_bytes(P, n_rows);
+  A3_REQUIRE(attend_steps(P, n_rows) < (1LL << 31) - 1024 && (long long)n_rows * P->n_q_heads < (1LL << 31), A3_ERR_UNSUPPORTED,
+             "a3_paged_attention: too many rows for a page table of this width");
+  const int shares = attend_shares(P, n_rows);
+  attend_args a{args_of(P), q, out, row_req, row_len, n_rows, shares,
+                (float)((P->sm_scale != 0.f ? (double)P->sm_scale : 1.0 / sqrt((double)P->head_dim)) * 1.4426950408889634074)};
+  const size_t need = attend_ws(P, shares, ws, &a);
   A3_REQUIRE(ws && a3_aligned16(ws) && ws_bytes >= need, A3_ERR_WORKSPACE, "a3_paged_attention: workspace %zu bytes (16-byte aligned), need %zu",
              ws ? ws_bytes : 0, need);
-  attend_args a{args_of(P), q, out, row_req, row_len, n_rows, P->sm_scale != 0.f ? P->sm_scale : 1.0f / sqrtf((float)P->head_dim)};
+  const dim3 join((unsigned)shares, (unsigned)(P->n_q_heads / P->n_kv_heads));
   with_format(P, [&](auto elem, auto d, auto q8) {
-    hipLaunchKernelGGL((paged_attention_kernel<decltype(elem), d.value, q8.value>), dim3((unsigned)(n_rows * P->n_q_heads)), dim3(256), 0,
-                       (hipStream_t)stream, a);
+    hipLaunchKernelGGL((paged_attention_kernel<decltype(elem), d.value, q8.value>), dim3((unsigned)shares), dim3(256), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((paged_attention_join_kernel<decltype(elem), d.value>), join, dim3(256), 0, (hipStream_t)stream, a);
   });
   A3_CHECK_LAUNCH("a3_paged_attention");
   return A3_OK;
