@@ -88,8 +88,14 @@ logits_f32_kernel(logits_args a) {
 }
 
 // ---------------------------------------------------------------------------------------
-// log probabilities: one workgroup per row, the row read once for each of its maximum, its sums and its alternatives
+// log probabilities: every row read once
 // ---------------------------------------------------------------------------------------
+// A workgroup reads a row, or with few rows a slice of one, in chunks of 32 values a thread.  Sums: every thread keeps the maximum m of
+// its own values, z = sum e^(x - m) and t = sum e^(x - m) (x - m) in units of log 2 and rescales them when a chunk brings a larger value
+// (t' = f (t + (m - m') z), f = 2^(m - m')).  Alternatives: a chunk none of whose values exceeds the n-th best so far costs one comparison
+// (later equal values lose: higher index); otherwise every wave finds the n-th largest of its lanes' maxima, bit by bit with ballots,
+// and only values not below the largest of these four bounds are gathered and ranked.  Pieces of a row that was cut into slices
+// are put together by a second kernel, with the same selection.
 struct logprob_args {
   const void *x;
   long long ld;
@@ -97,70 +103,238 @@ struct logprob_args {
   const int *tokens;
   float *logprob, *entropy, *top_logprob;
   int *top_idx;
+  int slices;                        // of a row; 1: no second kernel
+  float4 *part;                      // [n_rows, slices] (m, z, t) of a slice
+  unsigned long long *part_top;      // [n_rows, slices, n_top]
 };
 
-// Order of the alternatives as one number: larger logit, then lower index; -0 equals 0, NaN below everything.
-__device__ __forceinline__ unsigned long long top_key(float x, int v) {
-  const unsigned b = __float_as_uint(x + 0.f);
-  const unsigned o = x != x ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return ((unsigned long long)o << 32) | (unsigned)~v;
+constexpr int kLpThreads = 256, kLpValues = 32, kLpTop = 64, kLpCands = 1024;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+
+// Order of the alternatives as one number: larger logit, then lower index; -0 equals 0, NaN below everything (0: no value).
+__device__ __forceinline__ uint32_t top_order(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return x != x ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ unsigned long long top_key(float x, int v) { return ((unsigned long long)top_order(x) << 32) | (uint32_t)~v; }
 __device__ __forceinline__ float top_value(unsigned long long key) {
-  const unsigned o = (unsigned)(key >> 32);
+  const uint32_t o = (uint32_t)(key >> 32);
   return o == 0u ? __uint_as_float(0x7fc00000u) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256)
-logprobs_kernel(logprob_args a) {
-  __shared__ float red[4][2];
-  __shared__ unsigned long long best[4];
-  const int row = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
-  const T *x = (const T *)a.x + (size_t)row * a.ld;
-  float m = -INFINITY;
-  bool nan = false;
-  for (int v = tid; v < a.vocab; v += 256) { const float f = (float)x[v]; m = fmaxf(m, f); nan |= f != f; }
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((tid & 63) == 0) red[wave][0] = m;
-  nan = __syncthreads_or(nan);
-  m = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
-  __syncthreads();
-  float z = 0.f, t = 0.f;
-  for (int v = tid; v < a.vocab; v += 256) {
-    const float d = (float)x[v] - m, e = expf(d);
-    z += e;
-    if (e > 0.f) t += e * d;
+struct lp_shared {
+  float red[4][4];
+  uint32_t bound[4];
+  int count;
+  unsigned long long best[4], list[kLpTop], cand[kLpCands + kLpTop];
+};
+
+// list (the n best so far, sorted, 0: none) becomes the n best of itself and of all threads' key(0) .. key(N - 1); order(i) is
+// the upper half of key(i).  The keys of all threads differ, except for 0, which is none.
+template <int N, class Order, class Key>
+__device__ __forceinline__ void top_update(lp_shared &s, int n, Order order, Key key) {
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = max(top, order(i));
+  uint32_t bound = 0;                                          // the n-th largest of the wave's maxima (at least n values reach it)
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t t = bound | 1u << b;
+    if (__popcll(__ballot(top >= t)) >= n) bound = t;
   }
-  for (int o = 32; o; o >>= 1) { z += __shfl_xor(z, o); t += __shfl_xor(t, o); }
-  if ((tid & 63) == 0) { red[wave][0] = z; red[wave][1] = t; }
+  if (tid == 0) s.count = n;
+  if ((tid & 63) == 0) s.bound[wave] = bound;
+  if (tid < n) s.cand[tid] = s.list[tid];
   __syncthreads();
-  z = (red[0][0] + red[1][0]) + (red[2][0] + red[3][0]);
-  t = (red[0][1] + red[1][1]) + (red[2][1] + red[3][1]);
-  if (nan || m == INFINITY || m == -INFINITY) z = __uint_as_float(0x7fc00000u);
+  bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3]));
+  const unsigned long long last = s.list[n - 1];
+  if (top >= bound)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (order(i) >= bound) {
+        const unsigned long long k = key(i);
+        if (k > last) {
+          const int at = atomicAdd(&s.count, 1);
+          if (at < kLpCands + kLpTop) s.cand[at] = k;
+        }
+      }
+  __syncthreads();
+  const int count = s.count;
+  if (count <= kLpCands + kLpTop) {                            // every candidate's place is the number of larger ones
+    for (int c = tid; c < count; c += kLpThreads) {
+      const unsigned long long k = s.cand[c];
+      int rank = 0;
+      for (int o = 0; o < count; ++o) rank += s.cand[o] > k || (s.cand[o] == k && o < c);
+      if (rank < n) s.list[rank] = k;
+    }
+    __syncthreads();
+    return;
+  }
+  // a great many equal values: one after the other, the largest below the last one taken (s.cand[0 .. n - 1]: the list before)
+  unsigned long long prev = ~0ull;
+  int old = 0;
+  for (int j = 0; j < n; ++j) {
+    unsigned long long b = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const unsigned long long k = key(i);
+      if (k < prev && k > b) b = k;
+    }
+    for (int o = 32; o; o >>= 1) { const unsigned long long k = __shfl_xor(b, o); b = k > b ? k : b; }
+    if ((tid & 63) == 0) s.best[wave] = b;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) b = s.best[w] > b ? s.best[w] : b;
+    const unsigned long long from_list = s.cand[old];
+    if (from_list > b) { b = from_list; ++old; } else prev = b;
+    if (tid == 0) s.list[j] = b;
+    __syncthreads();
+  }
+}
+
+// What a row's m, z, t and best values give.
+template <typename T>
+__device__ __forceinline__ void logprobs_write(const logprob_args &a, const lp_shared &s, int row, const T *x, float m, float z, float t) {
   const float log_z = logf(z);
-  if (tid == 0 && a.entropy) a.entropy[row] = log_z - t / z;
-  for (int j = tid; j < a.n_given; j += 256) {
+  const bool none = m == -INFINITY;
+  if (threadIdx.x == 0 && a.entropy) a.entropy[row] = none ? __uint_as_float(0x7fc00000u) : log_z - kLn2 * t / z;
+  for (int j = threadIdx.x; j < a.n_given; j += kLpThreads) {
     const int tok = a.tokens[(size_t)row * a.n_given + j];
     a.logprob[(size_t)row * a.n_given + j] = tok < 0 || tok >= a.vocab ? -INFINITY : ((float)x[tok] - m) - log_z;
   }
-  unsigned long long last = ~0ull;
-  for (int j = 0; j < a.n_top; ++j) {
-    unsigned long long b = 0;
-    for (int v = tid; v < a.vocab; v += 256) {
-      const unsigned long long k = top_key((float)x[v], v);
-      if (k < last && k > b) b = k;
-    }
-    for (int o = 32; o; o >>= 1) { const unsigned long long k = __shfl_xor(b, o); b = k > b ? k : b; }
-    __syncthreads();
-    if ((tid & 63) == 0) best[wave] = b;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) b = best[w] > b ? best[w] : b;
-    if (tid == 0) {
-      a.top_idx[(size_t)row * a.n_top + j] = (int)~(unsigned)b;
-      a.top_logprob[(size_t)row * a.n_top + j] = (top_value(b) - m) - log_z;
-    }
-    last = b;
+  for (int j = threadIdx.x; j < a.n_top; j += kLpThreads) {
+    const unsigned long long k = s.list[j];
+    a.top_idx[(size_t)row * a.n_top + j] = (int)~(uint32_t)k;
+    a.top_logprob[(size_t)row * a.n_top + j] = (top_value(k) - m) - log_z;
   }
+}
+
+// (from - to) in units of log 2: what moves a sum from reference `from` to the larger `to`.  Bounded, so that a sum whose weight
+// is 0 (masks of the type's lowest value: the difference overflows) leaves no NaN.
+__device__ __forceinline__ float lp_shift(float from, float to) { return from == -INFINITY ? 0.f : fmaxf((from - to) * kLog2e, -1e30f); }
+
+// (m, z, t) of a workgroup's threads, or of pieces, as one
+__device__ __forceinline__ void lp_join(float &m, float &z, float &t, float m1, float z1, float t1) {
+  const float top = fmaxf(m, m1);
+  const float d = lp_shift(m, top), d1 = lp_shift(m1, top);
+  const float f = __builtin_amdgcn_exp2f(d), f1 = __builtin_amdgcn_exp2f(d1);
+  t = f * fmaf(d, z, t) + f1 * fmaf(d1, z1, t1);
+  z = f * z + f1 * z1;
+  m = top;
+}
+__device__ __forceinline__ void lp_join_workgroup(lp_shared &s, float &m, float &z, float &t) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    // both sides of a pair form the same numbers: the lower lane's first
+    const float m1 = __shfl_xor(m, o), z1 = __shfl_xor(z, o), t1 = __shfl_xor(t, o);
+    if (threadIdx.x & o) { float a = m1, b = z1, c = t1; lp_join(a, b, c, m, z, t); m = a; z = b; t = c; }
+    else lp_join(m, z, t, m1, z1, t1);
+  }
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) { s.red[wave][0] = m; s.red[wave][1] = z; s.red[wave][2] = t; }
+  __syncthreads();
+  m = s.red[0][0]; z = s.red[0][1]; t = s.red[0][2];
+  for (int w = 1; w < 4; ++w) lp_join(m, z, t, s.red[w][0], s.red[w][1], s.red[w][2]);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLpThreads)
+logprobs_kernel(logprob_args a) {
+  constexpr int V = a3_elem<T>::kVec, U = kLpValues / V;
+  typedef T vec_t __attribute__((ext_vector_type(V)));
+  __shared__ lp_shared s;
+  const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x;
+  const T *x = (const T *)a.x + (size_t)row * a.ld;
+  // the row as aligned vectors: vector v holds elements v V - skew .. (skew: how far the row starts behind a 16-byte border)
+  const int skew = (int)(((uintptr_t)x & 15) / sizeof(T)), n_vec = (int)(((long long)a.vocab + skew + V - 1) / V);
+  const int v0 = (int)((long long)n_vec * slice / a.slices), v1 = (int)((long long)n_vec * (slice + 1) / a.slices);
+  for (int j = tid; j < a.n_top; j += kLpThreads) s.list[j] = 0;
+  __syncthreads();
+  float m = -INFINITY, z = 0.f, t = 0.f;
+  for (int c = v0; c < v1; c += U * kLpThreads) {
+    float y[kLpValues];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = c + u * kLpThreads + tid, e = v * V - skew;
+      vec_t raw;
+      if (v < v1 && e >= 0 && e + V <= a.vocab) raw = *reinterpret_cast<const vec_t *>(x + e);
+      else
+#pragma unroll
+        for (int i = 0; i < V; ++i) raw[i] = v < v1 && e + i >= 0 && e + i < a.vocab ? x[e + i] : (T)-INFINITY;
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[u * V + i] = (float)raw[i];
+    }
+    float top = y[0];
+#pragma unroll
+    for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, y[i]);
+    if (top > m) {
+      const float d = lp_shift(m, top), f = __builtin_amdgcn_exp2f(d);
+      t = f * fmaf(d, z, t);
+      z *= f;
+      m = top;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < kLpValues; ++i) {
+      const float d = (y[i] - ref) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+      z += e;
+      t = fmaf(e, fmaxf(d, -1e30f), t);                        // -inf: e = 0 (NaN stays in z)
+    }
+    if (a.n_top) {
+      const unsigned long long last = s.list[a.n_top - 1];
+      if (__syncthreads_or(last == 0 || !(top <= top_value(last)))) {
+        auto index = [&](int i) { return (c + i / V * kLpThreads + tid) * V - skew + i % V; };
+        auto inside = [&](int i) { return c + i / V * kLpThreads + tid < v1 && (unsigned)index(i) < (unsigned)a.vocab; };
+        top_update<kLpValues>(s, a.n_top, [&](int i) { return inside(i) ? top_order(y[i]) : 0u; },
+                              [&](int i) { return inside(i) ? top_key(y[i], index(i)) : 0ull; });
+      }
+    }
+  }
+  lp_join_workgroup(s, m, z, t);
+  if (a.slices == 1) {
+    logprobs_write(a, s, row, x, m, z, t);
+    return;
+  }
+  if (tid == 0) a.part[blockIdx.x] = make_float4(m, z, t, 0.f);
+  for (int j = tid; j < a.n_top; j += kLpThreads) a.part_top[(size_t)blockIdx.x * a.n_top + j] = s.list[j];
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLpThreads)
+logprobs_join_kernel(logprob_args a) {
+  __shared__ lp_shared s;
+  const int row = blockIdx.x, tid = threadIdx.x;
+  float m = -INFINITY, z = 0.f, t = 0.f;
+  if (tid < a.slices) {
+    const float4 p = a.part[(size_t)row * a.slices + tid];
+    m = p.x; z = p.y; t = p.z;
+  }
+  const unsigned long long *keys = a.part_top + (size_t)row * a.slices * a.n_top;
+  constexpr int N = 16;                                        // kLpSlices * kLpTop / kLpThreads
+  unsigned long long k[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) k[i] = i * kLpThreads + tid < a.slices * a.n_top ? keys[i * kLpThreads + tid] : 0ull;
+  for (int j = tid; j < a.n_top; j += kLpThreads) s.list[j] = 0;
+  lp_join_workgroup(s, m, z, t);
+  if (a.n_top) top_update<N>(s, a.n_top, [&](int i) { return (uint32_t)(k[i] >> 32); }, [&](int i) { return k[i]; });
+  logprobs_write(a, s, row, (const T *)a.x + (size_t)row * a.ld, m, z, t);
+}
+
+// Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of no less than two vectors a thread.
+constexpr int kLpSlices = 64;
+static_assert(kLpSlices * kLpTop == 16 * kLpThreads, "logprobs_join_kernel's keys");
+int logprob_slices(int n_rows, int vocab, int elem) {
+  const int by_rows = (1024 + n_rows - 1) / n_rows, by_size = (int)((long long)vocab * elem / (16 * 2 * kLpThreads));
+  const int n = by_rows < by_size ? by_rows : by_size;
+  return n < 1 ? 1 : n > kLpSlices ? kLpSlices : n;
+}
+size_t logprob_ws(int n_rows, int slices, int n_top, void *base, logprob_args *a) {
+  if (slices == 1) return 256;
+  a3_ws_cursor cur(base, 0);
+  float4 *part = (float4 *)cur.take((size_t)n_rows * slices * sizeof(float4));
+  unsigned long long *top = (unsigned long long *)cur.take((size_t)n_rows * slices * n_top * sizeof(unsigned long long));
+  if (a) { a->part = part; a->part_top = top; }
+  return cur.off;
 }
 
 }  // namespace
@@ -204,7 +378,7 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
 
 extern "C" size_t a3_token_logprobs_ws_bytes(int n_rows, int vocab, int n_top) {
   if (n_rows < 0 || vocab <= 0 || n_top < 0) return 0;
-  return 256;
+  return n_rows == 0 ? 256 : logprob_ws(n_rows, logprob_slices(n_rows, vocab, 4), n_top, nullptr, nullptr);   // (bf16: no more slices)
 }
 
 extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows, int vocab, long long ld, const int *tokens, int n_given,
@@ -212,6 +386,7 @@ extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows
                                        size_t ws_bytes, void *stream) {
   A3_REQUIRE(dtype == A3_F32 || dtype == A3_BF16, A3_ERR_INVALID_ARG, "a3_token_logprobs: unknown dtype %d", dtype);
   A3_REQUIRE(n_rows >= 0 && vocab > 0 && ld >= vocab, A3_ERR_INVALID_ARG, "a3_token_logprobs: n_rows %d, vocab %d, ld %lld", n_rows, vocab, ld);
+  A3_REQUIRE(vocab < (1 << 30), A3_ERR_UNSUPPORTED, "a3_token_logprobs: vocab %d (2^30 and more)", vocab);
   A3_REQUIRE(n_given >= 0 && n_top >= 0 && n_top <= vocab, A3_ERR_INVALID_ARG, "a3_token_logprobs: n_given %d, n_top %d of %d", n_given,
              n_top, vocab);
   A3_REQUIRE(n_top <= 64, A3_ERR_UNSUPPORTED, "a3_token_logprobs: n_top %d (64 at most)", n_top);
@@ -222,9 +397,17 @@ extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows
   const size_t need = a3_token_logprobs_ws_bytes(n_rows, vocab, n_top);
   A3_REQUIRE(ws && a3_aligned16(ws) && ws_bytes >= need, A3_ERR_WORKSPACE, "a3_token_logprobs: workspace %zu bytes (16-byte aligned), need %zu",
              ws ? ws_bytes : 0, need);
-  logprob_args a{logits, ld, vocab, n_given, n_top, tokens, logprob, entropy, top_logprob, top_idx};
-  if (dtype == A3_BF16) hipLaunchKernelGGL(logprobs_kernel<bf16_t>, dim3(n_rows), dim3(256), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(logprobs_kernel<float>, dim3(n_rows), dim3(256), 0, (hipStream_t)stream, a);
+  logprob_args a{logits, ld, vocab, n_given, n_top, tokens, logprob, entropy, top_logprob, top_idx,
+                 logprob_slices(n_rows, vocab, dtype == A3_BF16 ? 2 : 4), nullptr, nullptr};
+  A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_token_logprobs: too many rows");
+  logprob_ws(n_rows, a.slices, n_top, ws, &a);
+  auto launch = [&](auto elem) {
+    typedef decltype(elem) T;
+    hipLaunchKernelGGL(logprobs_kernel<T>, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
+    if (a.slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)n_rows), dim3(kLpThreads), 0, (hipStream_t)stream, a);
+  };
+  if (dtype == A3_BF16) launch(bf16_t{});
+  else launch(0.f);
   A3_CHECK_LAUNCH("a3_token_logprobs");
   return A3_OK;
 }
