@@ -92,10 +92,11 @@ logits_f32_kernel(logits_args a) {
 // ---------------------------------------------------------------------------------------
 // A workgroup reads a row, or with few rows a slice of one, in chunks of 32 values a thread.  Sums: every thread keeps the maximum m of
 // its own values, z = sum e^(x - m) and t = sum e^(x - m) (x - m) in units of log 2 and rescales them when a chunk brings a larger value
-// (t' = f (t + (m - m') z), f = 2^(m - m')).  Alternatives: a chunk none of whose values exceeds the n-th best so far costs one comparison
-// (later equal values lose: higher index); otherwise every wave finds the n-th largest of its lanes' maxima, bit by bit with ballots,
-// and only values not below the largest of these four bounds are gathered and ranked.  Pieces of a row that was cut into slices
-// are put together by a second kernel, with the same selection.
+// (t' = f (t + (m - m') z), f = 2^(m - m')).  Alternatives: while it reads, a thread only notes the maximum of each of its chunks.
+// Then the n-th largest of a wave's 64 lane maxima is found bit by bit with ballots: at least n values of the row are no smaller, so
+// what lies below the largest of the four waves' bounds is out, and only the chunks that reach it are looked at again (some n of
+// them, from cache) and their values ranked.  The order has no ties (a value's index is part of it), so rows of equal or masked
+// values leave no more than a few hundred candidates either.  Slices of a row are put together by a second kernel in the same way.
 struct logprob_args {
   const void *x;
   long long ld;
@@ -122,71 +123,82 @@ __device__ __forceinline__ float top_value(unsigned long long key) {
   return o == 0u ? __uint_as_float(0x7fc00000u) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
 
+constexpr int kLpChunks = 20;        // chunks whose maxima are noted before their alternatives are chosen: rows up to 163840 in one go
+
 struct lp_shared {
   float red[4][4];
-  uint32_t bound[4];
+  unsigned long long bound[4];
   int count;
-  unsigned long long best[4], list[kLpTop], cand[kLpCands + kLpTop];
+  unsigned long long best[4], list[kLpTop], cand[kLpCands];
 };
 
-// list (the n best so far, sorted, 0: none) becomes the n best of itself and of all threads' key(0) .. key(N - 1); order(i) is
-// the upper half of key(i).  The keys of all threads differ, except for 0, which is none.
-template <int N, class Order, class Key>
-__device__ __forceinline__ void top_update(lp_shared &s, int n, Order order, Key key) {
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) top = max(top, order(i));
-  uint32_t bound = 0;                                          // the n-th largest of the wave's maxima (at least n values reach it)
-  for (int b = 31; b >= 0; --b) {
-    const uint32_t t = bound | 1u << b;
-    if (__popcll(__ballot(top >= t)) >= n) bound = t;
+// The n-th largest of a wave's 64 keys, or something below it that no more values reach; 0 if fewer than n lanes have a key.
+__device__ __forceinline__ unsigned long long wave_bound(unsigned long long key, int n) {
+  const uint32_t hi = (uint32_t)(key >> 32), lo = (uint32_t)key;
+  uint32_t b = 0;
+#pragma unroll 4
+  for (int i = 31; i >= 0; --i) {
+    const uint32_t t = b | 1u << i;
+    if (__popcll(__ballot(hi >= t)) >= n) b = t;
   }
+  const unsigned long long equal = __ballot(hi == b && key != 0);
+  const int want = n - __popcll(__ballot(hi > b));             // of the lanes whose value is the n-th largest, those of lowest index
+  uint32_t l = 0;
+  if (__popcll(equal) > want)
+#pragma unroll 4
+    for (int i = 31; i >= 0; --i) {
+      const uint32_t t = l | 1u << i;
+      if (__popcll(__ballot(lo >= t) & equal) >= want) l = t;
+    }
+  return (unsigned long long)b << 32 | l;
+}
+
+// list (the n best so far, sorted, 0: none) becomes the n best of itself and of the values behind all threads' `top` keys (the largest of
+// a thread's values).  gather(bound, push) hands push() every key of the thread from `bound` on; below(key): the thread's largest
+// key below it.  All keys differ, except for 0, which is none.
+template <class Gather, class Below>
+__device__ __forceinline__ void top_update(lp_shared &s, int n, unsigned long long top, Gather gather, Below below) {
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned long long b = wave_bound(top, n);
   if (tid == 0) s.count = n;
-  if ((tid & 63) == 0) s.bound[wave] = bound;
+  if ((tid & 63) == 0) s.bound[wave] = b;
   if (tid < n) s.cand[tid] = s.list[tid];
   __syncthreads();
-  bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3]));
-  const unsigned long long last = s.list[n - 1];
-  if (top >= bound)
+  unsigned long long bound = s.list[n - 1] + 1;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (order(i) >= bound) {
-        const unsigned long long k = key(i);
-        if (k > last) {
-          const int at = atomicAdd(&s.count, 1);
-          if (at < kLpCands + kLpTop) s.cand[at] = k;
-        }
-      }
+  for (int w = 0; w < 4; ++w) bound = s.bound[w] > bound ? s.bound[w] : bound;
+  if (top >= bound)
+    gather(bound, [&](unsigned long long k) {
+      const int at = atomicAdd(&s.count, 1);
+      if (at < kLpCands) s.cand[at] = k;
+    });
   __syncthreads();
   const int count = s.count;
-  if (count <= kLpCands + kLpTop) {                            // every candidate's place is the number of larger ones
+  if (count <= kLpCands) {                                     // every candidate's place is the number of larger ones
     for (int c = tid; c < count; c += kLpThreads) {
       const unsigned long long k = s.cand[c];
       int rank = 0;
-      for (int o = 0; o < count; ++o) rank += s.cand[o] > k || (s.cand[o] == k && o < c);
-      if (rank < n) s.list[rank] = k;
+#pragma unroll 8
+      for (int o = 0; o < count; ++o) rank += s.cand[o] > k;
+      if (rank < n && k) s.list[rank] = k;
     }
     __syncthreads();
     return;
   }
-  // a great many equal values: one after the other, the largest below the last one taken (s.cand[0 .. n - 1]: the list before)
+  // more than there is room for (NaN everywhere, or one thread's values far above all others'): one after the other, the largest
+  // below the last one taken (s.cand[0 .. n - 1]: the list before)
   unsigned long long prev = ~0ull;
   int old = 0;
   for (int j = 0; j < n; ++j) {
-    unsigned long long b = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const unsigned long long k = key(i);
-      if (k < prev && k > b) b = k;
-    }
-    for (int o = 32; o; o >>= 1) { const unsigned long long k = __shfl_xor(b, o); b = k > b ? k : b; }
-    if ((tid & 63) == 0) s.best[wave] = b;
+    unsigned long long k = below(prev);
+    for (int o = 32; o; o >>= 1) { const unsigned long long x = __shfl_xor(k, o); k = x > k ? x : k; }
+    if ((tid & 63) == 0) s.best[wave] = k;
     __syncthreads();
-    for (int w = 0; w < 4; ++w) b = s.best[w] > b ? s.best[w] : b;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) k = s.best[w] > k ? s.best[w] : k;
     const unsigned long long from_list = s.cand[old];
-    if (from_list > b) { b = from_list; ++old; } else prev = b;
-    if (tid == 0) s.list[j] = b;
+    if (from_list > k) { k = from_list; ++old; } else prev = k;
+    if (tid == 0) s.list[j] = k;
     __syncthreads();
   }
 }
@@ -237,57 +249,122 @@ __device__ __forceinline__ void lp_join_workgroup(lp_shared &s, float &m, float 
   for (int w = 1; w < 4; ++w) lp_join(m, z, t, s.red[w][0], s.red[w][1], s.red[w][2]);
 }
 
-template <typename T>
+// ONE: no slice has more than one chunk, whose values then stay in registers.
+template <typename T, bool ONE>
 __global__ void __launch_bounds__(kLpThreads)
 logprobs_kernel(logprob_args a) {
-  constexpr int V = a3_elem<T>::kVec, U = kLpValues / V;
+  constexpr int V = a3_elem<T>::kVec, U = kLpValues / V, kChunk = U * kLpThreads;
   typedef T vec_t __attribute__((ext_vector_type(V)));
   __shared__ lp_shared s;
+  __shared__ float noted[ONE ? 1 : kLpChunks][kLpThreads];
   const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x;
   const T *x = (const T *)a.x + (size_t)row * a.ld;
   // the row as aligned vectors: vector v holds elements v V - skew .. (skew: how far the row starts behind a 16-byte border)
   const int skew = (int)(((uintptr_t)x & 15) / sizeof(T)), n_vec = (int)(((long long)a.vocab + skew + V - 1) / V);
   const int v0 = (int)((long long)n_vec * slice / a.slices), v1 = (int)((long long)n_vec * (slice + 1) / a.slices);
   for (int j = tid; j < a.n_top; j += kLpThreads) s.list[j] = 0;
-  __syncthreads();
-  float m = -INFINITY, z = 0.f, t = 0.f;
-  for (int c = v0; c < v1; c += U * kLpThreads) {
-    float y[kLpValues];
+  // the thread's 32 values of the chunk at vector c, -inf where the row has none; their elements
+  auto load = [&](int c, vec_t (&raw)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int v = c + u * kLpThreads + tid, e = v * V - skew;
-      vec_t raw;
-      if (v < v1 && e >= 0 && e + V <= a.vocab) raw = *reinterpret_cast<const vec_t *>(x + e);
+      if (v < v1 && e >= 0 && e + V <= a.vocab) raw[u] = *reinterpret_cast<const vec_t *>(x + e);
       else
 #pragma unroll
-        for (int i = 0; i < V; ++i) raw[i] = v < v1 && e + i >= 0 && e + i < a.vocab ? x[e + i] : (T)-INFINITY;
-#pragma unroll
-      for (int i = 0; i < V; ++i) y[u * V + i] = (float)raw[i];
+        for (int i = 0; i < V; ++i) raw[u][i] = v < v1 && e + i >= 0 && e + i < a.vocab ? x[e + i] : (T)-INFINITY;
     }
-    float top = y[0];
+  };
+  auto index = [&](int c, int i) { return (c + i / V * kLpThreads + tid) * V - skew + i % V; };
+  auto key = [&](int c, int i, float y) {
+    const bool inside = c + i / V * kLpThreads + tid < v1 && (unsigned)index(c, i) < (unsigned)a.vocab;
+    return inside ? top_key(y, index(c, i)) : 0ull;
+  };
+  auto largest = [&](const vec_t (&raw)[U]) {
+    float top = (float)raw[0][0];
 #pragma unroll
-    for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, y[i]);
-    if (top > m) {
-      const float d = lp_shift(m, top), f = __builtin_amdgcn_exp2f(d);
-      t = f * fmaf(d, z, t);
-      z *= f;
-      m = top;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
+    for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, (float)raw[i / V][i % V]);
+    return top;
+  };
+  // largest key below prev, of the 32 values
+  auto largest_below = [&](int c, const vec_t (&raw)[U], unsigned long long prev) {
+    unsigned long long b = 0;
 #pragma unroll
     for (int i = 0; i < kLpValues; ++i) {
-      const float d = (y[i] - ref) * kLog2e, e = __builtin_amdgcn_exp2f(d);
-      z += e;
-      t = fmaf(e, fmaxf(d, -1e30f), t);                        // -inf: e = 0 (NaN stays in z)
+      const unsigned long long k = key(c, i, (float)raw[i / V][i % V]);
+      if (k < prev && k > b) b = k;
     }
-    if (a.n_top) {
-      const unsigned long long last = s.list[a.n_top - 1];
-      if (__syncthreads_or(last == 0 || !(top <= top_value(last)))) {
-        auto index = [&](int i) { return (c + i / V * kLpThreads + tid) * V - skew + i % V; };
-        auto inside = [&](int i) { return c + i / V * kLpThreads + tid < v1 && (unsigned)index(i) < (unsigned)a.vocab; };
-        top_update<kLpValues>(s, a.n_top, [&](int i) { return inside(i) ? top_order(y[i]) : 0u; },
-                              [&](int i) { return inside(i) ? top_key(y[i], index(i)) : 0ull; });
+    return b;
+  };
+  float m = -INFINITY, z = 0.f, t = 0.f;
+  vec_t raw[U];
+  load(v0, raw);
+  for (int g0 = v0; g0 < v1; g0 += kLpChunks * kChunk) {       // chunks between two choices of alternatives
+    const int g1 = min(v1, g0 + kLpChunks * kChunk);
+    float best = -INFINITY;
+    int best_at = g0;
+    for (int c = g0; c < g1; c += kChunk) {
+      float y[kLpValues];
+#pragma unroll
+      for (int i = 0; i < kLpValues; ++i) y[i] = (float)raw[i / V][i % V];
+      if (!ONE && c + kChunk < v1) load(c + kChunk, raw);      // on its way while this chunk is worked on
+      float top = y[0];
+#pragma unroll
+      for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, y[i]);
+      if (!ONE) noted[(c - g0) / kChunk][tid] = top;
+      if (top > best) { best = top; best_at = c; }
+      if (top > m) {
+        const float d = lp_shift(m, top), f = __builtin_amdgcn_exp2f(d);
+        t = f * fmaf(d, z, t);
+        z *= f;
+        m = top;
       }
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < kLpValues; ++i) {
+        const float d = (y[i] - ref) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+        z += e;
+        t = fmaf(e, fmaxf(d, -1e30f), t);                      // -inf: e = 0 (NaN stays in z)
+      }
+    }
+    if (a.n_top == 0) continue;
+    __syncthreads();                                           // (list of the last choice, or cleared)
+    if constexpr (ONE) {
+      top_update(s, a.n_top, largest_below(v0, raw, ~0ull),
+                 [&](unsigned long long bound, auto push) {
+#pragma unroll
+                   for (int i = 0; i < kLpValues; ++i) {
+                     const unsigned long long k = key(v0, i, (float)raw[i / V][i % V]);
+                     if (k >= bound) push(k);
+                   }
+                 },
+                 [&](unsigned long long prev) { return largest_below(v0, raw, prev); });
+    } else {
+      vec_t again[U];
+      load(best_at, again);
+      top_update(s, a.n_top, largest_below(best_at, again, ~0ull),
+                 [&](unsigned long long bound, auto push) {
+                   const float value = top_value(bound);       // NaN: every chunk has to be looked at
+                   for (int c = g0; c < g1; c += kChunk) {
+                     if (noted[(c - g0) / kChunk][tid] < value) continue;
+                     load(c, again);
+#pragma unroll
+                     for (int i = 0; i < kLpValues; ++i) {
+                       const float y = (float)again[i / V][i % V];
+                       if (y < value) continue;
+                       const unsigned long long k = key(c, i, y);
+                       if (k >= bound) push(k);
+                     }
+                   }
+                 },
+                 [&](unsigned long long prev) {
+                   unsigned long long b = 0;
+                   for (int c = g0; c < g1; c += kChunk) {
+                     load(c, again);
+                     const unsigned long long k = largest_below(c, again, prev);
+                     b = k > b ? k : b;
+                   }
+                   return b;
+                 });
     }
   }
   lp_join_workgroup(s, m, z, t);
@@ -311,12 +388,27 @@ logprobs_join_kernel(logprob_args a) {
   }
   const unsigned long long *keys = a.part_top + (size_t)row * a.slices * a.n_top;
   constexpr int N = 16;                                        // kLpSlices * kLpTop / kLpThreads
-  unsigned long long k[N];
+  unsigned long long k[N], top = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) k[i] = i * kLpThreads + tid < a.slices * a.n_top ? keys[i * kLpThreads + tid] : 0ull;
   for (int j = tid; j < a.n_top; j += kLpThreads) s.list[j] = 0;
   lp_join_workgroup(s, m, z, t);
-  if (a.n_top) top_update<N>(s, a.n_top, [&](int i) { return (uint32_t)(k[i] >> 32); }, [&](int i) { return k[i]; });
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = k[i] > top ? k[i] : top;
+  if (a.n_top)
+    top_update(s, a.n_top, top,
+               [&](unsigned long long bound, auto push) {
+#pragma unroll
+                 for (int i = 0; i < N; ++i)
+                   if (k[i] >= bound) push(k[i]);
+               },
+               [&](unsigned long long prev) {
+                 unsigned long long b = 0;
+#pragma unroll
+                 for (int i = 0; i < N; ++i)
+                   if (k[i] < prev && k[i] > b) b = k[i];
+                 return b;
+               });
   logprobs_write(a, s, row, (const T *)a.x + (size_t)row * a.ld, m, z, t);
 }
 
@@ -401,9 +493,12 @@ extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows
                  logprob_slices(n_rows, vocab, dtype == A3_BF16 ? 2 : 4), nullptr, nullptr};
   A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_token_logprobs: too many rows");
   logprob_ws(n_rows, a.slices, n_top, ws, &a);
-  auto launch = [&](auto elem) {
-    typedef decltype(elem) T;
-    hipLaunchKernelGGL(logprobs_kernel<T>, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
+  const int elem = dtype == A3_BF16 ? 2 : 4;
+  const bool one = (long long)(vocab + 2LL * a.slices * (16 / elem)) * elem <= (long long)a.slices * kLpThreads * kLpValues * elem;
+  auto launch = [&](auto e) {
+    typedef decltype(e) T;
+    auto kern = one ? logprobs_kernel<T, true> : logprobs_kernel<T, false>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
     if (a.slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)n_rows), dim3(kLpThreads), 0, (hipStream_t)stream, a);
   };
   if (dtype == A3_BF16) launch(bf16_t{});
