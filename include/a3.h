@@ -475,7 +475,7 @@ a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows, int vocab
  *   "proj_ntw"        tile of the projection GEMM (2, 3, 4: 256 weight rows x 128, 192, 256 rows; 5, 6, 7: 128 weight
  *                     rows x 192, 128, 64 rows); set, it also sends calls with few rows to that kernel instead of
  *                     the weight-streaming one
- *   "gemm_tb"         the same tiles for the GEMMs of a3_block_tail; set, their reduction is not split
+ *   "gemm_tb"         the same tiles for the GEMMs of a3_block_tail and for a3_lm_head; set, the former's reduction is not split
  *   "proj_k64", "gemm_k64"   accepted, without effect (there is one way to fetch the rows)
  * A value must not change between a3_attention_plan and the a3_fused_attention_planned calls that use its plan:
  * if "attn_wgs" does, the plan lies elsewhere in the workspace, the kernels of the planned call notice (the

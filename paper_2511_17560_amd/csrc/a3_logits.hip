@@ -21,7 +21,7 @@ struct logits_args {
 template <class P>
 __global__ void __launch_bounds__(512)
 logits_bf16_kernel(logits_args a) {
-  constexpr int IB = P::kIB, JB = P::kJB, L = P::L;
+  constexpr int IB = P::kIB, JB = P::kJB;
   extern __shared__ __align__(16) unsigned char lds[];
   int wt, xt;
   if (!gemm_tile_of(a.n_wtiles, a.n_tok_tiles, a.group, blockIdx.x, wt, xt)) return;
@@ -31,30 +31,31 @@ logits_bf16_kernel(logits_args a) {
   P::mainloop(
       acc, lds, a.K / 64,
       [&](int) -> const char * { return reinterpret_cast<const char *>((const bf16_t *)a.w + (size_t)wt * P::BM * a.K); },
-      [&](int r) -> uint32_t {
-        int q, f;
-        P::row_of(r % (16 * IB), q, f);
-        f += (r / (16 * IB)) * (P::BM / 2) + 8 * IB * q;
-        return (uint32_t)min(f, a.N - 1 - wt * P::BM) * (uint32_t)a.K * 2u;      // clamp: computed but never stored
-      },
+      [&](int r) -> uint32_t { return (uint32_t)min(r, a.N - 1 - wt * P::BM) * (uint32_t)a.K * 2u; },   // clamp: computed but never stored
       [&](int) -> const char * { return reinterpret_cast<const char *>(a.x); },
       [&](int r) -> uint32_t {
         const int m = min(xt * P::BN + r, a.n_rows - 1);
         return (uint32_t)(a.row_idx ? a.row_idx[m] : m) * (uint32_t)a.K * 2u;
       });
-  // a lane holds L consecutive features of half 0 and of half 1 of one row
-  const int feat = wt * P::BM + grp * (P::BM / 2) + L * lg;
+  // block (i, j) as the matrix instruction leaves it: a lane has four consecutive features of one row, four lanes a 64-byte run
+  // (16 consecutive features a lane, one float at a time: 512 rows of 128256 x 4096 641 us, 4096 rows 4800; this 446 and 3215).
+  // Rows of the output start anywhere a float can.
+  typedef f32x4 f32x4_any __attribute__((aligned(4)));
+  const int feat = wt * P::BM + 16 * IB * grp + 4 * lg;
 #pragma unroll
   for (int j = 0; j < JB; ++j) {
     const int tok = xt * P::BN + 16 * (JB * wn + j) + l16;
-    float lo[L], hi[L];
-    gemm_lane_values<IB, JB>(acc, j, lo, hi);
     if (tok >= a.n_rows) continue;
-    float *p = a.out + (size_t)tok * a.ld;
+    float *p = a.out + (size_t)tok * a.ld + feat;
 #pragma unroll
-    for (int e = 0; e < L; ++e) {
-      if (feat + e < a.N) p[feat + e] = lo[e];
-      if (feat + 8 * IB + e < a.N) p[feat + 8 * IB + e] = hi[e];
+    for (int i = 0; i < IB; ++i) {
+      if (feat + 16 * i + 3 < a.N) {
+        *reinterpret_cast<f32x4_any *>(p + 16 * i) = acc[i][j];
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (feat + 16 * i + e < a.N) p[16 * i + e] = acc[i][j][e];
     }
   }
 }
@@ -94,9 +95,9 @@ logits_f32_kernel(logits_args a) {
 // its own values, z = sum e^(x - m) and t = sum e^(x - m) (x - m) in units of log 2 and rescales them when a chunk brings a larger value
 // (t' = f (t + (m - m') z), f = 2^(m - m')).  Alternatives: while it reads, a thread only notes the maximum of each of its chunks.
 // Then the n-th largest of a wave's 64 lane maxima is found bit by bit with ballots: at least n values of the row are no smaller, so
-// what lies below the largest of the four waves' bounds is out, and only the chunks that reach it are looked at again (some n of
-// them, from cache) and their values ranked.  The order has no ties (a value's index is part of it), so rows of equal or masked
-// values leave no more than a few hundred candidates either.  Slices of a row are put together by a second kernel in the same way.
+// what lies below the largest of the four waves' bounds is out.  The noted chunks that reach it (some n of them) are looked at again,
+// each by half a wave, and the values found are ranked.  Where too many equal the bound (rows that are masked or constant), only the
+// larger ones are gathered, and of the equal ones the first n in the row's order.  Slices of a row are put together by a second kernel.
 struct logprob_args {
   const void *x;
   long long ld;
@@ -124,94 +125,233 @@ __device__ __forceinline__ float top_value(unsigned long long key) {
 }
 
 constexpr int kLpChunks = 20;        // chunks whose maxima are noted before their alternatives are chosen: rows up to 163840 in one go
+constexpr int kLpQueue = 512;
 
 struct lp_shared {
   float red[4][4];
-  unsigned long long bound[4];
-  int count;
+  uint32_t bound[4];
+  int count, queued, total;
+  unsigned short queue[kLpQueue];    // noted chunks to look at: chunk * 256 + thread
   unsigned long long best[4], list[kLpTop], cand[kLpCands];
 };
 
-// The n-th largest of a wave's 64 keys, or something below it that no more values reach; 0 if fewer than n lanes have a key.
-__device__ __forceinline__ unsigned long long wave_bound(unsigned long long key, int n) {
-  const uint32_t hi = (uint32_t)(key >> 32), lo = (uint32_t)key;
-  uint32_t b = 0;
-#pragma unroll 4
-  for (int i = 31; i >= 0; --i) {
-    const uint32_t t = b | 1u << i;
-    if (__popcll(__ballot(hi >= t)) >= n) b = t;
+// Sum and maximum over a wave, in every lane, by data-parallel moves (a shuffle through LDS takes 130 cycles).
+#define A3_WAVE_REDUCE(OP, X, NONE)                                                                                                    \
+  X = OP(X, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, NONE), __builtin_bit_cast(int, X), 0x111, 0xf, 0xf, false))); \
+  X = OP(X, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, NONE), __builtin_bit_cast(int, X), 0x112, 0xf, 0xf, false))); \
+  X = OP(X, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, NONE), __builtin_bit_cast(int, X), 0x114, 0xf, 0xf, false))); \
+  X = OP(X, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, NONE), __builtin_bit_cast(int, X), 0x118, 0xf, 0xf, false))); \
+  X = OP(X, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, NONE), __builtin_bit_cast(int, X), 0x142, 0xa, 0xf, false))); \
+  X = OP(X, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, NONE), __builtin_bit_cast(int, X), 0x143, 0xc, 0xf, false))); \
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, X), 63));
+__device__ __forceinline__ float lp_add(float a, float b) { return a + b; }
+__device__ __forceinline__ float wave_sum(float x) { A3_WAVE_REDUCE(lp_add, x, 0.f) }
+__device__ __forceinline__ float wave_max(float x) { A3_WAVE_REDUCE(fmaxf, x, -INFINITY) }
+#undef A3_WAVE_REDUCE
+
+// (from - to) in units of log 2: what moves a sum from reference `from` to the larger `to`.  Bounded, so that a sum whose weight
+// is 0 (masks of the type's lowest value: the difference overflows) leaves no NaN.
+__device__ __forceinline__ float lp_shift(float from, float to) { return from == -INFINITY ? 0.f : fmaxf((from - to) * kLog2e, -1e30f); }
+
+// (m, z, t) of a workgroup's threads as one, in every thread
+__device__ __forceinline__ void lp_join_workgroup(lp_shared &s, float &m, float &z, float &t) {
+  const int wave = threadIdx.x >> 6;
+  const float mw = wave_max(m), dw = lp_shift(m, mw), fw = __builtin_amdgcn_exp2f(dw);
+  const float tw = wave_sum(fw * fmaf(dw, z, t)), zw = wave_sum(fw * z);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) { s.red[wave][0] = mw; s.red[wave][1] = zw; s.red[wave][2] = tw; }
+  __syncthreads();
+  m = fmaxf(fmaxf(s.red[0][0], s.red[1][0]), fmaxf(s.red[2][0], s.red[3][0]));
+  z = t = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float d = lp_shift(s.red[w][0], m), f = __builtin_amdgcn_exp2f(d);
+    t += f * fmaf(d, s.red[w][1], s.red[w][2]);
+    z += f * s.red[w][1];
   }
-  const unsigned long long equal = __ballot(hi == b && key != 0);
-  const int want = n - __popcll(__ballot(hi > b));             // of the lanes whose value is the n-th largest, those of lowest index
-  uint32_t l = 0;
-  if (__popcll(equal) > want)
-#pragma unroll 4
-    for (int i = 31; i >= 0; --i) {
-      const uint32_t t = l | 1u << i;
-      if (__popcll(__ballot(lo >= t) & equal) >= want) l = t;
-    }
-  return (unsigned long long)b << 32 | l;
 }
 
-// list (the n best so far, sorted, 0: none) becomes the n best of itself and of the values behind all threads' `top` keys (the largest of
-// a thread's values).  gather(bound, push) hands push() every key of the thread from `bound` on; below(key): the thread's largest
-// key below it.  All keys differ, except for 0, which is none.
-template <class Gather, class Below>
-__device__ __forceinline__ void top_update(lp_shared &s, int n, unsigned long long top, Gather gather, Below below) {
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const unsigned long long b = wave_bound(top, n);
-  if (tid == 0) s.count = n;
-  if ((tid & 63) == 0) s.bound[wave] = b;
-  if (tid < n) s.cand[tid] = s.list[tid];
-  __syncthreads();
-  unsigned long long bound = s.list[n - 1] + 1;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) bound = s.bound[w] > bound ? s.bound[w] : bound;
-  if (top >= bound)
-    gather(bound, [&](unsigned long long k) {
-      const int at = atomicAdd(&s.count, 1);
-      if (at < kLpCands) s.cand[at] = k;
-    });
-  __syncthreads();
-  const int count = s.count;
-  if (count <= kLpCands) {                                     // every candidate's place is the number of larger ones
-    for (int c = tid; c < count; c += kLpThreads) {
-      const unsigned long long k = s.cand[c];
-      int rank = 0;
-#pragma unroll 8
-      for (int o = 0; o < count; ++o) rank += s.cand[o] > k;
-      if (rank < n && k) s.list[rank] = k;
-    }
-    __syncthreads();
-    return;
+// The n-th largest of a wave's 64 numbers of so many bits (0: fewer than n are not 0).
+template <int BITS>
+__device__ __forceinline__ uint32_t wave_nth(uint32_t x, int n) {
+  uint32_t b = 0;
+#pragma unroll 4
+  for (int i = BITS - 1; i >= 0; --i) {
+    const uint32_t t = b | 1u << i;
+    if (__popcll(__ballot(x >= t)) >= n) b = t;
   }
-  // more than there is room for (NaN everywhere, or one thread's values far above all others'): one after the other, the largest
-  // below the last one taken (s.cand[0 .. n - 1]: the list before)
+  return b;
+}
+
+__device__ __forceinline__ void lp_push(lp_shared &s, unsigned long long k, unsigned long long last) {
+  if (k <= last) return;
+  const int at = atomicAdd(&s.count, 1);
+  if (at < kLpCands) s.cand[at] = k;
+}
+
+// list becomes the n best candidates: every candidate's place is the number of larger ones (all differ; 0: none).
+__device__ __forceinline__ void lp_rank(lp_shared &s, int n) {
+  const int count = s.count;
+  for (int c = threadIdx.x; c < count; c += kLpThreads) {
+    const unsigned long long k = s.cand[c];
+    int rank = 0;
+#pragma unroll 8
+    for (int o = 0; o < count; ++o) rank += s.cand[o] > k;
+    if (rank < n && k) s.list[rank] = k;
+  }
+  __syncthreads();
+}
+
+// The other way where there is no room for the candidates (NaN nearly everywhere, or one thread's values far above all others'):
+// one after the other, the largest below the last one taken.  below(prev): the thread's largest key below prev.
+template <class Below>
+__device__ __forceinline__ void lp_one_by_one(lp_shared &s, int n, Below below) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid < n) s.cand[tid] = s.list[tid];                      // the list before
+  __syncthreads();
   unsigned long long prev = ~0ull;
   int old = 0;
   for (int j = 0; j < n; ++j) {
     unsigned long long k = below(prev);
     for (int o = 32; o; o >>= 1) { const unsigned long long x = __shfl_xor(k, o); k = x > k ? x : k; }
-    if ((tid & 63) == 0) s.best[wave] = k;
+    if ((tid & 63) == 0) s.best[tid >> 6] = k;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 4; ++w) k = s.best[w] > k ? s.best[w] : k;
     const unsigned long long from_list = s.cand[old];
     if (from_list > k) { k = from_list; ++old; } else prev = k;
-    if (tid == 0) s.list[j] = k;
     __syncthreads();
+    if (tid == 0) s.list[j] = k;
   }
+  __syncthreads();
 }
 
-// What a row's m, z, t and best values give.
+// A row as aligned vectors: vector v holds elements v V - skew .. (skew: how far the row starts behind a 16-byte border); a slice is
+// vectors v0 .. v1 - 1, a chunk 256 U of them, element i of a thread's 32 in vector c + 256 (i / V) + thread.
 template <typename T>
-__device__ __forceinline__ void logprobs_write(const logprob_args &a, const lp_shared &s, int row, const T *x, float m, float z, float t) {
+struct lp_row {
+  static constexpr int V = a3_elem<T>::kVec, U = kLpValues / V, kChunk = U * kLpThreads;
+  typedef T vec_t __attribute__((ext_vector_type(V)));
+  const T *x;
+  int vocab, skew, v0, v1;
+  __device__ __forceinline__ vec_t vec(int v) const {          // -inf where the slice has none
+    const int e = v * V - skew;
+    if (v < v1 && e >= 0 && e + V <= vocab) return *reinterpret_cast<const vec_t *>(x + e);
+    vec_t r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = (T)-INFINITY;
+    if (v < v1)                                                // the first or the last of a row
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (e + i >= 0 && e + i < vocab) r[i] = x[e + i];
+    return r;
+  }
+  __device__ __forceinline__ unsigned long long key(int v, int i, float y) const {
+    const int e = v * V - skew + i;
+    return v < v1 && (unsigned)e < (unsigned)vocab ? top_key(y, e) : 0ull;
+  }
+};
+
+// The n best of the list so far and of chunks g0 .. (vectors) up to g1, whose maxima are noted.  most: the order of the thread's largest
+// value, 0 if it may have none but NaN.
+template <typename T>
+__device__ void lp_choose(lp_shared &s, const lp_row<T> &r, const float (*noted)[kLpThreads], int n, int g0, int g1, uint32_t most) {
+  constexpr int V = lp_row<T>::V, kChunk = lp_row<T>::kChunk;
+  const int tid = threadIdx.x, chunks = (g1 - g0 + kChunk - 1) / kChunk;
+  constexpr int kBits = 8 * sizeof(T);                         // of a value's order: bf16 values differ in the upper 16
+  const uint32_t mine = wave_nth<kBits>(most >> (32 - kBits), n);
+  if ((tid & 63) == 0) s.bound[tid >> 6] = mine;
+  for (int pass = 0;; ++pass) {                                // 0: what reaches the bound; 1: what exceeds it, and the first equal ones
+    if (tid == 0) { s.count = n; s.queued = 0; s.total = 0; }
+    __syncthreads();
+    const uint32_t bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3])) + pass;
+    const unsigned long long last = s.list[n - 1];
+    if (tid < n) s.cand[tid] = s.list[tid];
+    for (int c = 0; c < chunks; ++c) {
+      const float y = noted[c][tid];
+      // (a chunk of NaN notes -inf: without a bound everything is looked at)
+      if (bound == 0 || top_order(y) >> (32 - kBits) >= bound) {
+        const int at = atomicAdd(&s.queued, 1);
+        if (at < kLpQueue) s.queue[at] = (unsigned short)(c * kLpThreads + tid);
+      }
+    }
+    __syncthreads();
+    const int queued = s.queued;
+    if (queued <= kLpQueue) {
+#pragma unroll 4
+      for (int q = tid >> 5; q < queued; q += kLpThreads / 32) {
+        const int id = s.queue[q], i = tid & 31;
+        const int v = g0 + id / kLpThreads * kChunk + i / V * kLpThreads + id % kLpThreads, e = v * V - r.skew + i % V;
+        if (v < r.v1 && (unsigned)e < (unsigned)r.vocab) {
+          const unsigned long long k = top_key((float)r.x[e], e);
+          if ((uint32_t)(k >> (64 - kBits)) >= bound) lp_push(s, k, last);
+        }
+      }
+    }
+    __syncthreads();
+    if (pass == 1 && queued <= kLpQueue) {
+      for (int v = g0;; v += kLpThreads) {                     // the equal ones in the row's order
+        const typename lp_row<T>::vec_t raw = r.vec(v + tid);
+        int found = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const unsigned long long k = r.key(v + tid, i, (float)raw[i]);
+          found += k != 0 && (uint32_t)(k >> (64 - kBits)) == bound - 1;
+        }
+        const int incl = a3_wave_prefix(found);
+        if ((tid & 63) == 63) s.bound[tid >> 6] = incl;        // (the bounds are not needed any more)
+        const int before = s.total;
+        __syncthreads();
+        int at = before + incl - found;
+        for (int w = 0; w < (tid >> 6); ++w) at += s.bound[w];
+        const int all = before + s.bound[0] + s.bound[1] + s.bound[2] + s.bound[3];
+        if (found && at < n)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const unsigned long long k = r.key(v + tid, i, (float)raw[i]);
+            if (k != 0 && (uint32_t)(k >> (64 - kBits)) == bound - 1 && at++ < n) lp_push(s, k, last);
+          }
+        __syncthreads();
+        if (tid == 0) s.total = all;
+        __syncthreads();
+        if (all >= n || v + kLpThreads >= g1) break;
+      }
+    }
+    if (queued <= kLpQueue && s.count <= kLpCands) break;
+    if (pass == 0) { __syncthreads(); continue; }
+    lp_one_by_one(s, n, [&](unsigned long long prev) {
+      unsigned long long b = 0;
+      for (int v = g0 + tid; v < g1; v += kLpThreads) {
+        const typename lp_row<T>::vec_t raw = r.vec(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const unsigned long long k = r.key(v, i, (float)raw[i]);
+          if (k < prev && k > b) b = k;
+        }
+      }
+      return b;
+    });
+    return;
+  }
+  lp_rank(s, n);
+}
+
+// What a row's m, z, t and best values give.  given: the logits of the first given tokens, one a thread, fetched beforehand.
+template <typename T>
+__device__ __forceinline__ float lp_given(const logprob_args &a, int row, int j, const T *x) {
+  const int tok = j < a.n_given ? a.tokens[(size_t)row * a.n_given + j] : -1;
+  return tok < 0 || tok >= a.vocab ? -INFINITY : (float)x[tok];
+}
+template <typename T>
+__device__ __forceinline__ void logprobs_write(const logprob_args &a, const lp_shared &s, int row, const T *x, float given, float m, float z, float t) {
   const float log_z = logf(z);
   const bool none = m == -INFINITY;
   if (threadIdx.x == 0 && a.entropy) a.entropy[row] = none ? __uint_as_float(0x7fc00000u) : log_z - kLn2 * t / z;
   for (int j = threadIdx.x; j < a.n_given; j += kLpThreads) {
+    if (j >= kLpThreads) given = lp_given(a, row, j, x);
     const int tok = a.tokens[(size_t)row * a.n_given + j];
-    a.logprob[(size_t)row * a.n_given + j] = tok < 0 || tok >= a.vocab ? -INFINITY : ((float)x[tok] - m) - log_z;
+    a.logprob[(size_t)row * a.n_given + j] = tok < 0 || tok >= a.vocab ? -INFINITY : (given - m) - log_z;
   }
   for (int j = threadIdx.x; j < a.n_top; j += kLpThreads) {
     const unsigned long long k = s.list[j];
@@ -220,98 +360,43 @@ __device__ __forceinline__ void logprobs_write(const logprob_args &a, const lp_s
   }
 }
 
-// (from - to) in units of log 2: what moves a sum from reference `from` to the larger `to`.  Bounded, so that a sum whose weight
-// is 0 (masks of the type's lowest value: the difference overflows) leaves no NaN.
-__device__ __forceinline__ float lp_shift(float from, float to) { return from == -INFINITY ? 0.f : fmaxf((from - to) * kLog2e, -1e30f); }
-
-// (m, z, t) of a workgroup's threads, or of pieces, as one
-__device__ __forceinline__ void lp_join(float &m, float &z, float &t, float m1, float z1, float t1) {
-  const float top = fmaxf(m, m1);
-  const float d = lp_shift(m, top), d1 = lp_shift(m1, top);
-  const float f = __builtin_amdgcn_exp2f(d), f1 = __builtin_amdgcn_exp2f(d1);
-  t = f * fmaf(d, z, t) + f1 * fmaf(d1, z1, t1);
-  z = f * z + f1 * z1;
-  m = top;
-}
-__device__ __forceinline__ void lp_join_workgroup(lp_shared &s, float &m, float &z, float &t) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    // both sides of a pair form the same numbers: the lower lane's first
-    const float m1 = __shfl_xor(m, o), z1 = __shfl_xor(z, o), t1 = __shfl_xor(t, o);
-    if (threadIdx.x & o) { float a = m1, b = z1, c = t1; lp_join(a, b, c, m, z, t); m = a; z = b; t = c; }
-    else lp_join(m, z, t, m1, z1, t1);
-  }
-  const int wave = threadIdx.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) { s.red[wave][0] = m; s.red[wave][1] = z; s.red[wave][2] = t; }
-  __syncthreads();
-  m = s.red[0][0]; z = s.red[0][1]; t = s.red[0][2];
-  for (int w = 1; w < 4; ++w) lp_join(m, z, t, s.red[w][0], s.red[w][1], s.red[w][2]);
-}
-
-// ONE: no slice has more than one chunk, whose values then stay in registers.
-template <typename T, bool ONE>
+template <typename T>
 __global__ void __launch_bounds__(kLpThreads)
 logprobs_kernel(logprob_args a) {
-  constexpr int V = a3_elem<T>::kVec, U = kLpValues / V, kChunk = U * kLpThreads;
-  typedef T vec_t __attribute__((ext_vector_type(V)));
+  typedef lp_row<T> R;
+  constexpr int V = R::V, U = R::U, kChunk = R::kChunk;
   __shared__ lp_shared s;
-  __shared__ float noted[ONE ? 1 : kLpChunks][kLpThreads];
+  __shared__ float noted[kLpChunks][kLpThreads];
   const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x;
-  const T *x = (const T *)a.x + (size_t)row * a.ld;
-  // the row as aligned vectors: vector v holds elements v V - skew .. (skew: how far the row starts behind a 16-byte border)
-  const int skew = (int)(((uintptr_t)x & 15) / sizeof(T)), n_vec = (int)(((long long)a.vocab + skew + V - 1) / V);
-  const int v0 = (int)((long long)n_vec * slice / a.slices), v1 = (int)((long long)n_vec * (slice + 1) / a.slices);
+  R r;
+  r.x = (const T *)a.x + (size_t)row * a.ld;
+  r.vocab = a.vocab;
+  r.skew = (int)(((uintptr_t)r.x & 15) / sizeof(T));
+  const int n_vec = (int)(((long long)a.vocab + r.skew + V - 1) / V);
+  r.v0 = (int)((long long)n_vec * slice / a.slices);
+  r.v1 = (int)((long long)n_vec * (slice + 1) / a.slices);
+  typename R::vec_t raw[U];
+  auto load = [&](int c) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = r.vec(c + u * kLpThreads + tid);
+  };
+  load(r.v0);
+  const float given = a.slices == 1 ? lp_given(a, row, tid, r.x) : 0.f;
   for (int j = tid; j < a.n_top; j += kLpThreads) s.list[j] = 0;
-  // the thread's 32 values of the chunk at vector c, -inf where the row has none; their elements
-  auto load = [&](int c, vec_t (&raw)[U]) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = c + u * kLpThreads + tid, e = v * V - skew;
-      if (v < v1 && e >= 0 && e + V <= a.vocab) raw[u] = *reinterpret_cast<const vec_t *>(x + e);
-      else
-#pragma unroll
-        for (int i = 0; i < V; ++i) raw[u][i] = v < v1 && e + i >= 0 && e + i < a.vocab ? x[e + i] : (T)-INFINITY;
-    }
-  };
-  auto index = [&](int c, int i) { return (c + i / V * kLpThreads + tid) * V - skew + i % V; };
-  auto key = [&](int c, int i, float y) {
-    const bool inside = c + i / V * kLpThreads + tid < v1 && (unsigned)index(c, i) < (unsigned)a.vocab;
-    return inside ? top_key(y, index(c, i)) : 0ull;
-  };
-  auto largest = [&](const vec_t (&raw)[U]) {
-    float top = (float)raw[0][0];
-#pragma unroll
-    for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, (float)raw[i / V][i % V]);
-    return top;
-  };
-  // largest key below prev, of the 32 values
-  auto largest_below = [&](int c, const vec_t (&raw)[U], unsigned long long prev) {
-    unsigned long long b = 0;
-#pragma unroll
-    for (int i = 0; i < kLpValues; ++i) {
-      const unsigned long long k = key(c, i, (float)raw[i / V][i % V]);
-      if (k < prev && k > b) b = k;
-    }
-    return b;
-  };
   float m = -INFINITY, z = 0.f, t = 0.f;
-  vec_t raw[U];
-  load(v0, raw);
-  for (int g0 = v0; g0 < v1; g0 += kLpChunks * kChunk) {       // chunks between two choices of alternatives
-    const int g1 = min(v1, g0 + kLpChunks * kChunk);
-    float best = -INFINITY;
-    int best_at = g0;
+  for (int g0 = r.v0; g0 < r.v1; g0 += kLpChunks * kChunk) {   // chunks between two choices of alternatives
+    const int g1 = min(r.v1, g0 + kLpChunks * kChunk);
+    float most = -INFINITY;
     for (int c = g0; c < g1; c += kChunk) {
       float y[kLpValues];
 #pragma unroll
       for (int i = 0; i < kLpValues; ++i) y[i] = (float)raw[i / V][i % V];
-      if (!ONE && c + kChunk < v1) load(c + kChunk, raw);      // on its way while this chunk is worked on
+      if (c + kChunk < r.v1) load(c + kChunk);                 // on its way while this chunk is worked on
       float top = y[0];
 #pragma unroll
       for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, y[i]);
-      if (!ONE) noted[(c - g0) / kChunk][tid] = top;
-      if (top > best) { best = top; best_at = c; }
+      noted[(c - g0) / kChunk][tid] = top;
+      most = fmaxf(most, top);
       if (top > m) {
         const float d = lp_shift(m, top), f = __builtin_amdgcn_exp2f(d);
         t = f * fmaf(d, z, t);
@@ -327,49 +412,12 @@ logprobs_kernel(logprob_args a) {
       }
     }
     if (a.n_top == 0) continue;
-    __syncthreads();                                           // (list of the last choice, or cleared)
-    if constexpr (ONE) {
-      top_update(s, a.n_top, largest_below(v0, raw, ~0ull),
-                 [&](unsigned long long bound, auto push) {
-#pragma unroll
-                   for (int i = 0; i < kLpValues; ++i) {
-                     const unsigned long long k = key(v0, i, (float)raw[i / V][i % V]);
-                     if (k >= bound) push(k);
-                   }
-                 },
-                 [&](unsigned long long prev) { return largest_below(v0, raw, prev); });
-    } else {
-      vec_t again[U];
-      load(best_at, again);
-      top_update(s, a.n_top, largest_below(best_at, again, ~0ull),
-                 [&](unsigned long long bound, auto push) {
-                   const float value = top_value(bound);       // NaN: every chunk has to be looked at
-                   for (int c = g0; c < g1; c += kChunk) {
-                     if (noted[(c - g0) / kChunk][tid] < value) continue;
-                     load(c, again);
-#pragma unroll
-                     for (int i = 0; i < kLpValues; ++i) {
-                       const float y = (float)again[i / V][i % V];
-                       if (y < value) continue;
-                       const unsigned long long k = key(c, i, y);
-                       if (k >= bound) push(k);
-                     }
-                   }
-                 },
-                 [&](unsigned long long prev) {
-                   unsigned long long b = 0;
-                   for (int c = g0; c < g1; c += kChunk) {
-                     load(c, again);
-                     const unsigned long long k = largest_below(c, again, prev);
-                     b = k > b ? k : b;
-                   }
-                   return b;
-                 });
-    }
+    __syncthreads();                                           // (the list: cleared, or of the last choice)
+    lp_choose(s, r, noted, a.n_top, g0, g1, g0 + tid >= g1 || (most == -INFINITY && z != z) ? 0u : top_order(most));
   }
   lp_join_workgroup(s, m, z, t);
   if (a.slices == 1) {
-    logprobs_write(a, s, row, x, m, z, t);
+    logprobs_write(a, s, row, r.x, given, m, z, t);
     return;
   }
   if (tid == 0) a.part[blockIdx.x] = make_float4(m, z, t, 0.f);
@@ -380,36 +428,44 @@ template <typename T>
 __global__ void __launch_bounds__(kLpThreads)
 logprobs_join_kernel(logprob_args a) {
   __shared__ lp_shared s;
-  const int row = blockIdx.x, tid = threadIdx.x;
+  const int row = blockIdx.x, tid = threadIdx.x, n = a.n_top;
+  const T *x = (const T *)a.x + (size_t)row * a.ld;
   float m = -INFINITY, z = 0.f, t = 0.f;
   if (tid < a.slices) {
     const float4 p = a.part[(size_t)row * a.slices + tid];
     m = p.x; z = p.y; t = p.z;
   }
-  const unsigned long long *keys = a.part_top + (size_t)row * a.slices * a.n_top;
+  const unsigned long long *keys = a.part_top + (size_t)row * a.slices * n;
   constexpr int N = 16;                                        // kLpSlices * kLpTop / kLpThreads
   unsigned long long k[N], top = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) k[i] = i * kLpThreads + tid < a.slices * a.n_top ? keys[i * kLpThreads + tid] : 0ull;
-  for (int j = tid; j < a.n_top; j += kLpThreads) s.list[j] = 0;
+  for (int i = 0; i < N; ++i) k[i] = i * kLpThreads + tid < a.slices * n ? keys[i * kLpThreads + tid] : 0ull;
+  const float given = lp_given(a, row, tid, x);
   lp_join_workgroup(s, m, z, t);
+  if (n) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) top = k[i] > top ? k[i] : top;
-  if (a.n_top)
-    top_update(s, a.n_top, top,
-               [&](unsigned long long bound, auto push) {
+    for (int i = 0; i < N; ++i) top = k[i] > top ? k[i] : top;
+    const uint32_t mine = wave_nth<32>((uint32_t)(top >> 32), n);
+    if ((tid & 63) == 0) s.bound[tid >> 6] = mine;
+    if (tid < n) s.list[tid] = 0;
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    const uint32_t bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3]));
 #pragma unroll
-                 for (int i = 0; i < N; ++i)
-                   if (k[i] >= bound) push(k[i]);
-               },
-               [&](unsigned long long prev) {
-                 unsigned long long b = 0;
+    for (int i = 0; i < N; ++i)
+      if ((uint32_t)(k[i] >> 32) >= bound) lp_push(s, k[i], 0ull);
+    __syncthreads();
+    if (s.count <= kLpCands) lp_rank(s, n);
+    else
+      lp_one_by_one(s, n, [&](unsigned long long prev) {
+        unsigned long long b = 0;
 #pragma unroll
-                 for (int i = 0; i < N; ++i)
-                   if (k[i] < prev && k[i] > b) b = k[i];
-                 return b;
-               });
-  logprobs_write(a, s, row, (const T *)a.x + (size_t)row * a.ld, m, z, t);
+        for (int i = 0; i < N; ++i)
+          if (k[i] < prev && k[i] > b) b = k[i];
+        return b;
+      });
+  }
+  logprobs_write(a, s, row, x, given, m, z, t);
 }
 
 // Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of no less than two vectors a thread.
@@ -447,7 +503,8 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
   if (L->dtype == A3_BF16) {
     A3_REQUIRE(L->hidden % 64 == 0, A3_ERR_UNSUPPORTED, "a3_lm_head: bf16 needs hidden %% 64 == 0, got %d", L->hidden);
     A3_REQUIRE((long long)L->total_tokens * L->hidden * 2 < (1LL << 32), A3_ERR_UNSUPPORTED, "a3_lm_head: hidden tensor larger than 4 GiB");
-    return gemm_with_tile(gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile, [&](auto t) -> a3_status {
+    const int knob = gemm_tile_of_knob(a3_knob(A3_KNOB_GEMM_TB));
+    return gemm_with_tile(knob >= 0 ? knob : gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile, [&](auto t) -> a3_status {
       using P = decltype(t);
       auto kern = logits_bf16_kernel<P>;
       static a3_once_per_device lds_once;
@@ -493,12 +550,9 @@ extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows
                  logprob_slices(n_rows, vocab, dtype == A3_BF16 ? 2 : 4), nullptr, nullptr};
   A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_token_logprobs: too many rows");
   logprob_ws(n_rows, a.slices, n_top, ws, &a);
-  const int elem = dtype == A3_BF16 ? 2 : 4;
-  const bool one = (long long)(vocab + 2LL * a.slices * (16 / elem)) * elem <= (long long)a.slices * kLpThreads * kLpValues * elem;
   auto launch = [&](auto e) {
     typedef decltype(e) T;
-    auto kern = one ? logprobs_kernel<T, true> : logprobs_kernel<T, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(logprobs_kernel<T>, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
     if (a.slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)n_rows), dim3(kLpThreads), 0, (hipStream_t)stream, a);
   };
   if (dtype == A3_BF16) launch(bf16_t{});
