@@ -19,7 +19,7 @@ constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) |
 // SW / SX: LDS stages of the weight and of the activation ring (a stage = 64 elements of the reduction, 128 bytes a row)
 template <int IB, int JB, int SW, int SX>
 struct gemm_pp {
-  static constexpr int kIB = IB, kJB = JB, kSW = SW, kSX = SX;
+  static constexpr int kIB = IB, kJB = JB, kSW = SW, kSX = SX, kElems = 64;
   static constexpr int BM = 32 * IB, BN = 64 * JB, L = 2 * IB;
   static constexpr int kWStage = BM * 128, kXStage = BN * 128, kXBase = SW * kWStage;
   static constexpr int kLW = BM / 32, kLX = BN / 32;           // direct-to-LDS loads per wave of a group and slab
@@ -212,10 +212,24 @@ __device__ __forceinline__ void gemm_pp<IB, JB, SW, SX>::mainloop(f32x4 (&acc)[I
 // The same product for tiles too small to keep the matrix pipe busy (few activation rows, or little left per workgroup):
 // the path from the L2 and the latencies set the pace, so all eight waves stay in the same phase, every wave brings its
 // share of both operands, and the fragments of slab s + 1 are read under the products of slab s: one barrier per slab.
-// ST: LDS stages, each of BM + BN rows.
-template <int IB, int JB, int ST>
+// ST: LDS stages, each of BM + BN rows.  MUL: what a slab's 128 bytes a row are and how a 16-byte piece of two rows is multiplied.
+struct gemm_mul_bf16 {
+  static constexpr int kElems = 64;                                     // of a slab
+  __device__ static __forceinline__ void fma(const bf16x8 &w, const bf16x8 &x, f32x4 &acc) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, acc, 0, 0, 0);
+  }
+};
+struct gemm_mul_f32 {                                                   // a piece's four floats in four instructions: the lane groups' k of each
+  static constexpr int kElems = 32;
+  __device__ static __forceinline__ void fma(const bf16x8 &w, const bf16x8 &x, f32x4 &acc) {
+    const f32x4 wf = __builtin_bit_cast(f32x4, w), xf = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[e], xf[e], acc, 0, 0, 0);
+  }
+};
+template <int IB, int JB, int ST, class MUL = gemm_mul_bf16>
 struct gemm_pl {
-  static constexpr int kIB = IB, kJB = JB;
+  static constexpr int kIB = IB, kJB = JB, kElems = MUL::kElems;
   static constexpr int BM = 32 * IB, BN = 64 * JB, L = 2 * IB;
   static constexpr int kStage = (BM + BN) * 128, kLoads = (BM + BN) / 64;
   static constexpr size_t kLdsBytes = (size_t)ST * kStage;
@@ -273,7 +287,7 @@ struct gemm_pl {
 #pragma unroll
       for (int m = 0; m < kM; ++m) {
         const int ks = m / (IB * JB), i = (m / JB) % IB, j = m % JB;
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wc[ks][i], xc[ks][j], acc[i][j], 0, 0, 0);
+        MUL::fma(wc[ks][i], xc[ks][j], acc[i][j]);
         A3_PL_FENCE
 #pragma unroll
         for (int n = m * kR / kM; n < (m + 1) * kR / kM; ++n) A3_PL_READ(n, wx, xx, rd)

@@ -5,7 +5,7 @@
 namespace {
 
 // ---------------------------------------------------------------------------------------
-// logits, bf16: the row-tiled MFMA GEMM of a3_gemm_pp.h, float out
+// logits: the row-tiled MFMA GEMM of a3_gemm_pp.h (fp32: with the fp32 matrix instruction), float out
 // ---------------------------------------------------------------------------------------
 struct logits_args {
   const void *x;           // [*, K]
@@ -18,9 +18,9 @@ struct logits_args {
   int n_wtiles, n_tok_tiles, group;
 };
 
-template <class P>
+template <typename T, class P>
 __global__ void __launch_bounds__(512)
-logits_bf16_kernel(logits_args a) {
+logits_kernel(logits_args a) {
   constexpr int IB = P::kIB, JB = P::kJB;
   extern __shared__ __align__(16) unsigned char lds[];
   int wt, xt;
@@ -29,13 +29,13 @@ logits_bf16_kernel(logits_args a) {
   const int l16 = lane & 15, lg = lane >> 4, grp = wave >> 2, wn = wave & 3;
   f32x4 acc[IB][JB];
   P::mainloop(
-      acc, lds, a.K / 64,
-      [&](int) -> const char * { return reinterpret_cast<const char *>((const bf16_t *)a.w + (size_t)wt * P::BM * a.K); },
-      [&](int r) -> uint32_t { return (uint32_t)min(r, a.N - 1 - wt * P::BM) * (uint32_t)a.K * 2u; },   // clamp: computed but never stored
+      acc, lds, a.K / P::kElems,
+      [&](int) -> const char * { return reinterpret_cast<const char *>((const T *)a.w + (size_t)wt * P::BM * a.K); },
+      [&](int r) -> uint32_t { return (uint32_t)min(r, a.N - 1 - wt * P::BM) * (uint32_t)(a.K * sizeof(T)); },   // clamp: computed but never stored
       [&](int) -> const char * { return reinterpret_cast<const char *>(a.x); },
       [&](int r) -> uint32_t {
         const int m = min(xt * P::BN + r, a.n_rows - 1);
-        return (uint32_t)(a.row_idx ? a.row_idx[m] : m) * (uint32_t)a.K * 2u;
+        return (uint32_t)(a.row_idx ? a.row_idx[m] : m) * (uint32_t)(a.K * sizeof(T));
       });
   // block (i, j) as the matrix instruction leaves it: a lane has four consecutive features of one row, four lanes a 64-byte run
   // (16 consecutive features a lane, one float at a time: 512 rows of 128256 x 4096 641 us, 4096 rows 4800; this 446 and 3215).
@@ -58,34 +58,6 @@ logits_bf16_kernel(logits_args a) {
         if (feat + 16 * i + e < a.N) p[16 * i + e] = acc[i][j][e];
     }
   }
-}
-
-// ---------------------------------------------------------------------------------------
-// logits, fp32: 64 weight rows x 16 rows a workgroup
-// ---------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256)
-logits_f32_kernel(logits_args a) {
-  constexpr int R = 16, F = 64, BK = 32;
-  __shared__ float xs[R][BK + 1], ws[F][BK + 1];
-  const int f0 = blockIdx.x * F, m0 = blockIdx.y * R, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < a.K; k0 += BK) {
-    for (int i = tid; i < R * BK; i += 256) {
-      const int m = min(m0 + i / BK, a.n_rows - 1);
-      xs[i / BK][i % BK] = ((const float *)a.x)[(size_t)(a.row_idx ? a.row_idx[m] : m) * a.K + k0 + i % BK];
-    }
-    for (int i = tid; i < F * BK; i += 256)
-      ws[i / BK][i % BK] = ((const float *)a.w)[(size_t)min(f0 + i / BK, a.N - 1) * a.K + k0 + i % BK];
-    __syncthreads();
-    for (int c = 0; c < BK; ++c)
-#pragma unroll
-      for (int f = 0; f < 4; ++f) acc[f] = fmaf(xs[ty][c], ws[tx + 16 * f][c], acc[f]);
-    __syncthreads();
-  }
-  if (m0 + ty >= a.n_rows) return;
-#pragma unroll
-  for (int f = 0; f < 4; ++f)
-    if (f0 + tx + 16 * f < a.N) a.out[(size_t)(m0 + ty) * a.ld + f0 + tx + 16 * f] = acc[f];
 }
 
 // ---------------------------------------------------------------------------------------
@@ -500,29 +472,33 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
              "a3_lm_head: tensors must be 16-byte aligned (logits 4)");
   logits_args a{hidden, row_idx, n_rows, w, logits, ld, L->hidden, vocab, 0, 0, 0};
   hipStream_t st = (hipStream_t)stream;
-  if (L->dtype == A3_BF16) {
-    A3_REQUIRE(L->hidden % 64 == 0, A3_ERR_UNSUPPORTED, "a3_lm_head: bf16 needs hidden %% 64 == 0, got %d", L->hidden);
-    A3_REQUIRE((long long)L->total_tokens * L->hidden * 2 < (1LL << 32), A3_ERR_UNSUPPORTED, "a3_lm_head: hidden tensor larger than 4 GiB");
+  const bool bf16 = L->dtype == A3_BF16;
+  A3_REQUIRE(!bf16 || L->hidden % 64 == 0, A3_ERR_UNSUPPORTED, "a3_lm_head: bf16 needs hidden %% 64 == 0, got %d", L->hidden);
+  A3_REQUIRE((long long)L->total_tokens * L->hidden * (bf16 ? 2 : 4) < (1LL << 32), A3_ERR_UNSUPPORTED,
+             "a3_lm_head: hidden tensor larger than 4 GiB");
+  auto launch = [&](auto elem, auto tile) -> a3_status {
+    using P = decltype(tile);
+    auto kern = logits_kernel<decltype(elem), P>;
+    static a3_once_per_device lds_once;
+    if (a3_once(lds_once, [&]() { return hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)P::kLdsBytes); }) != hipSuccess)
+      return a3_fail(A3_ERR_HIP, "a3_lm_head: cannot raise the dynamic LDS limit");
+    logits_args b = a;
+    b.n_wtiles = (vocab + P::BM - 1) / P::BM;
+    b.n_tok_tiles = (n_rows + P::BN - 1) / P::BN;
+    b.group = gemm_tile_group(b.n_wtiles, b.n_tok_tiles);
+    A3_REQUIRE((long long)b.n_wtiles * b.n_tok_tiles < (1LL << 28), A3_ERR_UNSUPPORTED, "a3_lm_head: too many rows");
+    hipLaunchKernelGGL(kern, dim3(gemm_tile_grid(b.n_wtiles, b.n_tok_tiles)), dim3(512), P::kLdsBytes, st, b);
+    A3_CHECK_LAUNCH("a3_lm_head");
+    return A3_OK;
+  };
+  if (bf16) {
     const int knob = gemm_tile_of_knob(a3_knob(A3_KNOB_GEMM_TB));
-    return gemm_with_tile(knob >= 0 ? knob : gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile, [&](auto t) -> a3_status {
-      using P = decltype(t);
-      auto kern = logits_bf16_kernel<P>;
-      static a3_once_per_device lds_once;
-      if (a3_once(lds_once, [&]() { return hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)P::kLdsBytes); }) != hipSuccess)
-        return a3_fail(A3_ERR_HIP, "a3_lm_head: cannot raise the dynamic LDS limit");
-      logits_args b = a;
-      b.n_wtiles = (vocab + P::BM - 1) / P::BM;
-      b.n_tok_tiles = (n_rows + P::BN - 1) / P::BN;
-      b.group = gemm_tile_group(b.n_wtiles, b.n_tok_tiles);
-      hipLaunchKernelGGL(kern, dim3(gemm_tile_grid(b.n_wtiles, b.n_tok_tiles)), dim3(512), P::kLdsBytes, st, b);
-      A3_CHECK_LAUNCH("a3_lm_head");
-      return A3_OK;
-    });
+    return gemm_with_tile(knob >= 0 ? knob : gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile, [&](auto t) { return launch(bf16_t{}, t); });
   }
-  A3_REQUIRE((n_rows + 15) / 16 <= 65535, A3_ERR_UNSUPPORTED, "a3_lm_head: too many rows");
-  hipLaunchKernelGGL(logits_f32_kernel, dim3((vocab + 63) / 64, (n_rows + 15) / 16), dim3(256), 0, st, a);
-  A3_CHECK_LAUNCH("a3_lm_head");
-  return A3_OK;
+  // fp32: bound by the matrix pipe (138 TFLOP/s at 512 rows of 32000 x 4096).  128 rows a tile, which fetch less, or 64 where those would
+  // leave compute units without a tile (65 rows of 4099 x 512, 33 tiles of 128 rows: 34 us and 21; 512 rows, 132 tiles: 38 and 42).
+  const long long tiles = (long long)((vocab + 127) / 128) * ((n_rows + 127) / 128);
+  return n_rows <= 64 || tiles < 128 ? launch(0.f, gemm_pl<4, 1, 6, gemm_mul_f32>{}) : launch(0.f, gemm_pl<4, 2, 5, gemm_mul_f32>{});
 }
 
 extern "C" size_t a3_token_logprobs_ws_bytes(int n_rows, int vocab, int n_top) {

@@ -165,7 +165,7 @@ __device__ __forceinline__ bf16x8 codes8(const uint32_t (&w)[2]) {
 }
 
 // A step of a workgroup is 4 SK slots of one (row, KV head), SK a wave: 32, or 16 with fp32 pages.  The steps of the call, rows first, then
-// KV heads, then slots, are cut into as many equal runs as there are workgroups, whatever the lengths are: every workgroup
+// KV heads, then slots, are cut into as many runs, equal to one step, as there are workgroups, whatever the lengths are: every workgroup
 // forms the running sum of the rows' steps itself (lengths live on the device).  An item (row, KV head) that ends up whole in
 // one workgroup is finished there; of one that is cut, every workgroup leaves a piece in ws and a second kernel joins them.
 //
@@ -223,53 +223,67 @@ paged_attention_kernel(attend_args a) {
   using F = attend_form<T, D, Q8>;
   constexpr int SK = F::SK, kShift = SK == 16 ? 6 : 7, kOS = D + 4;
   static_assert(F::kStep == 1 << kShift, "step");
-  __shared__ int scan[6];
+  __shared__ int scan[8], found[5];
   __shared__ float2 ml[4][16];
   __shared__ __align__(16) float os[4][16][kOS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, lg = lane >> 4, G = a.p.Hq / a.p.Hkv, Hkv = a.p.Hkv;
 
   // ---- this workgroup's run of steps -----------------------------------------------------------------------
-  int mine = 0;
-  for (int r = tid; r < a.n_rows; r += 256) mine += steps_of(a, r, kShift);
-  for (int o = 32; o; o >>= 1) mine += __shfl_xor(mine, o);
-  if (lane == 0) scan[wave] = mine;
+  // Up to 256 rows: one thread a row.  More: the rows' sum first, then blocks of 256 rows up to the one the run begins in.
+  int st = tid < a.n_rows ? steps_of(a, tid, kShift) : 0, incl = a3_wave_prefix(st), sum = incl;
+  if (a.n_rows > 256) {
+    int mine = st;
+    for (int r = tid + 256; r < a.n_rows; r += 256) mine += steps_of(a, r, kShift);
+    sum = a3_wave_prefix(mine);
+  }
+  if (lane == 63) { scan[wave] = sum; scan[4 + wave] = incl; }
   __syncthreads();
-  const int total = (scan[0] + scan[1] + scan[2] + scan[3]) * Hkv;
-  const int each = (total + a.shares - 1) / a.shares, first = min((int)blockIdx.x * each, total), n_steps = min(each, total - first);
-  if (n_steps <= 0) {
-    if (tid == 0) a.cut[blockIdx.x] = make_int2(-1, 0);
+  const int total = (scan[0] + scan[1] + scan[2] + scan[3]) * Hkv, w = blockIdx.x;
+  const int each = total / a.shares, rest = total - each * a.shares;      // the first `rest` workgroups take one more
+  const int first = w * each + min(w, rest), n_steps = each + (w < rest ? 1 : 0);
+  if (n_steps == 0) {
+    if (tid == 0) a.cut[w] = make_int2(-1, 0);
     return;
   }
-  int before = 0;                                              // steps of the rows in front of a block of 256 rows
-  for (int r0 = 0;; r0 += 256) {
-    __syncthreads();
-    const int st = r0 + tid < a.n_rows ? steps_of(a, r0 + tid, kShift) : 0;
-    const int incl = a3_wave_prefix(st);
-    if (lane == 63) scan[wave] = incl;
-    __syncthreads();
+  for (int r0 = 0, before = 0;;) {                             // before: steps of the rows in front of this block
     int base = before;
-    for (int w = 0; w < wave; ++w) base += scan[w];
+    for (int i = 0; i < wave; ++i) base += scan[4 + i];
     const int lo = (base + incl - st) * Hkv, hi = (base + incl) * Hkv;
-    before += scan[0] + scan[1] + scan[2] + scan[3];
-    if (first >= lo && first < hi) { scan[4] = r0 + tid; scan[5] = first - lo; }
+    if (first >= lo && first < hi) {
+      const int r = r0 + tid;
+      found[0] = r;
+      found[1] = first - lo;
+      found[2] = st;
+      found[3] = max(0, min(a.row_len[r], a.p.slots));
+      found[4] = a.row_req ? a.row_req[r] : r;
+    }
+    before += scan[4] + scan[5] + scan[6] + scan[7];
     if (before * Hkv > first) break;
+    r0 += 256;
+    st = r0 + tid < a.n_rows ? steps_of(a, r0 + tid, kShift) : 0;
+    incl = a3_wave_prefix(st);
+    __syncthreads();
+    if (lane == 63) scan[4 + wave] = incl;
+    __syncthreads();
   }
   __syncthreads();
 
   // ---- where the workgroup stands: a step of a row's KV head (all scalar) ------------------------------------------
   struct place { int row, head, step, steps, len, req; };
   place now;
-  now.row = __builtin_amdgcn_readfirstlane(scan[4]);
-  const int inside = __builtin_amdgcn_readfirstlane(scan[5]);
-  auto enter = [&](place &p) {                                 // the row's own numbers
+  now.row = __builtin_amdgcn_readfirstlane(found[0]);
+  now.steps = __builtin_amdgcn_readfirstlane(found[2]);
+  now.len = __builtin_amdgcn_readfirstlane(found[3]);
+  now.req = __builtin_amdgcn_readfirstlane(found[4]);
+  const int inside = __builtin_amdgcn_readfirstlane(found[1]);
+  now.head = inside / now.steps;
+  now.step = inside - now.head * now.steps;
+  auto enter = [&](place &p) {                                 // another row's own numbers
     p.req = __builtin_amdgcn_readfirstlane(a.row_req ? a.row_req[p.row] : p.row);
     p.len = __builtin_amdgcn_readfirstlane(max(0, min(a.row_len[p.row], a.p.slots)));
     p.steps = __builtin_amdgcn_readfirstlane(steps_of(a, p.row, kShift));
   };
-  enter(now);
-  now.head = inside / now.steps;
-  now.step = inside - now.head * now.steps;
   auto advance = [&](place &p) {
     if (++p.step < p.steps) return;
     p.step = 0;
@@ -560,7 +574,9 @@ paged_attention_kernel(attend_args a) {
       finish(now, begins, ends);
       if (begins && !ends) {                                   // goes on in the workgroups behind: how many of them
         cut_item = now.row * Hkv + now.head;
-        cut_pieces = 1 + (now.steps - 1 - now.step + each - 1) / each;
+        // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+        const int last = first + i + now.steps - 1 - now.step, fat = rest * (each + 1);
+        cut_pieces = 1 - w + (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1));
       }
       if (more) {
         begins = true;
@@ -574,55 +590,62 @@ paged_attention_kernel(attend_args a) {
     step(i, sa, sb);
     if (i + 1 < n_steps) step(i + 1, sb, sa);
   }
-  if (tid == 0) a.cut[blockIdx.x] = make_int2(cut_item, cut_pieces);
+  if (tid == 0) a.cut[w] = make_int2(cut_item, cut_pieces);
 }
 
-// Joins the pieces of the item that goes on after workgroup blockIdx.x, query head blockIdx.y of its KV head.
+// Joins the pieces of the item that goes on after workgroup blockIdx.x.  A thread sums four coordinates of one query head over every
+// kth piece, all loads of four pieces on their way together; then the k partial sums are joined.  Nothing but latency: of the
+// 512 workgroups those without such an item end at once.
+constexpr int kJoinThreads = 512;
 template <typename T, int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kJoinThreads)
 paged_attention_join_kernel(attend_args a) {
-  constexpr int kGroups = 256 / D;
-  __shared__ float factor[1024], red[4], sum[256];
-  const int2 cut = a.cut[blockIdx.x];
+  __shared__ f32x4 os[kJoinThreads];
+  __shared__ float2 mls[kJoinThreads];
+  const int w = blockIdx.x, tid = threadIdx.x, G = a.p.Hq / a.p.Hkv, units = G * (D / 4), groups = kJoinThreads / units;
+  const int2 cut = a.cut[w];
   if (cut.x < 0) return;
-  const int tid = threadIdx.x, g = blockIdx.y, G = a.p.Hq / a.p.Hkv, n = cut.y, w = blockIdx.x;
-  auto slot_of = [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); };
-  float M = -INFINITY;
+  const int gr = tid / units, u = tid - gr * units, g = u / (D / 4), n = cut.y;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
   bool seen = false;
-  for (int i = tid; i < n; i += 256) {
-    factor[i] = a.part_ml[(size_t)slot_of(i) * G + g].x;
-    M = fmaxf(M, factor[i]);
-    seen |= a.part_seen[slot_of(i)] != 0;
-  }
-  for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-  if ((tid & 63) == 0) red[tid >> 6] = M;
-  seen = __syncthreads_or(seen);
-  M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  float L = 0.f;
-  for (int i = tid; i < n; i += 256) {
-    const float f = factor[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(factor[i] - M);
-    factor[i] = f;
-    if (f != 0.f) L += f * a.part_ml[(size_t)slot_of(i) * G + g].y;
-  }
-  for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
-  __syncthreads();
-  if ((tid & 63) == 0) red[tid >> 6] = L;
-  __syncthreads();
-  L = (red[0] + red[1]) + (red[2] + red[3]);
-  const int d = tid % D;
-  float o = 0.f;
-#pragma unroll 4
-  for (int i = tid / D; i < n; i += kGroups) {
-    const float x = a.part_o[((size_t)slot_of(i) * G + g) * D + d];
-    if (factor[i] != 0.f) o += factor[i] * x;
-  }
-  sum[tid] = o;
-  __syncthreads();
-  if (tid >= D) return;
-  o = 0.f;
+  if (gr < groups)
+    for (int i = gr; i < n; i += 4 * groups) {
+      f32x4 x[4];
+      float2 ml[4];
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) o += sum[tid + i * D];
-  ((T *)a.out)[((size_t)(cut.x / a.p.Hkv) * a.p.Hq + (cut.x % a.p.Hkv) * G + g) * D + tid] = (T)(seen ? o / L : 0.f);
+      for (int k = 0; k < 4; ++k) {
+        const int p = min(i + k * groups, n - 1), slot = p == 0 ? 2 * w + 1 : 2 * (w + p);
+        x[k] = *reinterpret_cast<const f32x4 *>(a.part_o + (size_t)slot * G * D + 4 * u);
+        ml[k] = a.part_ml[(size_t)slot * G + g];
+        seen |= a.part_seen[slot] != 0;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i + k * groups >= n || ml[k].x == -INFINITY) continue;
+        const float top = fmaxf(m, ml[k].x), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), f1 = __builtin_amdgcn_exp2f(ml[k].x - top);
+        o = o * f + x[k] * f1;
+        l = l * f + ml[k].y * f1;
+        m = top;
+      }
+    }
+  os[tid] = o;
+  mls[tid] = make_float2(m, l);
+  seen = __syncthreads_or(seen);
+  if (gr != 0) return;
+  for (int k = 1; k < groups; ++k) {
+    const float2 ml = mls[k * units + u];
+    if (ml.x == -INFINITY) continue;
+    const float top = fmaxf(m, ml.x), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), f1 = __builtin_amdgcn_exp2f(ml.x - top);
+    o = o * f + os[k * units + u] * f1;
+    l = l * f + ml.y * f1;
+    m = top;
+  }
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  vec4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (T)(seen ? o[e] / l : 0.f);
+  *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(cut.x / a.p.Hkv) * a.p.Hq + (cut.x % a.p.Hkv) * G) * D + 4 * u) = y;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -777,10 +800,9 @@ extern "C" a3_status a3_paged_attention(const a3_pages *P, const void *q, const 
   const size_t need = attend_ws(P, shares, ws, &a);
   A3_REQUIRE(ws && a3_aligned16(ws) && ws_bytes >= need, A3_ERR_WORKSPACE, "a3_paged_attention: workspace %zu bytes (16-byte aligned), need %zu",
              ws ? ws_bytes : 0, need);
-  const dim3 join((unsigned)shares, (unsigned)(P->n_q_heads / P->n_kv_heads));
   with_format(P, [&](auto elem, auto d, auto q8) {
     hipLaunchKernelGGL((paged_attention_kernel<decltype(elem), d.value, q8.value>), dim3((unsigned)shares), dim3(256), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL((paged_attention_join_kernel<decltype(elem), d.value>), join, dim3(256), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((paged_attention_join_kernel<decltype(elem), d.value>), dim3((unsigned)shares), dim3(kJoinThreads), 0, (hipStream_t)stream, a);
   });
   A3_CHECK_LAUNCH("a3_paged_attention");
   return A3_OK;
