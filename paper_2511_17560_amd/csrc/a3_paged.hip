@@ -170,7 +170,7 @@ __device__ __forceinline__ bf16x8 codes8(const uint32_t (&w)[2]) {
 // one workgroup is finished there; of one that is cut, every workgroup leaves a piece in ws and a second kernel joins them.
 //
 // Matrix instructions, operands straight from memory to registers, no LDS: S^T = K Q^T puts the query heads of the KV head (16
-// columns, those past G zero) beside the slots (rows), and O^T = V^T P^T wants of a lane 8 consecutive slots of one coordinate.
+// columns) beside the slots (rows), and O^T = V^T P^T wants of a lane 8 consecutive slots of one coordinate.
 //   - which slot a row of S^T is, is free: row i of block b is slot 8 (i / 4) + 4 b + i % 4, so that the weights a lane (column
 //     l16, lane group lg) gets are those of slots 8 lg .. 8 lg + 7, the P^T operand as it stands
 //   - which coordinate a row of O^T is, is free too: row l16 of block c is coordinate E l16 + c, so that a lane loads E consecutive
@@ -191,7 +191,8 @@ struct attend_args {
   float *part_o;           // [2 * shares, G, D] pieces: 2 w the one that began before workgroup w, 2 w + 1 the one that goes on after it
   float2 *part_ml;         // [2 * shares, G] (maximum, sum)
   int *part_seen;          // [2 * shares] whether the piece has a slot at all
-  int2 *cut;               // [shares] the item that goes on after workgroup w (-1: none), and its pieces
+  int2 *cut;               // [shares] the item that goes on after workgroup w (-1: none), and its pieces; or, with few items,
+  int by_item;             // [items] the workgroup that item begins in, and its pieces
 };
 
 template <typename T, int D, bool Q8>
@@ -243,7 +244,7 @@ paged_attention_kernel(attend_args a) {
   const int each = total / a.shares, rest = total - each * a.shares;      // the first `rest` workgroups take one more
   const int first = w * each + min(w, rest), n_steps = each + (w < rest ? 1 : 0);
   if (n_steps == 0) {
-    if (tid == 0) a.cut[w] = make_int2(-1, 0);
+    if (tid == 0 && !a.by_item) a.cut[w] = make_int2(-1, 0);
     return;
   }
   for (int r0 = 0, before = 0;;) {                             // before: steps of the rows in front of this block
@@ -344,25 +345,21 @@ paged_attention_kernel(attend_args a) {
   f32x4 qf[F::kF32 ? NQ : 1];
   bf16x8 qb[F::kF32 ? 1 : F::kQParts][F::kF32 ? 1 : NQ];
   auto load_queries = [&](const place &p) {
+    // (columns past G repeat the last head: nothing of them is stored)
     const T *q = (const T *)a.q + ((size_t)p.row * a.p.Hq + p.head * G + min(l16, G - 1)) * D;
-    const bool on = l16 < G;
     if constexpr (F::kF32) {
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(q + 16 * i + 4 * lg);
-        qf[i] = on ? x : f32x4{0.f, 0.f, 0.f, 0.f};
-      }
+      for (int i = 0; i < NQ; ++i) qf[i] = *reinterpret_cast<const f32x4 *>(q + 16 * i + 4 * lg);
     } else {
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
         const T *at = q + (Q8 ? 64 * (i >> 1) + 16 * lg + 8 * (i & 1) : 32 * i + 8 * lg);
         if constexpr (sizeof(T) == 2) {
-          const bf16x8 x = *reinterpret_cast<const bf16x8 *>(at), zero = {};
-          qb[0][i] = on ? x : zero;
+          qb[0][i] = *reinterpret_cast<const bf16x8 *>(at);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {                        // x as the sum of three bf16
-            float x = on ? at[e] : 0.f;
+            float x = at[e];
 #pragma unroll
             for (int k = 0; k < F::kQParts; ++k) {
               const bf16_t h = a3_f2bf(x);
@@ -571,16 +568,22 @@ paged_attention_kernel(attend_args a) {
     compute(cur);
     const bool ends = now.step == now.steps - 1;
     if (ends || !more) {
+      if (more) load_queries(next);                            // on their way while the item is put together
       finish(now, begins, ends);
-      if (begins && !ends) {                                   // goes on in the workgroups behind: how many of them
-        cut_item = now.row * Hkv + now.head;
-        // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
-        const int last = first + i + now.steps - 1 - now.step, fat = rest * (each + 1);
-        cut_pieces = 1 - w + (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1));
+      if (begins) {
+        const int item = now.row * Hkv + now.head;
+        int pieces = 1;
+        if (!ends) {                                           // goes on in the workgroups behind: how many of them
+          // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+          const int last = first + i + now.steps - 1 - now.step, fat = rest * (each + 1);
+          pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+          cut_item = item;
+          cut_pieces = pieces;
+        }
+        if (a.by_item && tid == 0) a.cut[item] = make_int2(w, pieces);
       }
       if (more) {
         begins = true;
-        load_queries(next);
         clear();
       }
     }
@@ -590,62 +593,84 @@ paged_attention_kernel(attend_args a) {
     step(i, sa, sb);
     if (i + 1 < n_steps) step(i + 1, sb, sa);
   }
-  if (tid == 0) a.cut[w] = make_int2(cut_item, cut_pieces);
+  if (tid == 0 && !a.by_item) a.cut[w] = make_int2(cut_item, cut_pieces);
 }
 
-// Joins the pieces of the item that goes on after workgroup blockIdx.x.  A thread sums four coordinates of one query head over every
-// kth piece, all loads of four pieces on their way together; then the k partial sums are joined.  Nothing but latency: of the
-// 512 workgroups those without such an item end at once.
-constexpr int kJoinThreads = 512;
+// Joins the pieces of an item: of item blockIdx.x, query head blockIdx.y (few items), or of the one that goes on after workgroup
+// blockIdx.x, as many of its heads' coordinates as there are threads.  A thread sums four coordinates over every kth piece, all
+// loads of eight pieces on their way together; then the k partial sums are joined.  Nothing but latency, and as few waves to
+// start as possible (1024 threads for each of 512 workgroups: 10 us, where this takes 5).
+constexpr int kJoinThreads = 256;
+__host__ __device__ inline int join_units(int by_item, int G, int D) {         // four coordinates each, of a workgroup
+  return by_item || G * (D / 4) < kJoinThreads ? (by_item ? D / 4 : G * (D / 4)) : kJoinThreads;
+}
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads)
 paged_attention_join_kernel(attend_args a) {
   __shared__ f32x4 os[kJoinThreads];
   __shared__ float2 mls[kJoinThreads];
-  const int w = blockIdx.x, tid = threadIdx.x, G = a.p.Hq / a.p.Hkv, units = G * (D / 4), groups = kJoinThreads / units;
-  const int2 cut = a.cut[w];
-  if (cut.x < 0) return;
-  const int gr = tid / units, u = tid - gr * units, g = u / (D / 4), n = cut.y;
+  const int tid = threadIdx.x, G = a.p.Hq / a.p.Hkv, units = join_units(a.by_item, G, D), groups = kJoinThreads / units;
+  const int2 cut = a.cut[blockIdx.x];
+  int w = blockIdx.x, item = cut.x;
+  const int n = cut.y;
+  if (a.by_item) {
+    item = blockIdx.x;
+    w = cut.x;
+    if (steps_of(a, item / a.p.Hkv, 30) == 0) return;          // a row that does not exist: `cut` says nothing
+  }
+  if (item < 0 || n < 2) return;
+  const int gr = tid / units, v = tid - gr * units, u = blockIdx.y * units + v, g = u / (D / 4);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  bool seen = false;
-  if (gr < groups)
-    for (int i = gr; i < n; i += 4 * groups) {
-      f32x4 x[4];
-      float2 ml[4];
+  int seen = 0;
+  constexpr int K = 8;
+  if (gr < groups && g < G)
+    for (int i = gr; i < n; i += K * groups) {
+      f32x4 x[K];
+      float2 ml[K];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < K; ++k) {
         const int p = min(i + k * groups, n - 1), slot = p == 0 ? 2 * w + 1 : 2 * (w + p);
         x[k] = *reinterpret_cast<const f32x4 *>(a.part_o + (size_t)slot * G * D + 4 * u);
         ml[k] = a.part_ml[(size_t)slot * G + g];
-        seen |= a.part_seen[slot] != 0;
+        seen |= a.part_seen[slot];
       }
+      float top = m;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (i + k * groups >= n || ml[k].x == -INFINITY) continue;
-        const float top = fmaxf(m, ml[k].x), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), f1 = __builtin_amdgcn_exp2f(ml[k].x - top);
-        o = o * f + x[k] * f1;
-        l = l * f + ml[k].y * f1;
-        m = top;
+      for (int k = 0; k < K; ++k) {
+        if (i + k * groups >= n) ml[k].x = -INFINITY;
+        top = fmaxf(top, ml[k].x);
+      }
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      o *= f;
+      l *= f;
+      m = top;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const float f1 = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - top);
+        if (f1 != 0.f) { o += x[k] * f1; l += ml[k].y * f1; }
       }
     }
   os[tid] = o;
   mls[tid] = make_float2(m, l);
   seen = __syncthreads_or(seen);
-  if (gr != 0) return;
-  for (int k = 1; k < groups; ++k) {
-    const float2 ml = mls[k * units + u];
-    if (ml.x == -INFINITY) continue;
-    const float top = fmaxf(m, ml.x), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), f1 = __builtin_amdgcn_exp2f(ml.x - top);
-    o = o * f + os[k * units + u] * f1;
-    l = l * f + ml.y * f1;
-    m = top;
+  if (gr != 0 || g >= G) return;
+#pragma unroll 8
+  for (int k = 1; k < groups; ++k) m = fmaxf(m, mls[k * units + v].x);
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < groups; ++k) {
+    const float2 ml = mls[k * units + v];
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+    o += os[k * units + v] * f;
+    l += ml.y * f;
   }
   typedef T vec4 __attribute__((ext_vector_type(4)));
   vec4 y;
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = (T)(seen ? o[e] / l : 0.f);
-  *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(cut.x / a.p.Hkv) * a.p.Hq + (cut.x % a.p.Hkv) * G) * D + 4 * u) = y;
+  *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(item / a.p.Hkv) * a.p.Hq + (item % a.p.Hkv) * G) * D + 4 * u) = y;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -794,15 +819,18 @@ extern "C" a3_status a3_paged_attention(const a3_pages *P, const void *q, const 
   A3_REQUIRE(a3_aligned16(q) && a3_aligned16(out), A3_ERR_INVALID_ARG, "a3_paged_attention: tensors must be 16-byte aligned");
   A3_REQUIRE(attend_steps(P, n_rows) < (1LL << 31) - 1024 && (long long)n_rows * P->n_q_heads < (1LL << 31), A3_ERR_UNSUPPORTED,
              "a3_paged_attention: too many rows for a page table of this width");
-  const int shares = attend_shares(P, n_rows);
+  const int shares = attend_shares(P, n_rows), items = n_rows * P->n_kv_heads, G = P->n_q_heads / P->n_kv_heads;
   attend_args a{args_of(P), q, out, row_req, row_len, n_rows, shares,
                 (float)((P->sm_scale != 0.f ? (double)P->sm_scale : 1.0 / sqrt((double)P->head_dim)) * 1.4426950408889634074)};
   const size_t need = attend_ws(P, shares, ws, &a);
   A3_REQUIRE(ws && a3_aligned16(ws) && ws_bytes >= need, A3_ERR_WORKSPACE, "a3_paged_attention: workspace %zu bytes (16-byte aligned), need %zu",
              ws ? ws_bytes : 0, need);
+  a.by_item = items <= shares && items * G <= kMaxShares;
+  const int units = join_units(a.by_item, G, P->head_dim);
+  const dim3 join((unsigned)(a.by_item ? items : shares), (unsigned)((G * (P->head_dim / 4) + units - 1) / units));
   with_format(P, [&](auto elem, auto d, auto q8) {
     hipLaunchKernelGGL((paged_attention_kernel<decltype(elem), d.value, q8.value>), dim3((unsigned)shares), dim3(256), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL((paged_attention_join_kernel<decltype(elem), d.value>), dim3((unsigned)shares), dim3(kJoinThreads), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((paged_attention_join_kernel<decltype(elem), d.value>), join, dim3(kJoinThreads), 0, (hipStream_t)stream, a);
   });
   A3_CHECK_LAUNCH("a3_paged_attention");
   return A3_OK;
