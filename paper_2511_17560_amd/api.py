@@ -176,8 +176,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:           # the current stream's handle (what torch.cuda.current_stream().cuda_stream is, 2.5 us sooner)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -296,6 +296,8 @@ class Pages:
         s.n_req, s.max_pages = page_table.shape
         s.k_pool, s.v_pool, s.page_table, s.rope_cs = _ptr(self.k_pool), _ptr(self.v_pool), _ptr(page_table), _ptr(self.rope_cs)
         self.struct = s
+        self.ref = C.byref(s)
+        self.torch_dtype, self.kv_elems, self.q_elems = torch_dtype(dtype), n_kv_heads * head_dim, n_q_heads * head_dim
         if fresh:
             a3_pages_prepare(self, stream)
 
@@ -305,10 +307,6 @@ class Pages:
         return Pages(dtype=self.dtype, n_q_heads=s.n_q_heads, n_kv_heads=s.n_kv_heads, head_dim=s.head_dim, page_size=s.page_size,
                      n_pages=s.n_pages, page_table=self.page_table, rope_base=s.rope_base, n_pos=s.n_pos, rope_layout=s.rope_layout,
                      q8=self.q8, sm_scale=s.sm_scale, rope_cs=self.rope_cs)
-
-    @property
-    def ref(self):
-        return C.byref(self.struct)
 
     def workspace(self, n_rows: int) -> torch.Tensor:
         return torch.empty(max(a3_paged_attention_ws_bytes(self, n_rows), 256), dtype=torch.uint8, device=self.device)
@@ -589,23 +587,27 @@ def a3_pages_prepare(pages: Pages, stream=None) -> None:
     _check(lib().a3_pages_prepare(pages.ref, _stream(stream)), "a3_pages_prepare")
 
 
-def _rows(where: torch.device, n_rows: int, dtype: torch.dtype, elems: int, **tensors) -> None:
-    """Refuses tensors that do not hold ``n_rows`` rows of ``elems`` elements of a type on the device the call runs on."""
-    if where.type != "cuda" or where.index != torch.cuda.current_device():
-        raise ValueError(f"the call's tensors are on {where}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in tensors.items():
-        if t is not None and not (t.device == where and t.dtype == dtype and t.dim() and t.shape[0] >= n_rows
-                                  and t.numel() == t.shape[0] * elems):
-            raise ValueError(f"{name}: {n_rows} rows of {elems} {dtype} on {where} are needed, got {tuple(t.shape)} {t.dtype} on {t.device}")
+def _current(where: torch.device) -> int:
+    """The index of the device a call's tensors are on, which has to be the current one."""
+    if where.type != "cuda" or where.index not in (None, torch.cuda.current_device()):
+        raise ValueError(f"the call's tensors are on {where}, the current device is another one")
+    return torch.cuda.current_device()
+
+
+def _hold(dev: int, dtype: torch.dtype, elems: int, *tensors) -> None:
+    """Refuses tensors that are not ``elems`` elements (or more) of a type on device ``dev``."""
+    for t in tensors:
+        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.numel() < elems):
+            raise ValueError(f"{elems} elements of {dtype} on cuda:{dev} are needed, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
 def a3_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row_req: Optional[torch.Tensor], row_slot: torch.Tensor,
                     row_pos: Optional[torch.Tensor], n_rows: int, q: Optional[torch.Tensor] = None,
                     q_out: Optional[torch.Tensor] = None, stream=None) -> None:
-    s, dt = pages.struct, torch_dtype(pages.dtype)
-    _rows(pages.device, n_rows, dt, s.n_kv_heads * s.head_dim, k=k, v=v)
-    _rows(pages.device, n_rows, dt, s.n_q_heads * s.head_dim, q=q, q_out=q_out)
-    _rows(pages.device, n_rows, torch.int32, 1, row_req=row_req, row_slot=row_slot, row_pos=row_pos)
+    dev = _current(pages.device)
+    _hold(dev, pages.torch_dtype, n_rows * pages.kv_elems, k, v)
+    _hold(dev, pages.torch_dtype, n_rows * pages.q_elems, q, q_out)
+    _hold(dev, torch.int32, n_rows, row_req, row_slot, row_pos)
     _check(lib().a3_paged_append(pages.ref, _ptr(k), _ptr(v), _ptr(row_req), _ptr(row_slot), _ptr(row_pos), int(n_rows), _ptr(q),
                                  _ptr(q_out), _stream(stream)), "a3_paged_append")
 
@@ -616,10 +618,10 @@ def a3_paged_attention_ws_bytes(pages: Pages, n_rows: int) -> int:
 
 def a3_paged_attention(pages: Pages, q: torch.Tensor, row_req: Optional[torch.Tensor], row_len: torch.Tensor, n_rows: int,
                        out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
-    s = pages.struct
-    _rows(pages.device, n_rows, torch_dtype(pages.dtype), s.n_q_heads * s.head_dim, q=q, out=out)
-    _rows(pages.device, n_rows, torch.int32, 1, row_req=row_req, row_len=row_len)
-    _rows(pages.device, 0, torch.uint8, 1, ws=ws)
+    dev = _current(pages.device)
+    _hold(dev, pages.torch_dtype, n_rows * pages.q_elems, q, out)
+    _hold(dev, torch.int32, n_rows, row_req, row_len)
+    _hold(dev, torch.uint8, 0, ws)
     _check(lib().a3_paged_attention(pages.ref, _ptr(q), _ptr(row_req), _ptr(row_len), int(n_rows), _ptr(out), _ptr(ws),
                                     ws.numel() if ws is not None else 0, _stream(stream)), "a3_paged_attention")
 
@@ -627,13 +629,16 @@ def a3_paged_attention(pages: Pages, q: torch.Tensor, row_req: Optional[torch.Te
 def a3_lm_head(layout: Layout, hidden: torch.Tensor, row_idx: Optional[torch.Tensor], n_rows: int, w: torch.Tensor,
                logits: torch.Tensor, stream=None) -> None:
     """``w`` [vocab, hidden]; ``logits`` float32 [>= n_rows, vocab], rows may be further apart than vocab."""
-    dt, h = torch_dtype(layout.dtype), layout.struct.hidden
-    _rows(hidden.device, 0 if row_idx is not None else n_rows, dt, h, hidden=hidden)
-    _rows(hidden.device, 0, dt, h, w=w)
-    _rows(hidden.device, n_rows, torch.int32, 1, row_idx=row_idx)
-    _rows(hidden.device, n_rows, torch.float32, w.shape[0], logits=logits)
-    if logits.dim() != 2 or logits.stride(1) != 1 or logits.stride(0) < logits.shape[1]:
-        raise ValueError("a3_lm_head: logits are rows of consecutive elements")
+    h, vocab = layout.struct.hidden, w.shape[0]
+    dev = _current(layout.device)
+    _hold(dev, torch_dtype(layout.dtype), 0 if row_idx is not None else n_rows * h, hidden)
+    _hold(dev, torch_dtype(layout.dtype), vocab * h, w)
+    _hold(dev, torch.int32, n_rows, row_idx)
+    _hold(dev, torch.float32, 0, logits)
+    if w.dim() != 2 or w.shape[1] != h or logits.dim() != 2 or logits.shape[0] < n_rows or logits.shape[1] != vocab \
+            or logits.stride(1) != 1 or (logits.shape[0] > 1 and logits.stride(0) < vocab):
+        raise ValueError(f"a3_lm_head: w is [vocab, {h}] and logits rows of vocab consecutive elements, got {tuple(w.shape)} and "
+                         f"{tuple(logits.shape)}")
     _check(lib().a3_lm_head(layout.ref, _ptr(hidden), _ptr(row_idx), int(n_rows), _ptr(w), int(w.shape[0]), logits.data_ptr(),
                             logits.stride(0) if logits.shape[0] > 1 else w.shape[0], _stream(stream)), "a3_lm_head")
 
@@ -646,9 +651,9 @@ def a3_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], out:
         raise ValueError("a3_token_logprobs: logits are float32 or bfloat16 rows of consecutive elements")
     if (tokens is None) != (out.n_given == 0):
         raise ValueError(f"a3_token_logprobs: tokens are int32 [{n_rows}, {out.n_given}], None for 0 given")
-    where = logits.device
-    _rows(where, n_rows, torch.int32, out.n_given, tokens=tokens)
-    _rows(where, n_rows, torch.float32, 1, entropy=out.entropy)
+    dev = _current(logits.device)
+    _hold(dev, torch.int32, n_rows * out.n_given, tokens)
+    _hold(dev, torch.float32, n_rows, out.entropy)
     _check(lib().a3_token_logprobs(A3_F32 if logits.dtype == torch.float32 else A3_BF16, logits.data_ptr(), n_rows, vocab,
                                    logits.stride(0) if n_rows > 1 else vocab, _ptr(tokens), out.n_given, out.n_top,
                                    _ptr(out.logprob), _ptr(out.entropy), _ptr(out.top_idx), _ptr(out.top_logprob), _ptr(out.ws),

@@ -207,6 +207,7 @@ struct attend_form {
   static constexpr int kVWords = E * kRow / D / 4;             // 32-bit words of one of them
   static constexpr int kQParts = Q8 && sizeof(T) == 4 ? 3 : 1, kPParts = sizeof(T) == 4 ? 3 : 2;
   static constexpr int kStep = 4 * SK;
+  static constexpr int kAhead = 1;                             // slabs on their way (8-bit pages with two: no faster)
 };
 // slots of a step by a3_pages (host and device agree through this)
 constexpr int step_shift(int dtype, int format) { return dtype == A3_F32 && format == A3_PAGES_PLAIN ? 6 : 7; }
@@ -472,27 +473,20 @@ paged_attention_kernel(attend_args a) {
           pf[k][i] = __builtin_bit_cast(bf16_t, (unsigned short)(h >> 16));
           w[i] -= __uint_as_float(h);
         }
-      bf16x8 vf[D / 16];
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
-        if constexpr (Q8) {
-          uint32_t x[4];
+        uint32_t x[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (Q8)
             x[i] = pack_codes((float)(signed char)(s.v[2 * i][0][c >> 2] >> 8 * (c & 3)), (float)(signed char)(s.v[2 * i + 1][0][c >> 2] >> 8 * (c & 3)));
-          vf[c] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
-        } else {
-          uint32_t x[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
+          else
             x[i] = __builtin_amdgcn_perm(s.v[2 * i + 1][0][c >> 1], s.v[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
-          vf[c] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
         }
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+        for (int k = 0; k < F::kPParts; ++k) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k], o[c], 0, 0, 0);
       }
-#pragma unroll
-      for (int k = 0; k < F::kPParts; ++k)
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], pf[k], o[c], 0, 0, 0);
     }
   };
 
@@ -549,49 +543,58 @@ paged_attention_kernel(attend_args a) {
     A3_LDS_BARRIER();
   };
 
-  // ---- the run of steps: the next slab is on its way while one is worked on ------------------------------------------
-  slab sa, sb;
+  // ---- the run of steps: the next slabs are on their way while one is worked on ---------------------------------------
+  slab ring[F::kAhead + 1];
+  place ahead = now;
   bool begins = now.step == 0;
-  load(sa, now);
+#pragma unroll
+  for (int k = 0; k < F::kAhead; ++k)
+    if (k < n_steps) {
+      if (k > 0) advance(ahead);
+      load(ring[k], ahead);
+    }
   load_queries(now);
   clear();
-  place next = now;
   int cut_item = -1, cut_pieces = 0;
-  auto step = [&](int i, slab &cur, slab &nxt) {
-    next = now;
-    const bool more = i + 1 < n_steps;
-    if (more) {
-      advance(next);
-      load(nxt, next);
+  auto step = [&](int i, slab &cur, slab &new_one) {
+    if (i + F::kAhead < n_steps) {
+      advance(ahead);
+      load(new_one, ahead);
     }
     __builtin_amdgcn_sched_barrier(0);
     compute(cur);
-    const bool ends = now.step == now.steps - 1;
-    if (ends || !more) {
-      if (more) load_queries(next);                            // on their way while the item is put together
-      finish(now, begins, ends);
-      if (begins) {
-        const int item = now.row * Hkv + now.head;
-        int pieces = 1;
-        if (!ends) {                                           // goes on in the workgroups behind: how many of them
-          // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
-          const int last = first + i + now.steps - 1 - now.step, fat = rest * (each + 1);
-          pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
-          cut_item = item;
-          cut_pieces = pieces;
-        }
-        if (a.by_item && tid == 0) a.cut[item] = make_int2(w, pieces);
-      }
-      if (more) {
-        begins = true;
-        clear();
-      }
+    const bool ends = now.step == now.steps - 1, more = i + 1 < n_steps;
+    if (!ends && more) {
+      ++now.step;
+      return;
     }
+    place next = now;
+    if (more) {
+      advance(next);
+      load_queries(next);                                      // on their way while the item is put together
+    }
+    finish(now, begins, ends);
+    if (begins) {
+      const int item = now.row * Hkv + now.head;
+      int pieces = 1;
+      if (!ends) {                                             // goes on in the workgroups behind: how many of them
+        // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+        const int last = first + i + now.steps - 1 - now.step, fat = rest * (each + 1);
+        pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+        cut_item = item;
+        cut_pieces = pieces;
+      }
+      if (a.by_item && tid == 0) a.cut[item] = make_int2(w, pieces);
+    }
+    begins = true;
+    clear();
     now = next;
   };
-  for (int i = 0; i < n_steps; i += 2) {
-    step(i, sa, sb);
-    if (i + 1 < n_steps) step(i + 1, sb, sa);
+  constexpr int R = F::kAhead + 1;
+  for (int i = 0; i < n_steps; i += R) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (i + k < n_steps) step(i + k, ring[k], ring[(k + F::kAhead) % R]);
   }
   if (tid == 0 && !a.by_item) a.cut[w] = make_int2(cut_item, cut_pieces);
 }
