@@ -227,7 +227,8 @@ struct gemm_mul_f32 {                                                   // a pie
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[e], xf[e], acc, 0, 0, 0);
   }
 };
-template <int IB, int JB, int ST, class MUL = gemm_mul_bf16>
+// NTW: the weights are read by one workgroup only and go past the caches.
+template <int IB, int JB, int ST, class MUL = gemm_mul_bf16, bool NTW = false>
 struct gemm_pl {
   static constexpr int kIB = IB, kJB = JB, kElems = MUL::kElems;
   static constexpr int BM = 32 * IB, BN = 64 * JB, L = 2 * IB;
@@ -260,8 +261,12 @@ struct gemm_pl {
 #define A3_PL_LOAD(J, STAGE, SLAB)                                                                                      \
   {                                                                                                                     \
     const char *gb_ = base[J] + (size_t)min((SLAB), n_slabs - 1) * 128;      /* past the end: the last slab, unused */    \
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"                                         \
-                 :: "s"(lds_base + (uint32_t)(STAGE) + (8 * (J) + wave) * 1024), "v"(src[J]), "s"(gb_) : "memory");      \
+    if (NTW && (J) < kLW)                                                                                               \
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"                                    \
+                   :: "s"(lds_base + (uint32_t)(STAGE) + (8 * (J) + wave) * 1024), "v"(src[J]), "s"(gb_) : "memory");    \
+    else                                                                                                                \
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"                                       \
+                   :: "s"(lds_base + (uint32_t)(STAGE) + (8 * (J) + wave) * 1024), "v"(src[J]), "s"(gb_) : "memory");    \
   }
 #define A3_PL_FENCE __builtin_amdgcn_sched_barrier(0);
     const int swz = (l16 >> 1) & 7;

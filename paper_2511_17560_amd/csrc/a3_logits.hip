@@ -493,7 +493,18 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
   };
   if (bf16) {
     const int knob = gemm_tile_of_knob(a3_knob(A3_KNOB_GEMM_TB));
-    return gemm_with_tile(knob >= 0 ? knob : gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile, [&](auto t) { return launch(bf16_t{}, t); });
+    const int tile = knob >= 0 ? knob : gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile;
+    // One tile of rows, and more weights than the 256 MB of the memory-side cache: nothing of them is read again before it is gone,
+    // so they go past the caches (1 row of 128256 x 4096, 1.05 GB: 175 -> 162 us; of 32003 x 4096, 262 MB: 58 -> 54.  Of 8000 x 4096,
+    // 66 MB and called again and again: 20 -> 25).
+    if (n_rows <= (tile == GEMM_128x64 ? 64 : 128) && (long long)vocab * L->hidden * 2 > (256LL << 20)) {
+      switch (tile) {
+        case GEMM_256x128: return launch(bf16_t{}, gemm_pl<8, 2, 3, gemm_mul_bf16, true>{});
+        case GEMM_128x128: return launch(bf16_t{}, gemm_pl<4, 2, 5, gemm_mul_bf16, true>{});
+        case GEMM_128x64: return launch(bf16_t{}, gemm_pl<4, 1, 6, gemm_mul_bf16, true>{});
+      }
+    }
+    return gemm_with_tile(tile, [&](auto t) { return launch(bf16_t{}, t); });
   }
   // fp32: bound by the matrix pipe (138 TFLOP/s at 512 rows of 32000 x 4096).  128 rows a tile, which fetch less, or 64 where those would
   // leave compute units without a tile (65 rows of 4099 x 512, 33 tiles of 128 rows: 34 us and 21; 512 rows, 132 tiles: 38 and 42).

@@ -317,11 +317,12 @@ paged_attention_kernel(attend_args a) {
     if (page < 0 || page >= a.p.n_pages) { s.n = 0; return; }
     const size_t block = ((size_t)page * Hkv + p.head) * head_bytes;
     const int at = slot & ((1 << a.p.page_shift) - 1);
+    // every byte is read once: nontemporal (8 requests of 64K tokens 362 -> 326 us, 48 of 4000 79 -> 71)
     const char *kb = a.p.k_pool + block + at * F::kRow, *vb = a.p.v_pool + block + at * F::kRow;
 #pragma unroll
     for (int b = 0; b < F::KB; ++b)
 #pragma unroll
-      for (int i = 0; i < F::NK; ++i) s.k[b][i] = *reinterpret_cast<const uint4 *>(kb + koff[b] + 64 * i);
+      for (int i = 0; i < F::NK; ++i) s.k[b][i] = a3_nt_load(kb + koff[b] + 64 * i);
     if constexpr (Q8) {
       const char *sc = a.p.k_pool + block + ((size_t)D << a.p.page_shift) + 4 * at + 32 * lg;
       s.ks[0] = *reinterpret_cast<const f32x4 *>(sc);
@@ -335,7 +336,7 @@ paged_attention_kernel(attend_args a) {
 #pragma unroll
       for (int j = 0; j < F::NP; ++j) {
         typedef uint32_t words __attribute__((ext_vector_type(F::kVWords == 1 ? 1 : F::kVWords)));
-        const words w = *reinterpret_cast<const words *>(vb + voff + i * F::kRow + j * 64 * F::kVWords);
+        const words w = __builtin_nontemporal_load(reinterpret_cast<const words *>(vb + voff + i * F::kRow + j * 64 * F::kVWords));
 #pragma unroll
         for (int u = 0; u < F::kVWords; ++u) s.v[i][j][u] = w[u];
       }
