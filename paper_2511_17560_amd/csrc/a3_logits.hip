@@ -66,8 +66,8 @@ logits_kernel(logits_args a) {
 // A workgroup reads a row, or with few rows a slice of one, in chunks of 32 values a thread.  Sums: every thread keeps the maximum m of
 // its own values, z = sum e^(x - m) and t = sum e^(x - m) (x - m) in units of log 2 and rescales them when a chunk brings a larger value
 // (t' = f (t + (m - m') z), f = 2^(m - m')).  Alternatives: while it reads, a thread only notes the maximum of each of its chunks.
-// Then the n-th largest of a wave's 64 lane maxima is found bit by bit with ballots: at least n values of the row are no smaller, so
-// what lies below the largest of the four waves' bounds is out.  The noted chunks that reach it (some n of them) are looked at again,
+// Then the n-th largest of a wave's 128 - every lane's two largest maxima of half chunks - is found bit by bit with ballots: at least
+// n values of the row are no smaller, so what lies below the largest of the four waves' bounds is out.  The noted chunks that reach it (some n of them) are looked at again,
 // each by half a wave, and the values found are ranked.  Where too many equal the bound (rows that are masked or constant), only the
 // larger ones are gathered, and of the equal ones the first n in the row's order.  Slices of a row are put together by a second kernel.
 struct logprob_args {
@@ -82,7 +82,7 @@ struct logprob_args {
   unsigned long long *part_top;      // [n_rows, slices, n_top]
 };
 
-constexpr int kLpThreads = 256, kLpValues = 32, kLpTop = 64, kLpCands = 1024;
+constexpr int kLpThreads = 256, kLpValues = 32, kLpTop = 64, kLpCands = 576;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
 // Order of the alternatives as one number: larger logit, then lower index; -0 equals 0, NaN below everything (0: no value).
@@ -143,14 +143,14 @@ __device__ __forceinline__ void lp_join_workgroup(lp_shared &s, float &m, float 
   }
 }
 
-// The n-th largest of a wave's 64 numbers of so many bits (0: fewer than n are not 0).
+// The n-th largest of a wave's 128 numbers of so many bits (0: fewer than n are not 0).
 template <int BITS>
-__device__ __forceinline__ uint32_t wave_nth(uint32_t x, int n) {
+__device__ __forceinline__ uint32_t wave_nth(uint32_t x, uint32_t y, int n) {
   uint32_t b = 0;
 #pragma unroll 4
   for (int i = BITS - 1; i >= 0; --i) {
     const uint32_t t = b | 1u << i;
-    if (__popcll(__ballot(x >= t)) >= n) b = t;
+    if (__popcll(__ballot(x >= t)) + __popcll(__ballot(y >= t)) >= n) b = t;
   }
   return b;
 }
@@ -225,14 +225,14 @@ struct lp_row {
   }
 };
 
-// The n best of the list so far and of chunks g0 .. (vectors) up to g1, whose maxima are noted.  most: the order of the thread's largest
-// value, 0 if it may have none but NaN.
+// The n best of the list so far and of chunks g0 .. (vectors) up to g1, whose maxima are noted.  most, second: the order of the largest
+// values of two halves of chunks of the thread's, 0 if there may be none but NaN.
 template <typename T>
-__device__ void lp_choose(lp_shared &s, const lp_row<T> &r, const float (*noted)[kLpThreads], int n, int g0, int g1, uint32_t most) {
+__device__ void lp_choose(lp_shared &s, const lp_row<T> &r, const float (*noted)[kLpThreads], int n, int g0, int g1, uint32_t most, uint32_t second) {
   constexpr int V = lp_row<T>::V, kChunk = lp_row<T>::kChunk;
   const int tid = threadIdx.x, chunks = (g1 - g0 + kChunk - 1) / kChunk;
   constexpr int kBits = 8 * sizeof(T);                         // of a value's order: bf16 values differ in the upper 16
-  const uint32_t mine = wave_nth<kBits>(most >> (32 - kBits), n);
+  const uint32_t mine = wave_nth<kBits>(most >> (32 - kBits), second >> (32 - kBits), n);
   if ((tid & 63) == 0) s.bound[tid >> 6] = mine;
   for (int pass = 0;; ++pass) {                                // 0: what reaches the bound; 1: what exceeds it, and the first equal ones
     if (tid == 0) { s.count = n; s.queued = 0; s.total = 0; }
@@ -349,6 +349,12 @@ logprobs_kernel(logprob_args a) {
   r.v1 = (int)((long long)n_vec * (slice + 1) / a.slices);
   typename R::vec_t raw[U];
   auto load = [&](int c) {
+    if (c * V >= r.skew && c + kChunk <= r.v1 && (long long)(c + kChunk) * V - r.skew <= r.vocab) {
+      const T *x = r.x + ((long long)c * V - r.skew);
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const typename R::vec_t *>(x + (u * kLpThreads + tid) * V);
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) raw[u] = r.vec(c + u * kLpThreads + tid);
   };
@@ -358,15 +364,17 @@ logprobs_kernel(logprob_args a) {
   float m = -INFINITY, z = 0.f, t = 0.f;
   for (int g0 = r.v0; g0 < r.v1; g0 += kLpChunks * kChunk) {   // chunks between two choices of alternatives
     const int g1 = min(r.v1, g0 + kLpChunks * kChunk);
-    float most = -INFINITY;
+    float most = -INFINITY, second = -INFINITY;
     for (int c = g0; c < g1; c += kChunk) {
       float y[kLpValues];
 #pragma unroll
       for (int i = 0; i < kLpValues; ++i) y[i] = (float)raw[i / V][i % V];
       if (c + kChunk < r.v1) load(c + kChunk);                 // on its way while this chunk is worked on
-      float top = y[0];
+      float top = y[0], half = y[kLpValues / 2];
 #pragma unroll
-      for (int i = 1; i < kLpValues; ++i) top = fmaxf(top, y[i]);
+      for (int i = 1; i < kLpValues / 2; ++i) { top = fmaxf(top, y[i]); half = fmaxf(half, y[kLpValues / 2 + i]); }
+      second = fmaxf(second, fmaxf(fminf(top, half), fminf(most, fmaxf(top, half))));
+      top = fmaxf(top, half);
       noted[(c - g0) / kChunk][tid] = top;
       most = fmaxf(most, top);
       if (top > m) {
@@ -385,7 +393,9 @@ logprobs_kernel(logprob_args a) {
     }
     if (a.n_top == 0) continue;
     __syncthreads();                                           // (the list: cleared, or of the last choice)
-    lp_choose(s, r, noted, a.n_top, g0, g1, g0 + tid >= g1 || (most == -INFINITY && z != z) ? 0u : top_order(most));
+    // (-inf may stand for no value at all: for the largest there is one unless the slice ends before it or NaN has been seen)
+    lp_choose(s, r, noted, a.n_top, g0, g1, g0 + tid >= g1 || (most == -INFINITY && z != z) ? 0u : top_order(most),
+              second == -INFINITY ? 0u : top_order(second));
   }
   lp_join_workgroup(s, m, z, t);
   if (a.slices == 1) {
@@ -417,7 +427,7 @@ logprobs_join_kernel(logprob_args a) {
   if (n) {
 #pragma unroll
     for (int i = 0; i < N; ++i) top = k[i] > top ? k[i] : top;
-    const uint32_t mine = wave_nth<32>((uint32_t)(top >> 32), n);
+    const uint32_t mine = wave_nth<32>((uint32_t)(top >> 32), 0u, n);
     if ((tid & 63) == 0) s.bound[tid >> 6] = mine;
     if (tid < n) s.list[tid] = 0;
     if (tid == 0) s.count = 0;
