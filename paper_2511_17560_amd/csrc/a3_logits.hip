@@ -143,14 +143,17 @@ __device__ __forceinline__ void lp_join_workgroup(lp_shared &s, float &m, float 
   }
 }
 
-// The n-th largest of a wave's 128 numbers of so many bits (0: fewer than n are not 0).
-template <int BITS>
-__device__ __forceinline__ uint32_t wave_nth(uint32_t x, uint32_t y, int n) {
+// The n-th largest of a wave's numbers, J of so many bits a lane (0: fewer than n are not 0).
+template <int BITS, int J>
+__device__ __forceinline__ uint32_t wave_nth(const uint32_t (&x)[J], int n) {
   uint32_t b = 0;
 #pragma unroll 4
   for (int i = BITS - 1; i >= 0; --i) {
     const uint32_t t = b | 1u << i;
-    if (__popcll(__ballot(x >= t)) + __popcll(__ballot(y >= t)) >= n) b = t;
+    int count = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) count += __popcll(__ballot(x[j] >= t));
+    if (count >= n) b = t;
   }
   return b;
 }
@@ -232,7 +235,7 @@ __device__ void lp_choose(lp_shared &s, const lp_row<T> &r, const float (*noted)
   constexpr int V = lp_row<T>::V, kChunk = lp_row<T>::kChunk;
   const int tid = threadIdx.x, chunks = (g1 - g0 + kChunk - 1) / kChunk;
   constexpr int kBits = 8 * sizeof(T);                         // of a value's order: bf16 values differ in the upper 16
-  const uint32_t mine = wave_nth<kBits>(most >> (32 - kBits), second >> (32 - kBits), n);
+  const uint32_t mine = wave_nth<kBits, 2>({most >> (32 - kBits), second >> (32 - kBits)}, n);
   if ((tid & 63) == 0) s.bound[tid >> 6] = mine;
   for (int pass = 0;; ++pass) {                                // 0: what reaches the bound; 1: what exceeds it, and the first equal ones
     if (tid == 0) { s.count = n; s.queued = 0; s.total = 0; }
@@ -345,8 +348,9 @@ logprobs_kernel(logprob_args a) {
   r.vocab = a.vocab;
   r.skew = (int)(((uintptr_t)r.x & 15) / sizeof(T));
   const int n_vec = (int)(((long long)a.vocab + r.skew + V - 1) / V);
-  r.v0 = (int)((long long)n_vec * slice / a.slices);
-  r.v1 = (int)((long long)n_vec * (slice + 1) / a.slices);
+  const int per = n_vec / a.slices, rest = n_vec - per * a.slices;
+  r.v0 = slice * per + min(slice, rest);
+  r.v1 = r.v0 + per + (slice < rest ? 1 : 0);
   typename R::vec_t raw[U];
   auto load = [&](int c) {
     if (c * V >= r.skew && c + kChunk <= r.v1 && (long long)(c + kChunk) * V - r.skew <= r.vocab) {
@@ -370,9 +374,9 @@ logprobs_kernel(logprob_args a) {
 #pragma unroll
       for (int i = 0; i < kLpValues; ++i) y[i] = (float)raw[i / V][i % V];
       if (c + kChunk < r.v1) load(c + kChunk);                 // on its way while this chunk is worked on
-      float top = y[0], half = y[kLpValues / 2];
+      float top = y[0], half = y[1];                           // every other value: a short slice fills both halves too
 #pragma unroll
-      for (int i = 1; i < kLpValues / 2; ++i) { top = fmaxf(top, y[i]); half = fmaxf(half, y[kLpValues / 2 + i]); }
+      for (int i = 2; i < kLpValues; i += 2) { top = fmaxf(top, y[i]); half = fmaxf(half, y[i + 1]); }
       second = fmaxf(second, fmaxf(fminf(top, half), fminf(most, fmaxf(top, half))));
       top = fmaxf(top, half);
       noted[(c - g0) / kChunk][tid] = top;
@@ -419,20 +423,22 @@ logprobs_join_kernel(logprob_args a) {
   }
   const unsigned long long *keys = a.part_top + (size_t)row * a.slices * n;
   constexpr int N = 16;                                        // kLpSlices * kLpTop / kLpThreads
-  unsigned long long k[N], top = 0;
+  unsigned long long k[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) k[i] = i * kLpThreads + tid < a.slices * n ? keys[i * kLpThreads + tid] : 0ull;
+  // every wave: the first of all slices' lists, two of each or, where that are fewer than n, eight; their n-th largest is the bound
+  constexpr int J = 8;
+  const int lane = tid & 63, deep = min(n, 2 * a.slices >= n ? 2 : J);
+  uint32_t head[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) head[j] = lane < a.slices && j < deep ? (uint32_t)(keys[lane * n + j] >> 32) : 0u;
   const float given = lp_given(a, row, tid, x);
   lp_join_workgroup(s, m, z, t);
   if (n) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = k[i] > top ? k[i] : top;
-    const uint32_t mine = wave_nth<32>((uint32_t)(top >> 32), 0u, n);
-    if ((tid & 63) == 0) s.bound[tid >> 6] = mine;
+    const uint32_t bound = deep <= 2 ? wave_nth<32, 2>({head[0], head[1]}, n) : wave_nth<32, J>(head, n);
     if (tid < n) s.list[tid] = 0;
     if (tid == 0) s.count = 0;
     __syncthreads();
-    const uint32_t bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3]));
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if ((uint32_t)(k[i] >> 32) >= bound) lp_push(s, k[i], 0ull);
