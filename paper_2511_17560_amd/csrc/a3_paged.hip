@@ -116,12 +116,8 @@ paged_append_kernel(append_args a) {
     scale = q8_scale(amax);
     if (!on) return;
     i8x16 code;
-    if (rotate) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) code[e] = (signed char)(int)q8_code(y[e], scale);
-    } else {
-      code = q8_codes(x, scale);
-    }
+    if (rotate) code = q8_codes(y, scale);
+    else code = q8_codes(x, scale);
     signed char *dst = base + (size_t)at * D;
     *reinterpret_cast<i8x8 *>(dst + e0) = __builtin_shufflevector(code, code, 0, 1, 2, 3, 4, 5, 6, 7);
     *reinterpret_cast<i8x8 *>(dst + e1) = __builtin_shufflevector(code, code, 8, 9, 10, 11, 12, 13, 14, 15);
@@ -212,11 +208,19 @@ struct attend_form {
 // slots of a step by a3_pages (host and device agree through this)
 constexpr int step_shift(int dtype, int format) { return dtype == A3_F32 && format == A3_PAGES_PLAIN ? 6 : 7; }
 
-__device__ __forceinline__ int steps_of(const attend_args &a, int row, int shift) {
-  const int req = a.row_req ? a.row_req[row] : row;
+__device__ __forceinline__ int steps_of(const attend_args &a, int req, int len, int shift) {
   if (req < 0 || req >= a.p.n_req) return 0;
-  const int len = min(a.row_len[row], a.p.slots);
+  len = min(len, a.p.slots);
   return len <= 0 ? 1 : ((len - 1) >> shift) + 1;                // (a row that sees nothing has its zeros written)
+}
+__device__ __forceinline__ int steps_of(const attend_args &a, int row, int shift) {
+  return steps_of(a, a.row_req ? a.row_req[row] : row, a.row_len[row], shift);
+}
+
+// One number at a wave-uniform place of an array that no kernel in flight writes, by a scalar load: a vector load would be waited for
+// together with all the slabs requested before it (they come back in order).
+__device__ __forceinline__ int scalar_at(const int *p, size_t i) {
+  return reinterpret_cast<const __attribute__((address_space(4))) int *>(reinterpret_cast<uintptr_t>(p))[i];
 }
 
 template <typename T, int D, bool Q8>
@@ -282,9 +286,10 @@ paged_attention_kernel(attend_args a) {
   now.head = inside / now.steps;
   now.step = inside - now.head * now.steps;
   auto enter = [&](place &p) {                                 // another row's own numbers
-    p.req = __builtin_amdgcn_readfirstlane(a.row_req ? a.row_req[p.row] : p.row);
-    p.len = __builtin_amdgcn_readfirstlane(max(0, min(a.row_len[p.row], a.p.slots)));
-    p.steps = __builtin_amdgcn_readfirstlane(steps_of(a, p.row, kShift));
+    const int len = scalar_at(a.row_len, p.row);
+    p.req = a.row_req ? scalar_at(a.row_req, p.row) : p.row;
+    p.len = max(0, min(len, a.p.slots));
+    p.steps = steps_of(a, p.req, len, kShift);
   };
   auto advance = [&](place &p) {
     if (++p.step < p.steps) return;
@@ -313,7 +318,7 @@ paged_attention_kernel(attend_args a) {
     const int slot = (p.step << kShift) + SK * wave;
     s.n = p.len - slot;
     if (s.n <= 0) { s.n = 0; return; }
-    const int page = __builtin_amdgcn_readfirstlane(a.p.table[(size_t)p.req * a.p.max_pages + (slot >> a.p.page_shift)]);
+    const int page = scalar_at(a.p.table, (size_t)p.req * a.p.max_pages + (slot >> a.p.page_shift));
     if (page < 0 || page >= a.p.n_pages) { s.n = 0; return; }
     const size_t block = ((size_t)page * Hkv + p.head) * head_bytes;
     const int at = slot & ((1 << a.p.page_shift) - 1);

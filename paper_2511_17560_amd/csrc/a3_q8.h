@@ -16,6 +16,27 @@ __device__ __forceinline__ float q8_code(double v, float s) {
   return (float)fmin(fmax(r, -127.0), 127.0);
 }
 
+// Codes of 16 doubles.  x * (1 / scale) is within 2^-51 of the quotient, so a division decides only where one comes that close to a
+// half (or the scale is 0): one check for all, so that its code is not even fetched otherwise.
+__device__ __forceinline__ i8x16 q8_codes(const double (&v)[16], float s) {
+  const double inv = 1.0 / (double)s;
+  double n[16];
+  bool near = !(s > 0.f);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const double q = v[e] * inv;
+    n[e] = rint(q);
+    near |= fabs(fabs(q - n[e]) - 0.5) < 1e-9;
+  }
+  i8x16 code;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) code[e] = (signed char)(int)fmin(fmax(n[e], -127.0), 127.0);
+  if (__builtin_expect(near, 0))
+#pragma unroll
+    for (int e = 0; e < 16; ++e) code[e] = (signed char)(int)q8_code(v[e], s);
+  return code;
+}
+
 // Codes of 16 floats, the division spared nearly always: n = x * (1 / scale) rounded is at most a step off, and x - n * scale
 // formed in one rounding says whether n is the nearest whole number (rounding is monotone and scale / 2 is a float, so a
 // rounded remainder below scale / 2 is a true one below it).  Only a remainder that is not below (a tie, a quotient within
