@@ -507,8 +507,12 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
     A3_CHECK_LAUNCH("a3_lm_head");
     return A3_OK;
   };
+  // Tiles of 64 x 64 where they all run at once: the more compute units, the better (64 rows, weights from HBM: 11699 x 3584, 183 tiles,
+  // 23 us, 128 x 64 32; 18702 x 4096, 293 tiles, 49 and 42.  fp32: 4099 x 512 13 and 20; 152064 x 512 127 and 110).
+  const bool small = (long long)((vocab + 63) / 64) * ((n_rows + 63) / 64) <= 256;
   if (bf16) {
     const int knob = gemm_tile_of_knob(a3_knob(A3_KNOB_GEMM_TB));
+    if (knob < 0 && small) return launch(bf16_t{}, gemm_pl<2, 1, 8>{});
     const int tile = knob >= 0 ? knob : gemm_choose_tile(vocab, n_rows, L->hidden / 64, 1).tile;
     // One tile of rows, and more weights than the 256 MB of the memory-side cache: nothing of them is read again before it is gone,
     // so they go past the caches (1 row of 128256 x 4096, 1.05 GB: 175 -> 162 us; of 32003 x 4096, 262 MB: 58 -> 54.  Of 8000 x 4096,
@@ -525,6 +529,7 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
   // fp32: bound by the matrix pipe (138 TFLOP/s at 512 rows of 32000 x 4096).  128 rows a tile, which fetch less, or 64 where those would
   // leave compute units without a tile (65 rows of 4099 x 512, 33 tiles of 128 rows: 34 us and 21; 512 rows, 132 tiles: 38 and 42).
   const long long tiles = (long long)((vocab + 127) / 128) * ((n_rows + 127) / 128);
+  if (small) return launch(0.f, gemm_pl<2, 1, 8, gemm_mul_f32>{});
   return n_rows <= 64 || tiles < 128 ? launch(0.f, gemm_pl<4, 1, 6, gemm_mul_f32>{}) : launch(0.f, gemm_pl<4, 2, 5, gemm_mul_f32>{});
 }
 
