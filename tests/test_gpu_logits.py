@@ -44,6 +44,39 @@ def test_lm_head(dtype, h, vocab, n):
     assert bool((wide[:, vocab:] == 7.0).all())
 
 
+@pytest.mark.parametrize("n,vocab,tb", [(3, 700, tb) for tb in (2, 3, 4, 5, 6, 7)] + [(300, 900, tb) for tb in (2, 3, 4, 5, 6, 7)] +
+                         [(33, 20001, -1), (70, 20001, -1), (150, 9000, -1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lm_head_other_tiles(dtype, n, vocab, tb, tuning):
+    """Every tile the product can run in, and shapes that the rule gives the larger ones."""
+    if tb >= 0:
+        tuning("gemm_tb", tb)
+    h = 192
+    rng = np.random.default_rng(vocab + n)
+    lay, x, w = _layout(dtype, h, n), _values(rng, dtype, n, h), _values(rng, dtype, vocab, h)
+    idx = rng.permutation(n)
+    logits = torch.empty((n, vocab), device="cuda")
+    _call_lm_head(lay, to_dev(x, dtype), idx, n, to_dev(w, dtype), logits)
+    torch.cuda.synchronize()
+    assert np.all(np.abs(to_host(logits) - x[idx] @ w.T) <= 8 * np.sqrt(h) * 2.0 ** -24 * (np.abs(x[idx]) @ np.abs(w).T))
+
+
+@pytest.mark.parametrize("n,vocab,h", [(5, 32003, 4224), (40, 140001, 1024), (100, 70001, 2048), (128, 131072, 1088)])
+def test_lm_head_weights_beyond_the_caches(n, vocab, h):
+    """More than 256 MB of weights: a sample of rows and features, the last of both among them."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(n, h, device="cuda", generator=g, dtype=torch.bfloat16)
+    w = torch.randn(vocab, h, device="cuda", generator=g, dtype=torch.bfloat16)
+    logits = torch.full((n, vocab), float("nan"), device="cuda")
+    api.a3_lm_head(_layout("bf16", h, n), x, None, n, w, logits)
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(logits).all())
+    feats = np.unique(np.concatenate([np.random.default_rng(n).integers(0, vocab, 4000), np.arange(vocab - 130, vocab), np.arange(130)]))
+    xh, wh = to_host(x), to_host(w[torch.from_numpy(feats).cuda()])
+    got = to_host(logits[:, torch.from_numpy(feats).cuda()])
+    assert np.all(np.abs(got - xh @ wh.T) <= 8 * np.sqrt(h) * 2.0 ** -24 * (np.abs(xh) @ np.abs(wh).T))
+
+
 def _call_lm_head(lay, x, row_idx, n, w, logits):
     api.a3_lm_head(lay, x, None if row_idx is None else idev(row_idx), n, w, logits)
 
