@@ -517,11 +517,12 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
     // One tile of rows, and weights that take more than half of the 256 MB of the memory-side cache, whose other half the rest of a step
     // turns over: nothing of them is read again before it is gone, so they go past the caches (1 row of 128256 x 4096, 1.05 GB: 175
     // -> 162 us; of 8000 x 4096, 66 MB and called again and again, 20 -> 25).  Up to 64 rows in tiles of which two fit a compute unit, one
-    // streaming while the other starts or ends: of 64 weight rows where those all run at once (32003 x 4096, 1 row 58 -> 47 us, 48 rows
-    // 60 -> 53), of 128 otherwise (65536 x 4096, 1 row 116 -> 96, 48 rows 121 -> 104; 152064 x 3584, 64 rows 223 -> 216; only 128256 x 4096
-    // at 64 rows, two full rounds of 256 x 128, is slower: 184 -> 196).
+    // streaming while the other starts or ends: of 64 weight rows where those all run at once and are not bound by the activation rows
+    // they read (32003 x 4096, 1 row 58 -> 47 us, 32 rows 60 -> 50), of 128 otherwise (65536 x 4096, 1 row 116 -> 96, 48 rows 121 ->
+    // 104; 152064 x 3584, 64 rows 223 -> 216; 18702 x 4096, 64 rows 42 -> 41 and 47 in tiles of 64; only 128256 x 4096 at 64 rows, two full
+    // rounds of 256 x 128, is slower: 184 -> 196).
     if (knob < 0 && n_rows <= 128 && (long long)vocab * L->hidden * 2 > (128LL << 20)) {
-      if (n_rows <= 64 && vocab <= 64 * 512) return launch(bf16_t{}, gemm_pl<2, 1, 5, gemm_mul_bf16, true>{});
+      if (n_rows <= 32 && vocab <= 64 * 512) return launch(bf16_t{}, gemm_pl<2, 1, 5, gemm_mul_bf16, true>{});
       if (n_rows <= 64) return launch(bf16_t{}, gemm_pl<4, 1, 3, gemm_mul_bf16, true>{});
       if (tile == GEMM_256x128) return launch(bf16_t{}, gemm_pl<8, 2, 3, gemm_mul_bf16, true>{});
       if (tile == GEMM_128x128) return launch(bf16_t{}, gemm_pl<4, 2, 5, gemm_mul_bf16, true>{});
