@@ -453,8 +453,8 @@ a3_status a3_paged_attention(const a3_pages *pages, const void *q, const int *ro
 a3_status a3_lm_head(const a3_layout *layout, const void *hidden, const int *row_idx, int n_rows, const void *w, int vocab,
                      float *logits, long long ld, void *stream);
 
-/* Log probabilities of rows of logits.  Row i is logits + i * ld (elements of `dtype`, an a3_dtype; ld >= vocab, any vocab and
- * ld; the base 16-byte aligned).  With m = max_v x_v and Z = sum_v e^(x_v - m):
+/* Log probabilities of rows of logits.  Row i is logits + i * ld (elements of `dtype`, an a3_dtype; ld >= vocab, vocab below 2^30, any
+ * ld, any start).  With m = max_v x_v and Z = sum_v e^(x_v - m):
  *   logprob[i, j]      x_t - m - log Z of t = tokens[i, j], j < n_given; -inf where t is outside [0, vocab)
  *   entropy[i]         log Z - sum_v e^(x_v - m) (x_v - m) / Z      (a logit of -inf adds nothing)
  *   top_idx[i, j]      the n_top largest logits, largest first, equal ones by the lower index (-0 equals 0; NaN comes last)

@@ -553,7 +553,7 @@ extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows
   if (n_rows == 0) return A3_OK;
   A3_REQUIRE(logits && (n_given == 0 || (tokens && logprob)) && (n_top == 0 || (top_idx && top_logprob)), A3_ERR_INVALID_ARG,
              "a3_token_logprobs: NULL tensor");
-  A3_REQUIRE(a3_aligned16(logits), A3_ERR_INVALID_ARG, "a3_token_logprobs: logits must be 16-byte aligned");
+  A3_REQUIRE(((uintptr_t)logits & (dtype == A3_BF16 ? 1 : 3)) == 0, A3_ERR_INVALID_ARG, "a3_token_logprobs: logits are not aligned to their type");
   const size_t need = a3_token_logprobs_ws_bytes(n_rows, vocab, n_top);
   A3_REQUIRE(ws && a3_aligned16(ws) && ws_bytes >= need, A3_ERR_WORKSPACE, "a3_token_logprobs: workspace %zu bytes (16-byte aligned), need %zu",
              ws ? ws_bytes : 0, need);

@@ -121,7 +121,7 @@ def test_logprobs_refuses():
     assert call(dtype=3) == bad and call(n=-1) == bad and call(V=0) == bad and call(ld=999) == bad
     assert call(given=-1) == bad and call(top=-1) == bad and call(V=10, ld=10, top=11) == bad and call(top=65) == api.A3_ERR_UNSUPPORTED
     assert call(x=None) == bad and call(tok=None) == bad and call(lp=None) == bad and call(idx=None) == bad and call(tl=None) == bad
-    assert call(x=X + 4) == bad
+    assert call(x=X + 2) == bad and call(dtype=api.A3_BF16, x=X + 1) == bad and call(V=1 << 30, ld=1 << 30) == api.A3_ERR_UNSUPPORTED
     assert call(ws=None) == api.A3_ERR_WORKSPACE and call(size=need - 1) == api.A3_ERR_WORKSPACE and call(ws=X + 8) == api.A3_ERR_WORKSPACE
 
 

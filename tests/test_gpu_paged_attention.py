@@ -235,3 +235,35 @@ def test_a_cache_beyond_32_bits():
     held = [put(p, 0, 0, k, v)]
     q = _values(rng, "bf16", 1, 16, 128)
     _check_rows(p, held, q, _attend(p, q, [2100]), [2100])
+
+
+def test_two_calls_at_once():
+    """Two streams over one cache, each with a workspace of its own."""
+    lens = [3000, 17, 900]
+    p, held, rng = _filled(lens)
+    q = [_values(rng, "bf16", 3, 8, 128) for _ in range(2)]
+    qd, n = [to_dev(x, "bf16") for x in q], idev(lens)
+    out, ws, streams = [torch.empty_like(x) for x in qd], [p.workspace(3) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            api.a3_paged_attention(p, qd[i], None, n, 3, out[i], ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        _check_rows(p, held, q[i], to_host(out[i]), lens)
+
+
+@pytest.mark.parametrize("n_rows,Hq,Hkv", [(64, 8, 1), (65, 8, 8), (300, 32, 2), (520, 16, 16)])
+def test_many_items_of_a_few_steps(n_rows, Hq, Hkv):
+    """Shares that hold several items, whole and cut, on both sides of the number of shares; requests that do not exist between them."""
+    rng = np.random.default_rng(n_rows)
+    lens = [0, 200, 385, 1, 513]
+    p, held, _ = _filled(lens, Hq=Hq, Hkv=Hkv, d=64)
+    req = rng.integers(0, 5, n_rows)
+    n = np.array([rng.integers(0, lens[r] + 1) for r in req])
+    q = _values(rng, "bf16", n_rows, Hq, 64)
+    named = np.where(rng.random(n_rows) < 0.2, 7, req)
+    got = _attend(p, q, n, req=named)
+    off = named == 7
+    assert np.all(got[off] == 9.0)
+    _check_rows(p, held, q[~off], got[~off], n[~off].tolist(), req=req[~off].tolist())
