@@ -254,13 +254,21 @@ __device__ void lp_choose(lp_shared &s, const lp_row<T> &r, const float (*noted)
     __syncthreads();
     const int queued = s.queued;
     if (queued <= kLpQueue) {
-#pragma unroll 4
-      for (int q = tid >> 5; q < queued; q += kLpThreads / 32) {
-        const int id = s.queue[q], i = tid & 31;
-        const int v = g0 + id / kLpThreads * kChunk + i / V * kLpThreads + id % kLpThreads, e = v * V - r.skew + i % V;
-        if (v < r.v1 && (unsigned)e < (unsigned)r.vocab) {
-          const unsigned long long k = top_key((float)r.x[e], e);
-          if ((uint32_t)(k >> (64 - kBits)) >= bound) lp_push(s, k, last);
+      constexpr int Q = 4, kHalves = kLpThreads / 32;          // half a wave a chunk, the loads of four on their way together
+      for (int q0 = tid >> 5; q0 < queued; q0 += Q * kHalves) {
+        T y[Q];
+        int e[Q];
+#pragma unroll
+        for (int k = 0; k < Q; ++k) {
+          const int id = s.queue[min(q0 + k * kHalves, queued - 1)], i = tid & 31;
+          const int v = g0 + id / kLpThreads * kChunk + i / V * kLpThreads + id % kLpThreads, at = v * V - r.skew + i % V;
+          e[k] = q0 + k * kHalves < queued && v < r.v1 && (unsigned)at < (unsigned)r.vocab ? at : -1;
+          y[k] = r.x[max(e[k], 0)];
+        }
+#pragma unroll
+        for (int k = 0; k < Q; ++k) {
+          const unsigned long long key = top_key((float)y[k], e[k]);
+          if (e[k] >= 0 && (uint32_t)(key >> (64 - kBits)) >= bound) lp_push(s, key, last);
         }
       }
     }
