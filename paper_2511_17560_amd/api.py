@@ -218,6 +218,7 @@ class Layout:
         max_ctx = int(np.max(ctx_len)) if n_req else 0
         max_q = int(np.max(q_len)) if n_req else 0
         self.total_tokens, self.n_req, self.n_chunks = T, n_req, n_chunks
+        self.max_len = int(np.max(ctx_h + q_h)) if n_req else 0     # of one request: context and question
         self.tok_pos = torch.empty(max(T, 1), dtype=torch.int32, device=dev)
         self.tok_req = torch.empty(max(T, 1), dtype=torch.int32, device=dev)
         self.tok_chunk = torch.empty(max(T, 1), dtype=torch.int32, device=dev)

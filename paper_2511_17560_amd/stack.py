@@ -22,6 +22,17 @@ def _bias(lw):
     return dict(bq=lw.get("bq"), bk=lw.get("bk"), bv=lw.get("bv"))
 
 
+def _fit(pages, n_layers: int, n_req: int, tokens: int) -> None:
+    """Refuses pages that cannot take what a call writes (a slot outside the page table would be skipped)."""
+    if len(pages) < n_layers:
+        raise ValueError(f"pages of {n_layers} layers are needed, got {len(pages)}")
+    for p in pages[:n_layers]:
+        s = p.struct
+        if s.n_req < n_req or s.max_pages * s.page_size < tokens:
+            raise ValueError(f"pages: {n_req} requests of up to {tokens} tokens are needed, "
+                             f"the table has {s.n_req} of {s.max_pages * s.page_size}")
+
+
 def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor,
                resid: torch.Tensor, k_cat: List[torch.Tensor], v_cat: List[torch.Tensor], sel_start: np.ndarray,
                q_rows: np.ndarray, stream=None, keep: bool = False, cache_stream=None, pages=None) -> dict:
@@ -43,6 +54,8 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     Hq, Hkv, d = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
     n_layers = len(layers)
     assert n_layers >= 2
+    if pages is not None:
+        _fit(pages, n_layers, layout.n_req, layout.max_len)
     total_k, nq = int(sel_start[-1]), int(len(q_rows))
     n_act = total_k + nq
     eps = float(shape.rms_eps)
@@ -151,6 +164,8 @@ def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Te
     T, h = layout.total_tokens, shape.hidden
     Hq, Hkv, d = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
     n_layers = len(layers)
+    if pages is not None:
+        _fit(pages, n_layers, layout.n_req, layout.max_len)
     eps = float(shape.rms_eps)
     ffn = int(layers[0]["w_gate"].shape[0])
     ws_attn = layout.workspace(T)
@@ -205,6 +220,7 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
     is -1 is padding: no cache row is written for it and its outputs mean nothing.  ``w_vocab`` [vocab, h]: logits of every
     row too.  Returns dict(hidden, resid, logits)."""
     n, eps, b = layout.n_req, float(shape.rms_eps), bufs
+    _fit(pages, len(layers), n if row_req is None else 0, 0)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
         api.a3_selected_qkv_proj(layout, b.x, None, n, lw["wq"], lw["wk"], lw["wv"], q_out=b.q, k_out=b.k, v_out=b.v,

@@ -211,3 +211,29 @@ def test_evicted_cache_goes_on():
         vv = np.concatenate([np.stack([v[rows[h], h] for h in range(2)], 1), nv[r:r + 1]])
         want = gen.attend(q[r], kk, vv, 128 ** -0.5)
         assert np.abs(to_host(out)[r] - want).max() <= (2.0 ** -8 * 2 + 1e-3) * np.abs(vv).max()
+
+
+def test_pages_that_cannot_take_a_prompt_are_refused():
+    shape, w, sw, layers = _setup("f32", [70, 5])
+    lay, g, resid = api.Layout.from_workload(w), to_dev(sw["g_final"], "f32"), to_dev(sw["resid0"], "f32")
+    small = make_pages([32, 32], dtype="f32", Hq=8, Hkv=2, d=64, page=32, slack=0)       # 32 slots a request
+    one = make_pages([100], dtype="f32", Hq=8, Hkv=2, d=64, page=32)                     # one request
+    for pages in ([small] * 3, [one] * 3, [make_pages([100, 100], dtype="f32", Hq=8, Hkv=2, d=64, page=32)] * 2):
+        with pytest.raises(ValueError):
+            stack.prefill_stack(lay, shape, layers, g, resid, pages=pages)
+
+
+def test_pages_that_just_fit_are_taken():
+    """The longest context and the longest question belong to different requests: their sum is no request's length."""
+    shape = SHAPES["f32"]
+    w = synth.custom(shape, [[60], [2]], [4, 50], seed=3)                # 64 and 52 tokens: two pages of 32 each
+    sw = synth.draw_stack_weights(w, 3)
+    layers = [{k: to_dev(v, "f32") for k, v in lw.items()} for lw in sw["layers"]]
+    lay, g = api.Layout.from_workload(w), to_dev(sw["g_final"], "f32")
+    pages = [make_pages([64, 52], dtype="f32", Hq=8, Hkv=2, d=64, page=32, base=shape.rope_base, layout=shape.rope_layout, slack=0)
+             for _ in range(3)]
+    r = stack.prefill_stack(lay, shape, layers, g, to_dev(sw["resid0"], "f32"), keep_kv=True, pages=pages)
+    for l in range(3):
+        for i, (a, b) in enumerate(zip(w.seg_start, w.seg_start[1:])):
+            k, v = get(pages[l], i, 0, b - a)
+            assert np.array_equal(k, to_host(r["k"][l])[a:b]) and np.array_equal(v, to_host(r["v"][l])[a:b])
