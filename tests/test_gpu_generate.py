@@ -237,3 +237,44 @@ def test_pages_that_just_fit_are_taken():
         for i, (a, b) in enumerate(zip(w.seg_start, w.seg_start[1:])):
             k, v = get(pages[l], i, 0, b - a)
             assert np.array_equal(k, to_host(r["k"][l])[a:b]) and np.array_equal(v, to_host(r["v"][l])[a:b])
+
+
+def test_steps_that_advance_inside_the_graph():
+    """Slots, lengths and positions move on in a kernel of the graph itself, in front of the calls that read them."""
+    lens, new = [50, 3, 129], 6
+    shape = SHAPES["bf16"]
+    rng = np.random.default_rng(21)
+    val = lambda *s: synth.round_to_storage(rng.standard_normal(s, dtype=np.float32), "bf16")
+    p = make_pages([n + new for n in lens], Hq=8, Hkv=2, page=32, base=shape.rope_base, layout=1, n_pos=300)
+    prompt = [(val(n, 2, 128), val(n, 2, 128)) for n in lens]
+    for r, (k, v) in enumerate(prompt):
+        n = lens[r]
+        api.a3_paged_append(p, to_dev(k, "bf16"), to_dev(v, "bf16"), idev([r] * n), idev(np.arange(n)), None, n)
+    slot = idev(lens) - 1
+    length = slot + 1
+    k, v, q = (torch.empty((3, h, 128), dtype=torch.bfloat16, device="cuda") for h in (2, 2, 8))
+    q_out, out, ws = torch.empty_like(q), torch.empty_like(q), p.workspace(3)
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        slot.add_(1)
+        length.add_(1)
+        api.a3_paged_append(p, k, v, None, slot, slot, 3, q=q, q_out=q_out)
+        api.a3_paged_attention(p, q_out, None, length, 3, out, ws)
+    held = [(a.astype(np.float64), b.astype(np.float64)) for a, b in prompt]
+    for t in range(new):
+        nk, nv, nq = val(3, 2, 128), val(3, 2, 128), val(3, 8, 128)
+        for dst, src in ((k, nk), (v, nv), (q, nq)):
+            dst.copy_(to_dev(src, "bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        pos = np.array(lens) + t
+        kt, qt = gen.turn(nk, pos, shape.rope_base, 1, "bf16"), gen.turn(nq, pos, shape.rope_base, 1, "bf16")
+        for r in range(3):
+            held[r] = (np.concatenate([held[r][0], kt[r:r + 1]]), np.concatenate([held[r][1], nv[r:r + 1]]))
+            want = gen.attend(qt[r], *held[r], 128 ** -0.5)
+            # half a step of the output; and turned coordinates (of size 4 at most, nearly) that fp32 puts on the other side of a
+            # tie: one moves its logit by 2^-7 * 4 * 4 / sqrt(128) = 0.011, an output by half of that times the largest value;
+            # some 1e-4 of them do (fp32's error against a step of bf16), so that 0.02 covers three in one row
+            assert np.abs(to_host(out)[r] - want).max() <= (2.0 ** -8 + 0.02) * np.abs(held[r][1]).max()
