@@ -462,7 +462,7 @@ a3_status a3_lm_head(const a3_layout *layout, const void *hidden, const int *row
  * A row of nothing but -inf, or with a NaN or +inf, has no distribution: its logprob, entropy and top_logprob are NaN.
  * tokens: device int32 [n_rows, n_given]; logprob, entropy, top_logprob: float; top_idx: int32.  entropy may be NULL; tokens and
  * logprob are not looked at for n_given = 0, the top outputs for n_top = 0.  0 <= n_top <= min(vocab, 64).
- * ws: a3_token_logprobs_ws_bytes() bytes, 16-byte aligned, contents of no concern before or after. */
+ * ws: a3_token_logprobs_ws_bytes() bytes (which serve fewer rows too), 16-byte aligned, contents of no concern before or after. */
 size_t a3_token_logprobs_ws_bytes(int n_rows, int vocab, int n_top);
 a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows, int vocab, long long ld, const int *tokens, int n_given,
                             int n_top, float *logprob, float *entropy, int *top_idx, float *top_logprob, void *ws,

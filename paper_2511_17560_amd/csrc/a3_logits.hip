@@ -471,16 +471,19 @@ logprobs_join_kernel(logprob_args a) {
 // Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of no less than two vectors a thread.
 constexpr int kLpSlices = 64;
 static_assert(kLpSlices * kLpTop == 16 * kLpThreads, "logprobs_join_kernel's keys");
-int logprob_slices(int n_rows, int vocab, int elem) {
-  const int by_rows = (1024 + n_rows - 1) / n_rows, by_size = (int)((long long)vocab * elem / (16 * 2 * kLpThreads));
-  const int n = by_rows < by_size ? by_rows : by_size;
-  return n < 1 ? 1 : n > kLpSlices ? kLpSlices : n;
+constexpr int kLpPieces = 1024;                                // of all rows, about
+int logprob_slices_by_size(int vocab, int elem) {
+  const long long n = (long long)vocab * elem / (16 * 2 * kLpThreads);
+  return n < 1 ? 1 : n > kLpSlices ? kLpSlices : (int)n;
 }
-size_t logprob_ws(int n_rows, int slices, int n_top, void *base, logprob_args *a) {
-  if (slices == 1) return 256;
+int logprob_slices(int n_rows, int vocab, int elem) {
+  const int by_rows = n_rows >= kLpPieces ? 1 : (kLpPieces + n_rows - 1) / n_rows, by_size = logprob_slices_by_size(vocab, elem);
+  return by_rows < by_size ? by_rows : by_size;
+}
+size_t logprob_ws(size_t pieces, int n_top, void *base, logprob_args *a) {
   a3_ws_cursor cur(base, 0);
-  float4 *part = (float4 *)cur.take((size_t)n_rows * slices * sizeof(float4));
-  unsigned long long *top = (unsigned long long *)cur.take((size_t)n_rows * slices * n_top * sizeof(unsigned long long));
+  float4 *part = (float4 *)cur.take(pieces * sizeof(float4));
+  unsigned long long *top = (unsigned long long *)cur.take(pieces * n_top * sizeof(unsigned long long));
   if (a) { a->part = part; a->part_top = top; }
   return cur.off;
 }
@@ -550,7 +553,12 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
 
 extern "C" size_t a3_token_logprobs_ws_bytes(int n_rows, int vocab, int n_top) {
   if (n_rows < 0 || vocab <= 0 || n_top < 0) return 0;
-  return n_rows == 0 ? 256 : logprob_ws(n_rows, logprob_slices(n_rows, vocab, 4), n_top, nullptr, nullptr);   // (bf16: no more slices)
+  // What serves every smaller number of rows too (the last piece of many rows is one): r rows are r min(s, ceil(1024 / r)) pieces, which
+  // is r s at most, below 1024 + r, and nothing from r = 1024 on.  (bf16: no more slices than float.)
+  const size_t rows = n_rows < kLpPieces ? n_rows : kLpPieces - 1, s = logprob_slices_by_size(vocab, 4);
+  const size_t pieces = rows * s < kLpPieces + rows ? rows * s : kLpPieces + rows;
+  const size_t need = s == 1 ? 0 : logprob_ws(pieces, n_top, nullptr, nullptr);
+  return need < 256 ? 256 : need;
 }
 
 extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows, int vocab, long long ld, const int *tokens, int n_given,
@@ -572,7 +580,7 @@ extern "C" a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows
   logprob_args a{logits, ld, vocab, n_given, n_top, tokens, logprob, entropy, top_logprob, top_idx,
                  logprob_slices(n_rows, vocab, dtype == A3_BF16 ? 2 : 4), nullptr, nullptr};
   A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_token_logprobs: too many rows");
-  logprob_ws(n_rows, a.slices, n_top, ws, &a);
+  if (a.slices > 1) logprob_ws((size_t)n_rows * a.slices, n_top, ws, &a);
   auto launch = [&](auto e) {
     typedef decltype(e) T;
     hipLaunchKernelGGL(logprobs_kernel<T>, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);

@@ -135,3 +135,13 @@ def test_binding_refuses_tensors_on_another_device():
         api.a3_token_logprobs(torch.zeros(2, 10, dtype=torch.float16), None, out)
     with pytest.raises(ValueError):
         api.a3_token_logprobs(torch.zeros(10, 2).t(), None, out)
+
+
+@pytest.mark.parametrize("vocab", [501, 8200, 32003, 128256])
+@pytest.mark.parametrize("n_top", [0, 8, 64])
+def test_a_workspace_of_log_probabilities_serves_fewer_rows(vocab, n_top):
+    """What is allocated for n rows has to do for every smaller number of them (few rows are cut into slices, many are not)."""
+    size = api.lib().a3_token_logprobs_ws_bytes
+    sizes = [size(n, vocab, n_top) for n in (*range(0, 2100), 5000, 100000, 2 ** 31 - 1)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0
+    assert sizes[-1] <= 2 << 20

@@ -278,3 +278,19 @@ def test_steps_that_advance_inside_the_graph():
             # tie: one moves its logit by 2^-7 * 4 * 4 / sqrt(128) = 0.011, an output by half of that times the largest value;
             # some 1e-4 of them do (fp32's error against a step of bf16), so that 0.02 covers three in one row
             assert np.abs(to_host(out)[r] - want).max() <= (2.0 ** -8 + 0.02) * np.abs(held[r][1]).max()
+
+
+@pytest.mark.parametrize("n, at_once", [(1100, 1024), (1030, 500)])
+def test_scores_whose_last_piece_has_few_rows(n, at_once):
+    """1024 rows and more are read whole, the rest behind them in slices, with the one workspace of all."""
+    h, vocab = 64, 16500
+    rng = np.random.default_rng(31)
+    x, w = rng.standard_normal((n, h), dtype=np.float32), 0.3 * rng.standard_normal((vocab, h), dtype=np.float32)
+    lay = api.Layout.decode(dtype="f32", n_q_heads=1, n_kv_heads=1, head_dim=64, hidden=h, rope_base=1e4, n_req=n)
+    tokens = rng.integers(0, vocab, (n, 1))
+    r = stack.score_tokens(lay, to_dev(x, "f32"), None, n, to_dev(w, "f32"), idev(tokens), api.TokenLogprobs(n, vocab, 1, 3), rows_at_once=at_once)
+    lp = gen.log_probs(x.astype(np.float64) @ w.T.astype(np.float64))
+    # logits below 16: 64 products and sums of fp32 (64 * 2^-24 * sum |x w|, below 64 * 6e-8 * 40), twice
+    assert np.abs(to_host(r.logprob) - gen.given(lp, tokens)).max() <= 4e-4
+    assert np.abs(to_host(r.top_logprob) - np.sort(lp, axis=1)[:, :-4:-1]).max() <= 4e-4
+    assert np.abs(to_host(r.entropy) - gen.entropy(lp)).max() <= 4e-4 * 2
