@@ -206,7 +206,8 @@ class DecodeBuffers:
         self.q, self.out = new(n, shape.n_q_heads, shape.head_dim), new(n, shape.n_q_heads, shape.head_dim)
         self.k, self.v = new(n, shape.n_kv_heads, shape.head_dim), new(n, shape.n_kv_heads, shape.head_dim)
         self.ws_attn = pages[0].workspace(n)
-        self.ws_tail = torch.empty(max(api.a3_block_tail_ws_bytes(layout, ffn, n), 256), dtype=torch.uint8, device=dev)
+        # (few rows can need more than many: their reductions are split, and the partial results want room)
+        self.ws_tail = torch.empty(max([256] + [api.a3_block_tail_ws_bytes(layout, ffn, m) for m in range(1, n + 1)]), dtype=torch.uint8, device=dev)
         self.logits = torch.empty((n, vocab), dtype=torch.float32, device=dev) if vocab else None
 
 
@@ -220,6 +221,8 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
     is -1 is padding: no cache row is written for it and its outputs mean nothing.  ``w_vocab`` [vocab, h]: logits of every
     row too.  Returns dict(hidden, resid, logits)."""
     n, eps, b = layout.n_req, float(shape.rms_eps), bufs
+    if len(b.x) < n or (w_vocab is not None and b.logits is None):
+        raise ValueError(f"buffers of {len(b.x)} rows{' without logits' if b.logits is None else ''} for a step of {n}")
     _fit(pages, len(layers), n if row_req is None else 0, 0)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
@@ -232,7 +235,7 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
                           resid, b.x, b.ws_tail, stream=stream)
     if w_vocab is not None:
         api.a3_lm_head(layout, b.x, None, n, w_vocab, b.logits, stream=stream)
-    return dict(hidden=b.x, resid=resid, logits=b.logits if w_vocab is not None else None)
+    return dict(hidden=b.x[:n], resid=resid, logits=b.logits[:n] if w_vocab is not None else None)
 
 
 def score_tokens(layout: api.Layout, hidden: torch.Tensor, row_idx, n_rows: int, w_vocab: torch.Tensor, tokens,

@@ -294,3 +294,28 @@ def test_scores_whose_last_piece_has_few_rows(n, at_once):
     assert np.abs(to_host(r.logprob) - gen.given(lp, tokens)).max() <= 4e-4
     assert np.abs(to_host(r.top_logprob) - np.sort(lp, axis=1)[:, :-4:-1]).max() <= 4e-4
     assert np.abs(to_host(r.entropy) - gen.entropy(lp)).max() <= 4e-4 * 2
+
+
+def test_buffers_serve_smaller_steps():
+    """Requests end: 80 rows' step in the buffers of 90 (whose block tails ask for less memory), as in buffers of its own."""
+    shape, w, sw, layers = _setup("bf16", [5] * 90, n_layers=2)
+    g, n = to_dev(sw["g_final"], "bf16"), 80
+    rng = np.random.default_rng(41)
+    x = synth.round_to_storage(rng.standard_normal((n, shape.hidden), dtype=np.float32), "bf16")
+    wv = to_dev(synth.round_to_storage(0.1 * rng.standard_normal((300, shape.hidden), dtype=np.float32), "bf16"), "bf16")
+    lay = lambda m: api.Layout.decode(dtype="bf16", n_q_heads=8, n_kv_heads=2, head_dim=128, hidden=shape.hidden, rope_base=shape.rope_base, n_req=m)
+    runs = []
+    for m in (90, 80):
+        pages = _pages(shape, [5] * 90, 2)
+        stack.prefill_stack(api.Layout.from_workload(w), shape, layers, g, to_dev(sw["resid0"], "bf16"), pages=pages)
+        bufs = stack.DecodeBuffers(lay(m), shape, shape.ffn, pages, 300)
+        slot = idev([5] * n)
+        r = stack.decode_stack(lay(n), shape, layers, g, to_dev(x, "bf16"), pages, slot, slot, slot + 1, bufs, w_vocab=wv)
+        assert r["hidden"].shape == (n, shape.hidden) and r["logits"].shape == (n, 300)
+        runs.append((to_host(r["hidden"]), to_host(r["logits"])))
+    assert np.array_equal(runs[0][0], runs[1][0]) and np.array_equal(runs[0][1], runs[1][1])
+    with pytest.raises(ValueError):
+        stack.decode_stack(lay(81), shape, layers, g, to_dev(x, "bf16"), pages, slot, slot, slot + 1, bufs)
+    with pytest.raises(ValueError):
+        stack.decode_stack(lay(n), shape, layers, g, to_dev(x, "bf16"), pages, slot, slot, slot + 1,
+                           stack.DecodeBuffers(lay(n), shape, shape.ffn, pages), w_vocab=wv)
