@@ -438,7 +438,8 @@ a3_status a3_paged_append(const a3_pages *pages, const void *k, const void *v, c
  * u < row_len[i] of request r = row_req[i] (NULL: i).  q, out: [n_rows, n_q_heads, head_dim], may be the same buffer; row_len:
  * device int32 [n_rows].  Rows may name the same request (with lengths of their own).  A row that sees nothing (length
  * <= 0) gets zeros; a length beyond the table is cut to it; the slots of a page that does not exist count as not seen; a row
- * whose request does not exist is left as it was.  Which bytes lie behind row_len in a page does not matter, NaN included.
+ * whose request does not exist is left as it was.  Which bytes lie behind row_len in a page does not matter, NaN included; a NaN in a
+ * seen key makes its head's output NaN, one in a seen value its coordinate.
  * Softmax statistics, weights' sums and products in float.  How the sums of a row are cut depends on the lengths of all rows:
  * a row may differ in its last bits between calls with other lengths, never between calls with the same.
  * ws: a3_paged_attention_ws_bytes(pages, n_rows) bytes, 16-byte aligned, contents of no concern before or after; one buffer

@@ -664,7 +664,8 @@ paged_attention_join_kernel(attend_args a) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const float f1 = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - top);
-        if (f1 != 0.f) { o += x[k] * f1; l += ml[k].y * f1; }
+        // (by number, not by weight: a piece whose logits are all NaN has no maximum, and its NaN stays one times 0)
+        if (i + k * groups < n) { o += x[k] * f1; l += ml[k].y * f1; }
       }
     }
   os[tid] = o;
