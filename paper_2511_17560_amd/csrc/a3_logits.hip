@@ -386,7 +386,9 @@ logprobs_kernel(logprob_args a) {
 #pragma unroll
       for (int i = 0; i < kLpValues; ++i) y[i] = (float)raw[i / V][i % V];
       if (c + kChunk < r.v1) load(c + kChunk);                 // on its way while this chunk is worked on
-      float top = y[0], half = y[1];                           // every other value: a short slice fills both halves too
+      // every other value: a short slice fills both halves too.  A half of nothing but NaN is -inf: left NaN, fminf below would take
+      // the other half's maximum for both, one value for two
+      float top = fmaxf(-INFINITY, y[0]), half = fmaxf(-INFINITY, y[1]);
 #pragma unroll
       for (int i = 2; i < kLpValues; i += 2) { top = fmaxf(top, y[i]); half = fmaxf(half, y[i + 1]); }
       second = fmaxf(second, fmaxf(fminf(top, half), fminf(most, fmaxf(top, half))));
