@@ -450,7 +450,8 @@ a3_status a3_paged_attention(const a3_pages *pages, const void *q, const int *ro
 
 /* logits[i, v] = sum_c hidden[row_idx[i], c] * w[v, c], float, row i at logits + i * ld.  hidden: [total_tokens, hidden] in the
  * layout's dtype (the final-normed rows a3_block_tail leaves); row_idx: device int32 [n_rows], NULL = rows 0 .. n_rows-1, a row
- * may be named more than once; w: [vocab, hidden], 16-byte aligned; ld >= vocab.  Any vocab; 4-byte aligned logits. */
+ * may be named more than once, and the logits of one outside [0, total_tokens) are left as they were (a padded list marks its rows
+ * with -1); w: [vocab, hidden], 16-byte aligned; ld >= vocab.  Any vocab; 4-byte aligned logits. */
 a3_status a3_lm_head(const a3_layout *layout, const void *hidden, const int *row_idx, int n_rows, const void *w, int vocab,
                      float *logits, long long ld, void *stream);
 

@@ -629,10 +629,11 @@ def a3_paged_attention(pages: Pages, q: torch.Tensor, row_req: Optional[torch.Te
 
 def a3_lm_head(layout: Layout, hidden: torch.Tensor, row_idx: Optional[torch.Tensor], n_rows: int, w: torch.Tensor,
                logits: torch.Tensor, stream=None) -> None:
-    """``w`` [vocab, hidden]; ``logits`` float32 [>= n_rows, vocab], rows may be further apart than vocab."""
+    """``hidden`` [total_tokens, hidden] (without ``row_idx`` n_rows rows do); ``w`` [vocab, hidden]; ``logits`` float32 [>= n_rows,
+    vocab], rows may be further apart than vocab."""
     h, vocab = layout.struct.hidden, w.shape[0]
     dev = _current(layout.device)
-    _hold(dev, torch_dtype(layout.dtype), 0 if row_idx is not None else n_rows * h, hidden)
+    _hold(dev, torch_dtype(layout.dtype), (layout.total_tokens if row_idx is not None else n_rows) * h, hidden)
     _hold(dev, torch_dtype(layout.dtype), vocab * h, w)
     _hold(dev, torch.int32, n_rows, row_idx)
     _hold(dev, torch.float32, 0, logits)

@@ -12,7 +12,7 @@ namespace {
 struct logits_args {
   const void *x;           // [*, K]
   const int *row_idx;
-  int n_rows;
+  int n_rows, total;       // rows of the list, and of x
   const void *w;           // [N, K]
   float *out;
   long long ld;
@@ -36,8 +36,8 @@ logits_kernel(logits_args a) {
       [&](int r) -> uint32_t { return (uint32_t)min(r, a.N - 1 - wt * P::BM) * (uint32_t)(a.K * sizeof(T)); },   // clamp: computed but never stored
       [&](int) -> const char * { return reinterpret_cast<const char *>(a.x); },
       [&](int r) -> uint32_t {
-        const int m = min(xt * P::BN + r, a.n_rows - 1);
-        return (uint32_t)(a.row_idx ? a.row_idx[m] : m) * (uint32_t)(a.K * sizeof(T));
+        const int m = min(xt * P::BN + r, a.n_rows - 1), row = a.row_idx ? a.row_idx[m] : m;
+        return ((uint32_t)row < (uint32_t)a.total ? (uint32_t)row : 0u) * (uint32_t)(a.K * sizeof(T));             // (no such row: likewise)
       });
   // block (i, j) as the matrix instruction leaves it: a lane has four consecutive features of one row, four lanes a 64-byte run
   // (16 consecutive features a lane, one float at a time: 512 rows of 128256 x 4096 641 us, 4096 rows 4800; this 446 and 3215).
@@ -47,7 +47,7 @@ logits_kernel(logits_args a) {
 #pragma unroll
   for (int j = 0; j < JB; ++j) {
     const int tok = xt * P::BN + 16 * (JB * wn + j) + l16;
-    if (tok >= a.n_rows) continue;
+    if (tok >= a.n_rows || (a.row_idx && (uint32_t)a.row_idx[tok] >= (uint32_t)a.total)) continue;
     float *p = a.out + (size_t)tok * a.ld + feat;
 #pragma unroll
     for (int i = 0; i < IB; ++i) {
@@ -503,7 +503,7 @@ extern "C" a3_status a3_lm_head(const a3_layout *L, const void *hidden, const in
   A3_REQUIRE(hidden && w && logits, A3_ERR_INVALID_ARG, "a3_lm_head: NULL tensor");
   A3_REQUIRE(a3_aligned16(hidden) && a3_aligned16(w) && ((uintptr_t)logits & 3) == 0, A3_ERR_INVALID_ARG,
              "a3_lm_head: tensors must be 16-byte aligned (logits 4)");
-  logits_args a{hidden, row_idx, n_rows, w, logits, ld, L->hidden, vocab, 0, 0, 0};
+  logits_args a{hidden, row_idx, n_rows, L->total_tokens, w, logits, ld, L->hidden, vocab, 0, 0, 0};
   hipStream_t st = (hipStream_t)stream;
   const bool bf16 = L->dtype == A3_BF16;
   A3_REQUIRE(!bf16 || L->hidden % 64 == 0, A3_ERR_UNSUPPORTED, "a3_lm_head: bf16 needs hidden %% 64 == 0, got %d", L->hidden);
