@@ -651,7 +651,8 @@ def a3_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], out:
     n_rows, vocab = logits.shape
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1 or (n_rows > 1 and logits.stride(0) < vocab):
         raise ValueError("a3_token_logprobs: logits are float32 or bfloat16 rows of consecutive elements")
-    if (tokens is None) != (out.n_given == 0):
+    # (rows of tokens are n_given apart: a wider tensor would rate every row but the first on another row's tokens)
+    if (tokens is None) != (out.n_given == 0) or (tokens is not None and tokens.dim() > 1 and tokens.shape[-1] != out.n_given):
         raise ValueError(f"a3_token_logprobs: tokens are int32 [{n_rows}, {out.n_given}], None for 0 given")
     dev = _current(logits.device)
     _hold(dev, torch.int32, n_rows * out.n_given, tokens)
