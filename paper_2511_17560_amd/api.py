@@ -657,6 +657,10 @@ def a3_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], out:
     dev = _current(logits.device)
     _hold(dev, torch.int32, n_rows * out.n_given, tokens)
     _hold(dev, torch.float32, n_rows, out.entropy)
+    _hold(dev, torch.float32, n_rows * out.n_given, out.logprob)
+    _hold(dev, torch.float32, n_rows * out.n_top, out.top_logprob)
+    _hold(dev, torch.int32, n_rows * out.n_top, out.top_idx)
+    _hold(dev, torch.uint8, 0, out.ws)
     _check(lib().a3_token_logprobs(A3_F32 if logits.dtype == torch.float32 else A3_BF16, logits.data_ptr(), n_rows, vocab,
                                    logits.stride(0) if n_rows > 1 else vocab, _ptr(tokens), out.n_given, out.n_top,
                                    _ptr(out.logprob), _ptr(out.entropy), _ptr(out.top_idx), _ptr(out.top_logprob), _ptr(out.ws),
