@@ -181,6 +181,16 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def torch_stream(stream) -> torch.cuda.Stream:
+    """The same argument as a torch stream (None: the current one; a raw handle: that stream, 0 the device's default one)."""
+    if stream is None:
+        return torch.cuda.current_stream()
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = _stream(stream)
+    return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+
+
 def torch_dtype(dtype: str) -> torch.dtype:
     return {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
 

@@ -243,7 +243,7 @@ def score_tokens(layout: api.Layout, hidden: torch.Tensor, row_idx, n_rows: int,
     """Log probabilities of given tokens (and entropy, alternatives) behind rows of final-normed hidden states, as fuse_stack,
     prefill_stack and decode_stack return them: ``tokens`` int32 [n_rows, out.n_given] beside the packed rows ``row_idx`` (None:
     the first n_rows).  The logits of ``rows_at_once`` rows at a time are formed and read (1024 rows of 128256: 0.5 GB)."""
-    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):      # the logits live and die on it
+    with torch.cuda.stream(api.torch_stream(stream)):                # the logits live and die on it
         logits = torch.empty((min(max(n_rows, 1), rows_at_once), w_vocab.shape[0]), dtype=torch.float32, device=hidden.device)
         for i in range(0, n_rows, rows_at_once):
             m = min(rows_at_once, n_rows - i)
