@@ -296,6 +296,7 @@ class Pages:
             if tuple(p.shape) != shape or p.dtype != dt or p.device != dev:
                 raise ValueError(f"Pages: a pool is {shape} of {dt} on {dev}, got {tuple(p.shape)} of {p.dtype} on {p.device}")
         fresh = rope_cs is None
+        self.own_rope = fresh            # whether rope_cs is what rope_base says, and not a table of the caller's
         self.rope_cs = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=dev) if fresh else rope_cs
         if tuple(self.rope_cs.shape) != (n_pos, head_dim // 2, 2) or self.rope_cs.dtype != torch.float32 or self.rope_cs.device != dev:
             raise ValueError(f"Pages: rope_cs is float32 {(n_pos, head_dim // 2, 2)} on {dev}")
@@ -315,9 +316,11 @@ class Pages:
     def sibling(self) -> "Pages":
         """Another layer's cache: pools of its own, the same page table and position table."""
         s = self.struct
-        return Pages(dtype=self.dtype, n_q_heads=s.n_q_heads, n_kv_heads=s.n_kv_heads, head_dim=s.head_dim, page_size=s.page_size,
-                     n_pages=s.n_pages, page_table=self.page_table, rope_base=s.rope_base, n_pos=s.n_pos, rope_layout=s.rope_layout,
-                     q8=self.q8, sm_scale=s.sm_scale, rope_cs=self.rope_cs)
+        p = Pages(dtype=self.dtype, n_q_heads=s.n_q_heads, n_kv_heads=s.n_kv_heads, head_dim=s.head_dim, page_size=s.page_size,
+                  n_pages=s.n_pages, page_table=self.page_table, rope_base=s.rope_base, n_pos=s.n_pos, rope_layout=s.rope_layout,
+                  q8=self.q8, sm_scale=s.sm_scale, rope_cs=self.rope_cs)
+        p.own_rope = self.own_rope
+        return p
 
     def workspace(self, n_rows: int) -> torch.Tensor:
         return torch.empty(max(a3_paged_attention_ws_bytes(self, n_rows), 256), dtype=torch.uint8, device=self.device)

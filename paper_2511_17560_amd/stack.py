@@ -10,6 +10,7 @@ front of Eq. 3, and Eq. 3-5).  Call sequencing and buffer allocation only; all a
 """
 from __future__ import annotations
 
+import math
 from typing import Dict, List, Sequence
 
 import numpy as np
@@ -22,12 +23,24 @@ def _bias(lw):
     return dict(bq=lw.get("bq"), bk=lw.get("bk"), bv=lw.get("bv"))
 
 
-def _fit(pages, n_layers: int, n_req: int, tokens: int) -> None:
-    """Refuses pages that cannot take what a call writes (a slot outside the page table would be skipped)."""
+def _fit(pages, n_layers: int, n_req: int, tokens: int, layout: api.Layout, prompt: bool) -> None:
+    """Refuses pages that cannot take what a call writes (a slot outside the page table would be skipped), and pages of another
+    model than the layout's.  A prompt's keys come turned by the layout and its rows attended with the layout's scale, and the pages do
+    both from then on; in a decoding step the pages alone do (its layout's rotation is the identity)."""
     if len(pages) < n_layers:
         raise ValueError(f"pages of {n_layers} layers are needed, got {len(pages)}")
+    L = layout.struct
     for p in pages[:n_layers]:
         s = p.struct
+        same = ["dtype", "n_q_heads", "n_kv_heads", "head_dim"]
+        if prompt and s.n_pos > 0:                               # (without positions the pages turn nothing)
+            same += ["rope_layout", "rope_base"] if p.own_rope else ["rope_layout"]
+        for name in same:
+            if getattr(s, name) != getattr(L, name):
+                raise ValueError(f"pages: their {name} is {getattr(s, name)}, the layout's {getattr(L, name)}")
+        scale = [x.sm_scale or x.head_dim ** -0.5 for x in (s, L)]
+        if prompt and not math.isclose(*scale, rel_tol=1e-6):     # (0 stands for 1 / sqrt(head_dim); floats)
+            raise ValueError("pages: their sm_scale is %g, the layout's %g" % tuple(scale))
         if s.n_req < n_req or s.max_pages * s.page_size < tokens:
             raise ValueError(f"pages: {n_req} requests of up to {tokens} tokens are needed, "
                              f"the table has {s.n_req} of {s.max_pages * s.page_size}")
@@ -44,7 +57,7 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     from host memory into a ring of device buffers while the layers before it compute, and ``k_cat`` / ``v_cat``
     are ignored; its blocks may be 8-bit (position recovery and dequantisation then run in one kernel).
     ``pages`` (one api.Pages per layer, a request of theirs for each of the layout's) receives every layer's fused cache,
-    token p of a request in slot p, so that decode_stack can go on.
+    token p of a request in slot p, so that decode_stack can go on; type, heads, rotation and scale of both have to be the same.
     Returns dict(sel_idx, act_idx, n_act, scores, resid, hidden): ``hidden`` [T, h] holds the final-normed
     output at the active rows.  With ``keep`` every layer's attention output, caches, residual stream and the
     hidden states handed to the next layer are kept too (``per_layer[l]``: k, v, out, resid, x_next; whole arrays
@@ -55,7 +68,7 @@ def fuse_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     n_layers = len(layers)
     assert n_layers >= 2
     if pages is not None:
-        _fit(pages, n_layers, layout.n_req, layout.max_len)
+        _fit(pages, n_layers, layout.n_req, layout.max_len, layout, prompt=True)
     total_k, nq = int(sel_start[-1]), int(len(q_rows))
     n_act = total_k + nq
     eps = float(shape.rms_eps)
@@ -165,7 +178,7 @@ def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Te
     Hq, Hkv, d = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
     n_layers = len(layers)
     if pages is not None:
-        _fit(pages, n_layers, layout.n_req, layout.max_len)
+        _fit(pages, n_layers, layout.n_req, layout.max_len, layout, prompt=True)
     eps = float(shape.rms_eps)
     ffn = int(layers[0]["w_gate"].shape[0])
     ws_attn = layout.workspace(T)
@@ -223,7 +236,7 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
     n, eps, b = layout.n_req, float(shape.rms_eps), bufs
     if len(b.x) < n or (w_vocab is not None and b.logits is None):
         raise ValueError(f"buffers of {len(b.x)} rows{' without logits' if b.logits is None else ''} for a step of {n}")
-    _fit(pages, len(layers), n if row_req is None else 0, 0)
+    _fit(pages, len(layers), n if row_req is None else 0, 0, layout, prompt=False)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
         api.a3_selected_qkv_proj(layout, b.x, None, n, lw["wq"], lw["wk"], lw["wv"], q_out=b.q, k_out=b.k, v_out=b.v,
