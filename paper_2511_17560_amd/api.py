@@ -598,6 +598,7 @@ def a3_page_bytes(pages: Pages) -> int:
 
 
 def a3_pages_prepare(pages: Pages, stream=None) -> None:
+    _current(pages.device)
     _check(lib().a3_pages_prepare(pages.ref, _stream(stream)), "a3_pages_prepare")
 
 
