@@ -231,11 +231,13 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
     the residual stream.  Row i belongs to request ``row_req[i]`` of the pages (None: i); its K and V go to slot
     ``row_slot[i]``, turned to position ``row_pos[i]``, and it sees the slots below ``row_len[i]`` (its own included: row_slot +
     1).  All four are device int32, so that a captured step is replayed with the next values in them; a row whose request
-    is -1 is padding: no cache row is written for it and its outputs mean nothing.  ``w_vocab`` [vocab, h]: logits of every
-    row too.  Returns dict(hidden, resid, logits)."""
+    is -1 is padding: no cache row is written for it and its outputs mean nothing (nor do those of a row whose slot or position
+    lies outside the pages).  ``w_vocab`` [vocab, h]: logits of every row too.  Returns dict(hidden, resid, logits)."""
     n, eps, b = layout.n_req, float(shape.rms_eps), bufs
     if len(b.x) < n or (w_vocab is not None and b.logits is None):
         raise ValueError(f"buffers of {len(b.x)} rows{' without logits' if b.logits is None else ''} for a step of {n}")
+    if w_vocab is not None and w_vocab.shape[0] != b.logits.shape[1]:
+        raise ValueError(f"buffers of {b.logits.shape[1]} logits for a vocabulary of {w_vocab.shape[0]}")
     _fit(pages, len(layers), n if row_req is None else 0, 0, layout, prompt=False)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
