@@ -430,7 +430,7 @@ a3_status a3_pages_prepare(const a3_pages *pages, void *stream);
  * A row whose request, slot, page or position does not exist is skipped: nothing of it is written, q_out included (a padded
  * batch marks its rows with request or slot -1).  No two rows may name the same slot of the same request, no page may belong
  * to two requests.  Turned in float and rounded once; A3_PAGES_Q8: turned in double, so that the codes are those of the exact
- * values (finite values). */
+ * values (finite values: as with a3_quantize_q8, a NaN element does not stay one in 8 bits). */
 a3_status a3_paged_append(const a3_pages *pages, const void *k, const void *v, const int *row_req, const int *row_slot,
                           const int *row_pos, int n_rows, const void *q, void *q_out, void *stream);
 

@@ -6,8 +6,10 @@ namespace {
 
 // ---------------------------------------------------------------------------------------
 // logits: the row-tiled MFMA GEMM of a3_gemm_pp.h (fp32: with the fp32 matrix instruction), float out.  Few rows: bound by the weights'
-// way from HBM (4 rows of 128256 x 4096, 1.05 GB: 158 us, 6.7 TB/s).  Many: by the matrix pipe and its power (512 rows 414 - 450 us, 1.2 - 1.3
-// PFLOP/s; 4096 rows 3.2 ms, 1.34), where a large library product reaches 1.36.
+// way from HBM (4 rows of 128256 x 4096, 1.05 GB: 160 us, 6.6 TB/s).  Many: by the matrix pipe and its power (512 rows 443 us, 1.21
+// PFLOP/s; 4096 rows 3.1 ms, 1.38).  Medians of 300 launches in a row over three sets of inputs; the first dozen after a pause
+// take up to 560 us for 512 rows.  The library's product with bf16 results of the same inputs, calls in turn with this one's: 4 rows 186 us
+// (176 here), 64 rows of 152064 x 3584 209 (220), 512 rows 509 (453), 4096 rows 2.9 ms (3.1).
 // ---------------------------------------------------------------------------------------
 struct logits_args {
   const void *x;           // [*, K]
@@ -72,8 +74,10 @@ logits_kernel(logits_args a) {
 // n values of the row are no smaller, so what lies below the largest of the four waves' bounds is out.  The noted chunks that reach it (some n of them) are looked at again,
 // each by half a wave, and the values found are ranked.  Where too many equal the bound (rows that are masked or constant), only the
 // larger ones are gathered, and of the equal ones the first n in the row's order.  Slices of a row are put together by a second kernel.
-// Bound by HBM (1024 rows of 128256 fp32 92 us without alternatives, 5.7 TB/s, 104 with 20) or, bf16, by the 12 issue slots a value takes
-// (exponential 4; 50 us and 61); few rows by latency (1 row 9.6 + 4.8 us).
+// fp32: bound by HBM (1024 rows of 128256 91 us without alternatives, 5.8 TB/s, 103 with 20).  bf16: those rows take 50 us and 59, where
+// reading alone would take 37 (at the 7.1 TB/s that it reaches) and the vector unit is busy for 35 (10.4 issue slots a value, 2 of them
+// the exponential's): neither hides the other wholly.  1500 rows of 32003 bf16, all of them in flight at once: 22 us, and 5.5 more for choosing
+// 8 alternatives when all have been read.  Few rows: latency (1 row 9.6 + 4.8 us).
 struct logprob_args {
   const void *x;
   long long ld;

@@ -39,8 +39,9 @@ pages_rope_kernel(float2 *cs, long long total, int half, double base) {
 // A lane holds 16 coordinates of one head of one row, as two runs of 8 so that both RoPE pairings are inside it (half pairing:
 // 8c .. and d / 2 + 8c ..); d / 16 lanes a head, a wave 64 * 16 / d heads of one row, the row's heads in the order K, V, Q.
 // Everything a wave looks up (request, slot, position, page) is the same for all its lanes.
-// Bound by memory for a prompt (16448 rows of 8 KV heads x 128, 135 MB in and out: 27.3 us, 4.9 TB/s, as fast as a copy), by the chain
-// slot - page - store for a step's rows (1 row of 8 KV and 32 query heads 2.6 us; 32 rows into 8-bit pages 4.8).
+// Bound by memory for a prompt (16448 rows of 8 KV heads x 128, 135 MB in and out: 29 us, 4.6 TB/s; a copy reaches 5.35; into 8-bit pages,
+// 102 MB, 33 us, 3.1 TB/s), by the chain slot - page - store for a step's rows (1 row of 8 KV and 32 query heads 2.7 us; 32 rows into
+// 8-bit pages 4.8).
 struct append_args {
   pages_args p;
   const void *k, *v, *q;
@@ -180,9 +181,10 @@ __device__ __forceinline__ bf16x8 codes8(const uint32_t (&w)[2]) {
 // The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float): a
 // comparison a slab instead of a reduction over lanes.
 //
-// Bound by HBM; both kernels, 8 KV heads x 128: 64 requests of 32K tokens 1224 us (8.6 GB, 7.0 TB/s), 8 of 64K 315 (6.8 TB/s; 8-bit pages 178,
-// 6.2), 128 of 4096 (4 KV heads) 161 (6.7).  About 10 us of a call are not: the start (lengths, page numbers, first slabs: 5 us) and the
-// join (5 us); one request of 16K tokens takes 21 us, of 500 12.  Two workgroups of four waves a compute unit, 16 KB a wave on its way (one
+// Bound by HBM; both kernels, 8 KV heads x 128: 64 requests of 32K tokens 1224 us (8.6 GB, 7.0 TB/s), 8 of 64K 317 (6.8 TB/s; 8-bit pages 180,
+// 6.2), 128 of 4096 (4 KV heads) 161 (6.7); 8 KV heads x 64: 16 of 16K with fp32 pages 165 (6.5), with fp32 rows over 8-bit pages 69 (4.1).
+// About 10 us of a call are not: the start (lengths, page numbers, first slabs: 5 us) and the join (5 us); one request of 16K tokens takes
+// 21 us, of 500 12.  Two workgroups of four waves a compute unit, 16 KB a wave on its way (one
 // workgroup, or four half as long: up to 40 % and 15 % slower).
 struct attend_args {
   pages_args p;
@@ -329,7 +331,8 @@ paged_attention_kernel(attend_args a) {
     if (page < 0 || page >= a.p.n_pages) { s.n = 0; return; }
     const size_t block = ((size_t)page * Hkv + p.head) * head_bytes;
     const int at = slot & ((1 << a.p.page_shift) - 1);
-    // every byte is read once: nontemporal (8 requests of 64K tokens 362 -> 326 us, 48 of 4000 79 -> 71)
+    // a row reads every byte once: nontemporal (8 requests of 64K tokens 362 -> 326 us, 48 of 4000 79 -> 71; rows that name the
+    // same request read its bytes again)
     const char *kb = a.p.k_pool + block + at * F::kRow, *vb = a.p.v_pool + block + at * F::kRow;
 #pragma unroll
     for (int b = 0; b < F::KB; ++b)
