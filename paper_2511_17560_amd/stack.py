@@ -257,7 +257,8 @@ def score_tokens(layout: api.Layout, hidden: torch.Tensor, row_idx, n_rows: int,
                  out: api.TokenLogprobs, rows_at_once: int = 1024, stream=None) -> api.TokenLogprobs:
     """Log probabilities of given tokens (and entropy, alternatives) behind rows of final-normed hidden states, as fuse_stack,
     prefill_stack and decode_stack return them: ``tokens`` int32 [n_rows, out.n_given] beside the packed rows ``row_idx`` (None:
-    the first n_rows).  The logits of ``rows_at_once`` rows at a time are formed and read (1024 rows of 128256: 0.5 GB)."""
+    the first n_rows; of a row outside [0, total_tokens) the outputs mean nothing).  The logits of ``rows_at_once`` rows at a
+    time are formed and read (1024 rows of 128256: 0.5 GB).  ``stream``: a torch stream or a raw handle."""
     with torch.cuda.stream(api.torch_stream(stream)):                # the logits live and die on it
         logits = torch.empty((min(max(n_rows, 1), rows_at_once), w_vocab.shape[0]), dtype=torch.float32, device=hidden.device)
         for i in range(0, n_rows, rows_at_once):
