@@ -470,6 +470,76 @@ a3_status a3_token_logprobs(int dtype, const void *logits, int n_rows, int vocab
                             int n_top, float *logprob, float *entropy, int *top_idx, float *top_logprob, void *ws,
                             size_t ws_bytes, void *stream);
 
+/* ---- several candidates of one request at once ------------------------------------------------------------------
+ *
+ * Drafted tokens that the model verifies in one step, and beams, over the same pages.
+ *
+ * A drafted tree of n tokens, parents in front of their children, stands in slots group_len .. group_len + n - 1 of its request,
+ * behind the group_len committed ones; row 0 is its root (the last token that is certain).  The rows of a call are packed: those of
+ * group g are group_start[g] .. group_start[g + 1] - 1 of q and out (device int32 [n_groups + 1], in [0, n_rows], ascending: a
+ * group whose bounds are not counts as empty), of request group_req[g] (NULL: g).  a3_paged_append puts the drafted tokens' K
+ * and V there first (row_slot = group_len + j, row_pos = the position of their depth).
+ *
+ * a3_tree_attention: out[i, hq] = sum_u softmax_u(q[i, hq] . K[r, u, hq/G] * sm_scale) V[r, u, hq/G] over the slots u < group_len[g] and
+ * u = group_len[g] + t, t < n, that row i sees: bit t % 32 of mask[i, t / 32] (device int32 [n_rows, mask_words], 32 * mask_words >=
+ * max_rows; itself only with its own bit); mask NULL: the rows in front of it and itself (a chain).  q, out: [n_rows, n_q_heads,
+ * head_dim], may be the same buffer.  max_rows: the most rows of a group, 1 .. 1024 (host value; rows of a group behind it are left as
+ * they were, their slots not seen).  A row that sees nothing gets zeros; a negative group_len counts as 0; slots beyond the table, or
+ * of a page that does not exist, count as not seen; the rows of a group whose request does not exist and rows of no group are left
+ * as they were.  What lies in slots that a row does not see, behind the tree or in another branch of it, does not matter to that row,
+ * NaN included; a NaN in a seen key makes its head's output NaN, one in a seen value its coordinate.
+ * The cache is read once for all rows of a group.  Softmax statistics, weights' sums and products in float.  How sums are cut depends on
+ * n_groups, max_rows and all groups' lengths and rows: a row may differ in its last bits between calls where those differ.
+ * ws: a3_tree_attention_ws_bytes(pages, n_groups, max_rows) bytes (which serve fewer groups and rows too), 16-byte aligned, contents of no
+ * concern before or after; one buffer serves one call at a time. */
+size_t a3_tree_attention_ws_bytes(const a3_pages *pages, int n_groups, int max_rows);
+a3_status a3_tree_attention(const a3_pages *pages, const void *q, int n_groups, const int *group_start, const int *group_req,
+                            const int *group_len, const int *mask, int mask_words, int n_rows, int max_rows, void *out, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/* From the logits of drafted rows to the accepted path of every tree.  picked[i] = the largest logit's index of row i (equal ones: the
+ * lowest; -0 equals 0; NaN below everything); logits NULL: picked is given (a sampler's choice).  The path begins at row 0 and goes
+ * on, as long as there is one, to the first row c behind the last one, parent[c] = the last one (numbers inside the group), with
+ * tokens[c] = its picked token; a path of max_path rows ends.  For group g, with L = group_len[g]:
+ *   count[g]        rows of the path (0: the group is empty, everything else of it -1)
+ *   path[g, m]      their numbers inside the group; -1 behind the last
+ *   next_token[g]   what was picked behind the last one
+ *   src_slot[g, m], dst_slot[g, m]   L + path[g, m] and L + m (-1 behind the last): a3_paged_move brings the path to the front with them
+ * logits: rows of `dtype` (an a3_dtype), ld >= vocab apart, any start; tokens, parent, picked: device int32 [n_rows]; path, src_slot,
+ * dst_slot: int32 [n_groups, max_path]; count, next_token: [n_groups].  src_slot and dst_slot may be NULL both (group_len then too).
+ * Groups as above; rows of a group behind its max_rows-th (1 .. 1024) are not looked at.  1 <= max_path <= 64.
+ * ws: a3_tree_accept_ws_bytes() bytes (which serve fewer rows too; none is needed for logits NULL), 16-byte aligned. */
+size_t a3_tree_accept_ws_bytes(int n_rows, int vocab);
+a3_status a3_tree_accept(int dtype, const void *logits, int vocab, long long ld, int *picked, const int *tokens, const int *parent,
+                         int n_groups, const int *group_start, const int *group_len, int n_rows, int max_rows, int max_path, int *count,
+                         int *path, int *next_token, int *src_slot, int *dst_slot, void *ws, size_t ws_bytes, void *stream);
+
+/* Copies token rows (K and V, every KV head) between slots, in every layer: move i = s * set_size + m of set s copies slots src_slot[i] + o
+ * of request src_req[i] to slots dst_slot[i] + o of dst_req[i], o < n_slots[i] (NULL: 1; cut to max_slots, a host value).  src_req,
+ * dst_req NULL: s.  The moves of a set happen at once for every o: all are read before any is written, so that a set may shift or exchange rows
+ * (a path to the front of its tree; beam b continuing beam parent[b], slot by slot).  Nothing else is ordered: no slot may be
+ * written twice, and none that is written by one set, or at one o, may be read by another set, or at another o.  A move is left out
+ * where its source or target does not exist (request, slot, page; -1: padding), or where both are the same place.
+ * layers: HOST array of n_layers structs that share everything but their pools and their dtype's scale and rotation: format, dtype, heads,
+ * head_dim, page_size, n_pages, n_req, max_pages, page_table.  Index arrays: device int32 [n_sets, set_size], 1 <= set_size <= 64.
+ * Requests may share pages that nothing writes (a prompt's full pages among its beams). */
+a3_status a3_paged_move(const a3_pages *layers, int n_layers, const int *src_req, const int *src_slot, const int *dst_req,
+                        const int *dst_slot, const int *n_slots, int max_slots, int n_sets, int set_size, void *stream);
+
+/* The n_best best continuations of every group of n_beams beams.  Rows g * n_beams + b of logits belong to group g; the continuation of
+ * beam b with token v is worth score[row] + x_v - m - log Z (the row's log probability as in a3_token_logprobs), one of a beam with done[row]
+ * != 0 exists once, with end_token, and is worth score[row] (done NULL: none).  Best first; equal ones by the lower beam, then the lower token.
+ *   best_score[g, j] (float), best_row[g, j] (its row of logits), best_token[g, j]
+ * A token with a logit of -inf is none; a beam whose score is not finite, or whose row of logits has no distribution (NaN, +inf, nothing but
+ * -inf) and that is not done, has none; where a group has fewer than n_best, the rest is -inf, -1, -1.
+ * Z is summed and worths are compared beyond float's precision (double where terms meet).
+ * logits: `dtype` (an a3_dtype), ld >= vocab, any start; score: float [n_groups * n_beams]; done: int32.  1 <= n_beams, n_best <= 64.
+ * ws: a3_beam_select_ws_bytes() bytes (which serve fewer groups too), 16-byte aligned, contents of no concern. */
+size_t a3_beam_select_ws_bytes(int n_groups, int n_beams, int vocab, int n_best);
+a3_status a3_beam_select(int dtype, const void *logits, int n_groups, int n_beams, int vocab, long long ld, const float *score,
+                         const int *done, int end_token, int n_best, float *best_score, int *best_row, int *best_token, void *ws,
+                         size_t ws_bytes, void *stream);
+
 /* ---- tuning values (for tests and measurements; the defaults are what the library picks by itself) -----------
  * Process-wide integers, read when a call is made; value < 0 restores the library's own choice.  Names:
  *   "attn_wgs"        workgroups (shares of the work) per KV head in a3_fused_attention, 1 .. 1024

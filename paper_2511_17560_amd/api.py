@@ -28,6 +28,8 @@ EXPORTS = ["a3_workspace_bytes", "a3_layout_prepare", "a3_rope_realign", "a3_que
            "a3_select_chunk_edges", "a3_chunk_cache_load", "a3_rope_realign_q8", "a3_q8_row_bytes", "a3_quantize_q8",
            "a3_chunk_cache_load_q8", "a3_chunk_file_read", "a3_page_bytes", "a3_pages_prepare", "a3_paged_append",
            "a3_paged_attention_ws_bytes", "a3_paged_attention", "a3_lm_head", "a3_token_logprobs_ws_bytes", "a3_token_logprobs",
+           "a3_tree_attention_ws_bytes", "a3_tree_attention", "a3_tree_accept_ws_bytes", "a3_tree_accept", "a3_paged_move",
+           "a3_beam_select_ws_bytes", "a3_beam_select",
            "a3_set_tuning", "a3_recompute_count", "a3_chunk_edge_sel_start", "a3_strerror", "a3_last_error", "a3_version"]
 
 
@@ -150,7 +152,18 @@ def lib() -> C.CDLL:
     L.a3_token_logprobs_ws_bytes.argtypes = [I, I, I]
     L.a3_token_logprobs_ws_bytes.restype = C.c_size_t
     L.a3_token_logprobs.argtypes = [I, V, I, I, C.c_longlong, V, I, I, V, V, V, V, V, C.c_size_t, V]
-    for name in ("a3_pages_prepare", "a3_paged_append", "a3_paged_attention", "a3_lm_head", "a3_token_logprobs"):
+    L.a3_tree_attention_ws_bytes.argtypes = [G, I, I]
+    L.a3_tree_attention_ws_bytes.restype = C.c_size_t
+    L.a3_tree_attention.argtypes = [G, V, I, V, V, V, V, I, I, I, V, V, C.c_size_t, V]
+    L.a3_tree_accept_ws_bytes.argtypes = [I, I]
+    L.a3_tree_accept_ws_bytes.restype = C.c_size_t
+    L.a3_tree_accept.argtypes = [I, V, I, C.c_longlong, V, V, V, I, V, V, I, I, I, V, V, V, V, V, V, C.c_size_t, V]
+    L.a3_paged_move.argtypes = [G, I, V, V, V, V, V, I, I, I, V]
+    L.a3_beam_select_ws_bytes.argtypes = [I, I, I, I]
+    L.a3_beam_select_ws_bytes.restype = C.c_size_t
+    L.a3_beam_select.argtypes = [I, V, I, I, I, C.c_longlong, V, V, I, I, V, V, V, V, C.c_size_t, V]
+    for name in ("a3_pages_prepare", "a3_paged_append", "a3_paged_attention", "a3_lm_head", "a3_token_logprobs", "a3_tree_attention",
+                 "a3_tree_accept", "a3_paged_move", "a3_beam_select"):
         getattr(L, name).restype = I
     L.a3_set_tuning.argtypes = [C.c_char_p, I]
     L.a3_set_tuning.restype = I
@@ -325,6 +338,23 @@ class Pages:
     def workspace(self, n_rows: int) -> torch.Tensor:
         return torch.empty(max(a3_paged_attention_ws_bytes(self, n_rows), 256), dtype=torch.uint8, device=self.device)
 
+    def tree_workspace(self, n_groups: int, max_rows: int) -> torch.Tensor:
+        return torch.empty(max(a3_tree_attention_ws_bytes(self, n_groups, max_rows), 256), dtype=torch.uint8, device=self.device)
+
+
+class PageLayers:
+    """The pages of a stack's layers as one, for calls that work on all of them: they share the page table and its shape (as
+    ``Pages.sibling`` makes them)."""
+
+    def __init__(self, pages):
+        self.pages = list(pages)
+        if not self.pages:
+            raise ValueError("PageLayers: no pages")
+        self.device, self.page_table = self.pages[0].device, self.pages[0].page_table
+        if any(p.device != self.device or p.page_table.data_ptr() != self.page_table.data_ptr() for p in self.pages):
+            raise ValueError("PageLayers: the layers share one page table")
+        self.structs = (a3_pages * len(self.pages))(*[p.struct for p in self.pages])
+
 
 class TokenLogprobs:
     """What a3_token_logprobs writes, and its workspace, allocated once for up to ``n_rows`` rows."""
@@ -343,6 +373,30 @@ class TokenLogprobs:
         part.logprob, part.entropy = self.logprob[first:end], self.entropy[first:end]
         part.top_idx, part.top_logprob = self.top_idx[first:end], self.top_logprob[first:end]
         return part
+
+
+class TreeAccepted:
+    """What a3_tree_accept writes, and its workspace, allocated once for up to ``n_groups`` trees of ``n_rows`` rows together.
+    ``vocab`` 0: the picked tokens are given."""
+
+    def __init__(self, n_groups: int, n_rows: int, max_path: int, vocab: int = 0, device="cuda"):
+        new = lambda *s: torch.empty(s, dtype=torch.int32, device=device)
+        self.max_path = max_path
+        self.picked, self.count, self.next_token = new(n_rows), new(n_groups), new(n_groups)
+        self.path, self.src_slot, self.dst_slot = (new(n_groups, max_path) for _ in range(3))
+        n = int(lib().a3_tree_accept_ws_bytes(n_rows, vocab)) if vocab else 0
+        self.ws = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+class BeamChoice:
+    """What a3_beam_select writes, and its workspace, allocated once for up to ``n_groups`` groups of ``n_beams`` beams."""
+
+    def __init__(self, n_groups: int, n_beams: int, vocab: int, n_best: int, device="cuda"):
+        new = lambda dtype: torch.empty((n_groups, n_best), dtype=dtype, device=device)
+        self.n_beams, self.n_best = n_beams, n_best
+        self.score, self.row, self.token = new(torch.float32), new(torch.int32), new(torch.int32)
+        n = int(lib().a3_beam_select_ws_bytes(n_groups, n_beams, vocab, n_best))
+        self.ws = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
 # ---- entry points (same names as the C ABI) -----------------------------------------------------
@@ -680,3 +734,89 @@ def a3_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], out:
                                    _ptr(out.logprob), _ptr(out.entropy), _ptr(out.top_idx), _ptr(out.top_logprob), _ptr(out.ws),
                                    out.ws.numel(), _stream(stream)), "a3_token_logprobs")
     return out
+
+
+# ---- several candidates of one request at once -------------------------------------------------------
+
+def a3_tree_attention_ws_bytes(pages: Pages, n_groups: int, max_rows: int) -> int:
+    return int(lib().a3_tree_attention_ws_bytes(pages.ref, int(n_groups), int(max_rows)))
+
+
+def a3_tree_attention(pages: Pages, q: torch.Tensor, group_start: torch.Tensor, group_req: Optional[torch.Tensor],
+                      group_len: torch.Tensor, mask: Optional[torch.Tensor], n_rows: int, max_rows: int, out: torch.Tensor,
+                      ws: torch.Tensor, stream=None) -> None:
+    """``group_start`` int32 [n_groups + 1]; ``mask`` int32 [n_rows, words] or None (chains)."""
+    dev, n_groups = _current(pages.device), group_start.numel() - 1
+    _hold(dev, pages.torch_dtype, n_rows * pages.q_elems, q, out)
+    _hold(dev, torch.int32, n_groups, group_req, group_len)
+    _hold(dev, torch.int32, 1, group_start)
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] < n_rows:
+            raise ValueError(f"a3_tree_attention: mask is int32 [{n_rows}, words], got {tuple(mask.shape)}")
+        _hold(dev, torch.int32, 0, mask)
+        words = mask.shape[1]
+    _hold(dev, torch.uint8, 0, ws)
+    _check(lib().a3_tree_attention(pages.ref, _ptr(q), n_groups, _ptr(group_start), _ptr(group_req), _ptr(group_len), _ptr(mask), words,
+                                   int(n_rows), int(max_rows), _ptr(out), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)),
+           "a3_tree_attention")
+
+
+def a3_tree_accept(logits: Optional[torch.Tensor], tokens: torch.Tensor, parent: torch.Tensor, group_start: torch.Tensor,
+                   group_len: torch.Tensor, n_rows: int, max_rows: int, out: TreeAccepted, stream=None) -> TreeAccepted:
+    """``logits`` [n_rows, vocab] float32 or bfloat16, rows may be further apart than vocab; None: ``out.picked`` holds the picked
+    tokens.  ``tokens``, ``parent`` int32 [n_rows].  Writes the first n_groups rows of ``out`` and returns it."""
+    n_groups = group_start.numel() - 1
+    vocab = ld = dtype = 0
+    if logits is not None:
+        vocab, ld, dtype = _logit_rows("a3_tree_accept", logits, n_rows)
+    dev = _current(out.picked.device)
+    if logits is not None and logits.get_device() != dev:
+        raise ValueError(f"a3_tree_accept: logits are on {logits.device}, the outputs on cuda:{dev}")
+    _hold(dev, torch.int32, n_rows, tokens, parent, out.picked)
+    _hold(dev, torch.int32, n_groups, group_len, out.count, out.next_token)
+    _hold(dev, torch.int32, 1, group_start)
+    _hold(dev, torch.int32, n_groups * out.max_path, out.path, out.src_slot, out.dst_slot)
+    _hold(dev, torch.uint8, 0, out.ws)
+    _check(lib().a3_tree_accept(dtype, None if logits is None else logits.data_ptr(), vocab, ld, _ptr(out.picked), _ptr(tokens), _ptr(parent),
+                                n_groups, _ptr(group_start), _ptr(group_len), int(n_rows), int(max_rows), out.max_path, _ptr(out.count),
+                                _ptr(out.path), _ptr(out.next_token), _ptr(out.src_slot), _ptr(out.dst_slot), _ptr(out.ws), out.ws.numel(),
+                                _stream(stream)), "a3_tree_accept")
+    return out
+
+
+def a3_paged_move(layers: PageLayers, src_req: Optional[torch.Tensor], src_slot: torch.Tensor, dst_req: Optional[torch.Tensor],
+                  dst_slot: torch.Tensor, n_slots: Optional[torch.Tensor], max_slots: int, n_sets: int, set_size: int, stream=None) -> None:
+    """Index tensors int32 [n_sets, set_size]."""
+    dev = _current(layers.device)
+    _hold(dev, torch.int32, n_sets * set_size, src_req, src_slot, dst_req, dst_slot, n_slots)
+    _check(lib().a3_paged_move(layers.structs, len(layers.structs), _ptr(src_req), _ptr(src_slot), _ptr(dst_req), _ptr(dst_slot), _ptr(n_slots),
+                               int(max_slots), int(n_sets), int(set_size), _stream(stream)), "a3_paged_move")
+
+
+def a3_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[torch.Tensor], end_token: int, out: BeamChoice,
+                   stream=None) -> BeamChoice:
+    """``logits`` [n_groups * out.n_beams, vocab] float32 or bfloat16, rows may be further apart than vocab; ``score`` float32 and
+    ``done`` int32 (or None) of every row.  Writes the first n_groups rows of ``out`` and returns it."""
+    n_rows = logits.shape[0]
+    if n_rows % out.n_beams:
+        raise ValueError(f"a3_beam_select: {n_rows} rows of logits are no groups of {out.n_beams} beams")
+    vocab, ld, dtype = _logit_rows("a3_beam_select", logits, n_rows)
+    dev, n_groups = _current(logits.device), n_rows // out.n_beams
+    _hold(dev, torch.float32, n_rows, score)
+    _hold(dev, torch.int32, n_rows, done)
+    _hold(dev, torch.float32, n_groups * out.n_best, out.score)
+    _hold(dev, torch.int32, n_groups * out.n_best, out.row, out.token)
+    _hold(dev, torch.uint8, 0, out.ws)
+    _check(lib().a3_beam_select(dtype, logits.data_ptr(), n_groups, out.n_beams, vocab, ld, _ptr(score), _ptr(done), int(end_token), out.n_best,
+                                _ptr(out.score), _ptr(out.row), _ptr(out.token), _ptr(out.ws), out.ws.numel(), _stream(stream)), "a3_beam_select")
+    return out
+
+
+def _logit_rows(who: str, logits: torch.Tensor, n_rows: int):
+    """(vocab, distance of rows, a3_dtype) of rows of logits."""
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or logits.shape[0] < n_rows or logits.stride(1) != 1 \
+            or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]):
+        raise ValueError(f"{who}: logits are float32 or bfloat16 rows of consecutive elements, {n_rows} of them, got {tuple(logits.shape)} {logits.dtype}")
+    vocab = logits.shape[1]
+    return vocab, logits.stride(0) if logits.shape[0] > 1 else vocab, A3_F32 if logits.dtype == torch.float32 else A3_BF16

@@ -6,7 +6,8 @@ front of Eq. 3, and Eq. 3-5).  Call sequencing and buffer allocation only; all a
                    Q of the rows [Re, Q] -> attention (Eq. 4) -> H(.)
     layers >= 2    realign the layer's chunk cache (Eq. 2); Q/K/V of the rows [Re, Q] from X_l = H(O_{l-1}),
                    K/V stored into the cache (Eq. 5); attention; H(.)
-    afterwards     one token per request and step: every layer's fused cache goes on as pages that grow (decode_stack)
+    afterwards     one token per request and step: every layer's fused cache goes on as pages that grow (decode_stack); drafted
+                   tokens of a request verified in one step (verify_stack), several beams of a request (beam_stack)
 """
 from __future__ import annotations
 
@@ -210,15 +211,18 @@ def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Te
 
 class DecodeBuffers:
     """What one decoding step of up to ``layout.n_req`` rows writes, allocated once (a captured graph keeps using them).
-    ``layout`` is an api.Layout.decode; ``pages`` one api.Pages per layer; ``vocab`` > 0 asks for logits too."""
+    ``layout`` is an api.Layout.decode; ``pages`` one api.Pages per layer; ``vocab`` > 0 asks for logits too; ``tree`` (trees, most
+    tokens of one) for steps over drafted trees."""
 
-    def __init__(self, layout: api.Layout, shape, ffn: int, pages: Sequence[api.Pages], vocab: int = 0):
+    def __init__(self, layout: api.Layout, shape, ffn: int, pages: Sequence[api.Pages], vocab: int = 0, tree=None):
         dev, dt, n = layout.device, api.torch_dtype(layout.dtype), layout.n_req
         new = lambda *s: torch.empty(s, dtype=dt, device=dev)
         self.x = new(n, shape.hidden)
         self.q, self.out = new(n, shape.n_q_heads, shape.head_dim), new(n, shape.n_q_heads, shape.head_dim)
         self.k, self.v = new(n, shape.n_kv_heads, shape.head_dim), new(n, shape.n_kv_heads, shape.head_dim)
         self.ws_attn = pages[0].workspace(n)
+        self.ws_tree = pages[0].tree_workspace(*tree) if tree else None
+        self.rows = torch.arange(n, dtype=torch.int32, device=dev)
         # (few rows can need more than many: their reductions are split, and the partial results want room)
         self.ws_tail = torch.empty(max([256] + [api.a3_block_tail_ws_bytes(layout, ffn, m) for m in range(1, n + 1)]), dtype=torch.uint8, device=dev)
         self.logits = torch.empty((n, vocab), dtype=torch.float32, device=dev) if vocab else None
@@ -226,31 +230,106 @@ class DecodeBuffers:
 
 def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor,
                  resid: torch.Tensor, pages: Sequence[api.Pages], row_slot: torch.Tensor, row_pos: torch.Tensor,
-                 row_len: torch.Tensor, bufs: DecodeBuffers, row_req=None, w_vocab=None, stream=None) -> dict:
+                 row_len, bufs: DecodeBuffers, row_req=None, w_vocab=None, stream=None, tree: "TreeRows" = None) -> dict:
     """One new token per row through every block.  ``resid`` [n_req, h] holds the tokens' embeddings and is overwritten by
     the residual stream.  Row i belongs to request ``row_req[i]`` of the pages (None: i); its K and V go to slot
     ``row_slot[i]``, turned to position ``row_pos[i]``, and it sees the slots below ``row_len[i]`` (its own included: row_slot +
     1).  All four are device int32, so that a captured step is replayed with the next values in them; a row whose request
     is -1 is padding: no cache row is written for it and its outputs mean nothing (nor do those of a row whose slot or position
-    lies outside the pages).  ``w_vocab`` [vocab, h]: logits of every row too.  Returns dict(hidden, resid, logits)."""
+    lies outside the pages).  ``w_vocab`` [vocab, h]: logits of every row too.  With ``tree`` the rows are drafted tokens, which see what
+    it says (``row_len`` is not looked at).  Returns dict(hidden, resid, logits)."""
     n, eps, b = layout.n_req, float(shape.rms_eps), bufs
     if len(b.x) < n or (w_vocab is not None and b.logits is None):
         raise ValueError(f"buffers of {len(b.x)} rows{' without logits' if b.logits is None else ''} for a step of {n}")
     if w_vocab is not None and w_vocab.shape[0] != b.logits.shape[1]:
         raise ValueError(f"buffers of {b.logits.shape[1]} logits for a vocabulary of {w_vocab.shape[0]}")
+    if tree is not None and b.ws_tree is None:
+        raise ValueError("buffers without room for trees for a step over trees")
     _fit(pages, len(layers), n if row_req is None else 0, 0, layout, prompt=False)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
         api.a3_selected_qkv_proj(layout, b.x, None, n, lw["wq"], lw["wk"], lw["wv"], q_out=b.q, k_out=b.k, v_out=b.v,
                                  stream=stream, **_bias(lw))
         api.a3_paged_append(pages[l], b.k, b.v, row_req, row_slot, row_pos, n, q=b.q, q_out=b.q, stream=stream)
-        api.a3_paged_attention(pages[l], b.q, row_req, row_len, n, b.out, b.ws_attn, stream=stream)
+        if tree is None:
+            api.a3_paged_attention(pages[l], b.q, row_req, row_len, n, b.out, b.ws_attn, stream=stream)
+        else:
+            api.a3_tree_attention(pages[l], b.q, tree.group_start, tree.group_req, tree.group_len, tree.mask, n, tree.max_rows, b.out,
+                                  b.ws_tree, stream=stream)
         g_next = layers[l + 1]["g_in"] if l + 1 < len(layers) else g_final
         api.a3_block_tail(layout, b.out, None, n, lw["wo"], lw["g_post"], lw["w_gate"], lw["w_up"], lw["w_down"], g_next, eps,
                           resid, b.x, b.ws_tail, stream=stream)
     if w_vocab is not None:
         api.a3_lm_head(layout, b.x, None, n, w_vocab, b.logits, stream=stream)
     return dict(hidden=b.x[:n], resid=resid, logits=b.logits[:n] if w_vocab is not None else None)
+
+
+class TreeRows:
+    """Drafted trees of a batch as one step takes them, device int32 all (a captured step is replayed with the next ones in them).
+    ``parents[g]``: the parent of every token of tree g inside it, -1 for the root in front; ``lens[g]``: the committed slots of its
+    request, ``reqs[g]`` (None: g); ``tokens``: of all rows, the roots' ones are not looked at; ``positions[g]`` of the root (None:
+    lens[g]; after an eviction another); ``max_path``: of the api.TreeAccepted that the step writes."""
+
+    def __init__(self, parents, lens, tokens=None, reqs=None, positions=None, max_rows: int = 0, max_path: int = 16, device="cuda"):
+        i32 = lambda a: torch.as_tensor(np.ascontiguousarray(a, dtype=np.int32), device=device)
+        rows = [len(p) for p in parents]
+        n, self.max_rows = sum(rows), max(rows + [1, max_rows])
+        words = -(-self.max_rows // 32)
+        seen, depth = np.zeros((n, 32 * words), dtype=np.uint8), np.zeros(n, dtype=np.int64)
+        start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int64)
+        for g, tree in enumerate(parents):
+            for j, p in enumerate(tree):
+                if not (p == -1 if j == 0 else 0 <= p < j):
+                    raise ValueError(f"TreeRows: row {j} of tree {g} has parent {p}: row 0 is the root, parents stand in front")
+                row = start[g] + j
+                if j:
+                    seen[row], depth[row] = seen[start[g] + p], depth[start[g] + p] + 1
+                seen[row, j] = 1
+        reqs = np.arange(len(rows)) if reqs is None else np.asarray(reqs)
+        first = np.asarray(lens if positions is None else positions, dtype=np.int64)
+        inside = np.arange(n) - np.repeat(start[:-1], rows)
+        self.n_rows, self.tokens = n, i32(np.zeros(n) if tokens is None else tokens)
+        self.group_start, self.group_req, self.group_len = i32(start), i32(reqs), i32(lens)
+        self.parent = i32(np.concatenate([np.asarray(p, dtype=np.int32) for p in parents] + [np.zeros(0, dtype=np.int32)]))
+        self.mask = i32(np.packbits(seen, axis=1, bitorder="little").view(np.int32)) if n else i32(np.zeros((0, words)))
+        self.path_req = i32(np.repeat(reqs[:, None], max_path, 1))
+        self.row_req, self.row_slot = i32(np.repeat(reqs, rows)), i32(np.repeat(np.asarray(lens), rows) + inside)
+        self.row_pos = i32(np.repeat(first, rows) + depth)
+
+
+def verify_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor, resid: torch.Tensor,
+                 pages: api.PageLayers, tree: TreeRows, bufs: DecodeBuffers, w_vocab: torch.Tensor, out: api.TreeAccepted,
+                 stream=None) -> dict:
+    """Drafted tokens through every block at once, and what of them the model would have said: ``resid`` [tree.n_rows, h] holds the
+    embeddings of the trees' tokens (row 0 of a tree: its request's last certain token, whose K and V are not in the cache yet).
+    ``out`` receives the picked tokens (largest logits), the accepted paths and the tokens behind them; the accepted rows of every
+    layer's cache move to the slots behind the committed ones, so that a request has ``group_len + count`` of them afterwards (what
+    lies behind is free).  ``layout`` has a row for each drafted token.  Returns decode_stack's dict."""
+    if out.max_path != tree.path_req.shape[1]:
+        raise ValueError(f"verify_stack: paths of {out.max_path} for trees of paths of {tree.path_req.shape[1]}")
+    r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, tree.row_slot, tree.row_pos, None, bufs, row_req=tree.row_req,
+                     w_vocab=w_vocab, stream=stream, tree=tree)
+    api.a3_tree_accept(r["logits"], tree.tokens, tree.parent, tree.group_start, tree.group_len, layout.n_req, tree.max_rows, out, stream=stream)
+    api.a3_paged_move(pages, tree.path_req, out.src_slot, tree.path_req, out.dst_slot, None, 1, len(tree.path_req), out.max_path, stream=stream)
+    return r
+
+
+def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tensor]], g_final: torch.Tensor, resid: torch.Tensor,
+               pages: api.PageLayers, row_slot: torch.Tensor, row_pos: torch.Tensor, row_len: torch.Tensor, bufs: DecodeBuffers,
+               w_vocab: torch.Tensor, score: torch.Tensor, first_slot: torch.Tensor, n_slots: torch.Tensor, max_slots: int,
+               out: api.BeamChoice, done=None, end_token: int = 0, stream=None) -> dict:
+    """One step of beam search: a token of every beam through every block, the best continuations of every group of ``out.n_beams`` rows
+    (row = beam = request of the pages), and the caches of the beams that go on in place of the others: beam j of a group takes over
+    slots ``first_slot`` .. + ``n_slots`` (at most ``max_slots``) of row ``out.row[g, j]``; in front of them the beams of a group have the same
+    tokens, in pages of their own or shared.  ``first_slot``, ``n_slots``: device int32 [rows], the latter counting the new token.
+    ``score`` of every row, ``done`` and ``end_token`` as for a3_beam_select; ``out`` has as many best ones as beams.  Returns decode_stack's
+    dict."""
+    if out.n_best != out.n_beams:
+        raise ValueError(f"beam_stack: {out.n_best} continuations for {out.n_beams} beams")
+    r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, row_slot, row_pos, row_len, bufs, w_vocab=w_vocab, stream=stream)
+    api.a3_beam_select(r["logits"], score, done, end_token, out, stream=stream)
+    api.a3_paged_move(pages, out.row, first_slot, bufs.rows, first_slot, n_slots, max_slots, layout.n_req // out.n_beams, out.n_beams, stream=stream)
+    return r
 
 
 def score_tokens(layout: api.Layout, hidden: torch.Tensor, row_idx, n_rows: int, w_vocab: torch.Tensor, tokens,
