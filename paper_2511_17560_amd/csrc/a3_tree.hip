@@ -10,90 +10,688 @@ struct tree_args {
   const int *start, *req, *len, *mask;
   int n_groups, n_rows, max_rows, mask_words;
   float scale;             // of the logits, in units of log 2
+  int shares, tiles, units;          // workgroups; most items of a (group, KV head); a workgroup of the join's columns' four coordinates
+  float *part_o;           // [2 * shares, columns, D] pieces: 2 w the one that began before run w, 2 w + 1 the one that goes on after it
+  float2 *part_ml;         // [2 * shares, columns] (maximum, sum; sum < 0: nothing seen)
+  int4 *cut;               // of run w: the item that goes on after it (group or -1, KV head and item of it, w, its pieces); with few items, of
+  int by_item;             // each: the same, w the run that it begins in
 };
 
-// Rows of a group, first of all rows: none where its bounds are not in order.
-__device__ __forceinline__ int group_rows(const tree_args &a, int g, int &first) {
-  first = a.start[g];
-  const int end = a.start[g + 1];
-  return first < 0 || end > a.n_rows || end < first ? 0 : min(end - first, a.max_rows);
+// The rows of a group are packed with the query heads of a KV head: column m = row * G + head of it.  An item is 16 NB WC columns of one
+// (group, KV head): NB blocks of 16 a wave, WC waves beside each other; the other waves of the four take further slots.  A step of a workgroup
+// is WS SK slots, SK a wave: 32, or 16 with fp32 pages.  The steps of the call, groups first, then KV heads, then items, then slots, are cut
+// into as many runs, equal to one step, as there are workgroups, whatever the lengths are: every workgroup forms the running sum of the
+// groups' steps itself (they live on the device).  An item that ends up whole in one workgroup is finished there; of one that is cut, every
+// workgroup leaves a piece in ws and a second kernel joins them in the order of the slots.
+//
+// Matrix instructions, operands straight from memory to registers: S^T = K Q^T puts 16 columns beside the slots (rows), and O^T = V^T P^T
+// wants of a lane 8 consecutive slots of one coordinate.
+//   - which slot a row of S^T is, is free: row i of block b is slot 8 (i / 4) + 4 b + i % 4, so that the weights a lane (column l16, lane group
+//     lg) gets are those of slots 8 lg .. 8 lg + 7, the P^T operand as it stands
+//   - which coordinate a row of O^T is, is free too: row l16 of block c is coordinate E l16 + c, so that a lane loads E consecutive
+//     coordinates of its 8 slots and the V^T operands are a transposition inside the lane, formed once for all NB blocks of columns
+//   - the weights go in as a sum of two bf16 (three where rows are fp32), so that the only rounding of bf16 size is the output's; each
+//     part but the last is cut off below the weight, so that none is zero or negative and an infinite value stays one
+//   - codes of 8-bit pages are whole numbers that bf16 holds; the scales join the logits and the weights
+// The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float).
+//
+// One slab of registers is enough to have the next one on its way: K of the next is asked for as soon as the products with this one's have
+// read it, V as soon as its operands are formed, so that each is under way for most of a step.  Nothing of that is conditional (a slab that
+// does not exist is read from the pool's start and counts nothing): a wait for V would otherwise have to be one for the next K too.
+//
+// A lane's eight slots of a column are eight bits of the row's mask.  Only slabs that reach behind the committed slots look at it: a slot that
+// is not seen has weight 0.  0 times a value that is not finite would be NaN in the rows that do not see it, so there such values are taken out
+// of the product and, where there are any, added to the rows that see them when the item is put together (its result there is not finite
+// whatever the weights are).
+template <typename T, int D, bool Q8, int NB_, int WC_>
+struct tree_form {
+  static constexpr int NB = NB_, WC = WC_, WS = 4 / WC_;
+  static constexpr bool kF32 = sizeof(T) == 4 && !Q8;          // fp32 matrix instructions
+  static constexpr int SK = kF32 ? 16 : 32;                    // slots of a wave's slab
+  static constexpr int KB = SK / 16;                           // row blocks of S^T
+  static constexpr int kRow = Q8 ? D : D * (int)sizeof(T);     // bytes of a slot
+  static constexpr int NK = kRow / 64;                         // 16-byte loads of a lane and row block: bytes 64 s + 16 lg ..
+  static constexpr int NS = SK / 4;                            // slots whose weights a lane has
+  static constexpr int E = kF32 ? 4 : D / 16, NP = D / (16 * E);   // a lane's coordinates: 16 E j + E l16 .. + E - 1, j < NP
+  static constexpr int kVWords = E * kRow / D / 4;             // 32-bit words of one of them
+  static constexpr int kQParts = Q8 && sizeof(T) == 4 ? 3 : 1, kPParts = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int TC = 16 * NB * WC;                      // columns of an item
+  static constexpr int kStep = WS * SK;
+  static constexpr bool kOnce = WC_ == 1;                      // a cache is read once: nontemporal
+};
+
+// Steps of a group's item, and items of its KV heads (0 steps: nothing of the group is written).
+struct group_work { int first, rows, req, len, end, steps, tiles; };
+template <int STEP, int TC>
+__device__ __forceinline__ group_work work_of(const tree_args &a, int start, int stop, int req, int len) {
+  group_work w;
+  w.first = start;
+  w.rows = start < 0 || stop > a.n_rows || stop < start ? 0 : min(stop - start, a.max_rows);
+  w.req = req;
+  w.len = max(0, min(len, a.p.slots));
+  w.end = (int)min((long long)w.len + w.rows, (long long)a.p.slots);
+  w.steps = w.rows == 0 || req < 0 || req >= a.p.n_req ? 0 : (w.end - 1) / STEP + 1;
+  w.tiles = (w.rows * (a.p.Hq / a.p.Hkv) + TC - 1) / TC;
+  return w;
 }
 
-// One workgroup a row and query head, a wave every fourth slot.
-template <typename T, int D, bool Q8>
-__global__ void __launch_bounds__(256)
+template <class F, typename T, int D, bool Q8>
+__global__ void __launch_bounds__(256, F::NB == 1 || (F::NB == 2 && (sizeof(T) == 2 || D == 64)) ? 2 : 1)
 tree_attention_kernel(tree_args a) {
-  constexpr int E = D / 64;
-  __shared__ float2 ml[4];
-  __shared__ int any[4];
-  __shared__ float os[4][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int g = blockIdx.x / a.max_rows, j = blockIdx.x - g * a.max_rows, h = blockIdx.y, kv = h / (a.p.Hq / a.p.Hkv);
-  int first;
-  const int n = group_rows(a, g, first), req = a.req ? a.req[g] : g;
-  if (j >= n || req < 0 || req >= a.p.n_req) return;
-  const int L = max(0, min(a.len[g], a.p.slots)), end = (int)min((long long)L + n, (long long)a.p.slots);
-  const size_t row = (size_t)first + j, at = (row * a.p.Hq + h) * D + lane * E;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-  bool seen = false;
-#pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = (float)((const T *)a.q)[at + e]; o[e] = 0.f; }
-  const size_t head_bytes = page_head_bytes(Q8 ? A3_PAGES_Q8 : A3_PAGES_PLAIN, sizeof(T), 1 << a.p.page_shift, D);
-  for (int u = wave; u < end; u += 4) {
-    const int t = u - L;
-    if (t >= 0 && !(a.mask ? (a.mask[row * a.mask_words + (t >> 5)] >> (t & 31)) & 1 : t <= j)) continue;
-    const int page = a.p.table[(size_t)req * a.p.max_pages + (u >> a.p.page_shift)], in = u & ((1 << a.p.page_shift) - 1);
-    if (page < 0 || page >= a.p.n_pages) continue;
-    const char *kp = a.p.k_pool + ((size_t)page * a.p.Hkv + kv) * head_bytes, *vp = a.p.v_pool + ((size_t)page * a.p.Hkv + kv) * head_bytes;
-    float k[E], v[E], s = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const size_t c = (size_t)in * D + lane * E + e;
-      if constexpr (Q8) {
-        const size_t sc = ((size_t)D << a.p.page_shift) + 4 * in;
-        k[e] = (float)((const signed char *)kp)[c] * *(const float *)(kp + sc);
-        v[e] = (float)((const signed char *)vp)[c] * *(const float *)(vp + sc);
-      } else {
-        k[e] = (float)((const T *)kp)[c];
-        v[e] = (float)((const T *)vp)[c];
-      }
-      s = fmaf(q[e], k[e], s);
-    }
-    for (int x = 32; x; x >>= 1) s += __shfl_xor(s, x);
-    s *= a.scale;
-    seen = true;
-    const float next = fmaxf(m, s), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
-    const float w = s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - (next == -INFINITY ? 0.f : next));
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * v[e];
-    m = next;
+  constexpr int SK = F::SK, NB = F::NB, WS = F::WS, WC = F::WC, kOS = D + 4;
+  __shared__ int scan[8], found[2];
+  __shared__ float2 ml[4][16];
+  __shared__ int sees[4][16];
+  __shared__ __align__(16) float os[4][16][kOS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, lg = lane >> 4, G = a.p.Hq / a.p.Hkv, Hkv = a.p.Hkv, wc = wave % WC, wsl = wave / WC;
+
+  // ---- this workgroup's run of steps -----------------------------------------------------------------------
+  // Up to 256 groups: one thread a group.  More: the groups' sum first, then blocks of 256 up to the one the run begins in.
+  auto steps_of = [&](int g) {
+    if (g >= a.n_groups) return 0;
+    const group_work w = work_of<F::kStep, F::TC>(a, a.start[g], a.start[g + 1], a.req ? a.req[g] : g, a.len[g]);
+    return w.steps * w.tiles;
+  };
+  int st = steps_of(tid), incl = a3_wave_prefix(st), sum = incl;
+  if (a.n_groups > 256) {
+    int mine = st;
+    for (int g = tid + 256; g < a.n_groups; g += 256) mine += steps_of(g);
+    sum = a3_wave_prefix(mine);
   }
-  if (lane == 0) { ml[wave] = make_float2(m, l); any[wave] = seen; }
-#pragma unroll
-  for (int e = 0; e < E; ++e) os[wave][lane * E + e] = o[e];
+  if (lane == 63) { scan[wave] = sum; scan[4 + wave] = incl; }
   __syncthreads();
-  if (wave != 0) return;
-  float M = -INFINITY, sum = 0.f, y[E] = {};
-  for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w].x);
-  for (int w = 0; w < 4; ++w) {
-    const float f = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
-    sum += ml[w].x == -INFINITY ? ml[w].y : ml[w].y * f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] += ml[w].x == -INFINITY ? os[w][lane * E + e] : os[w][lane * E + e] * f;
+  const int total = (scan[0] + scan[1] + scan[2] + scan[3]) * Hkv;
+  // neighbouring runs, which may read the same slots for other columns, on one of the eight dies (workgroups are dealt out in turn)
+  const int w = a.shares % 8 == 0 ? (int)(blockIdx.x % 8) * (a.shares / 8) + blockIdx.x / 8 : blockIdx.x;
+  const int each = total / a.shares, rest = total - each * a.shares;      // the first `rest` workgroups take one more
+  const int first = w * each + min(w, rest), n_steps = each + (w < rest ? 1 : 0);
+  if (tid == 0 && !a.by_item) a.cut[w].x = -1;
+  if (n_steps == 0) return;
+  for (int g0 = 0, before = 0;;) {                             // before: steps of the groups in front of this block
+    int base = before;
+    for (int i = 0; i < wave; ++i) base += scan[4 + i];
+    const int lo = (base + incl - st) * Hkv, hi = (base + incl) * Hkv;
+    if (first >= lo && first < hi) { found[0] = g0 + tid; found[1] = first - lo; }
+    before += scan[4] + scan[5] + scan[6] + scan[7];
+    if (before * Hkv > first) break;
+    g0 += 256;
+    st = steps_of(g0 + tid);
+    incl = a3_wave_prefix(st);
+    __syncthreads();
+    if (lane == 63) scan[4 + wave] = incl;
+    __syncthreads();
   }
-  const bool some = any[0] | any[1] | any[2] | any[3];
+  __syncthreads();
+
+  // ---- where the workgroup stands: a step of an item (all scalar) --------------------------------------------------
+  struct place { int g, head, tile, step; group_work k; };
+  auto enter = [&](place &p) {
+    p.k = work_of<F::kStep, F::TC>(a, scalar_at(a.start, p.g), scalar_at(a.start, p.g + 1), a.req ? scalar_at(a.req, p.g) : p.g, scalar_at(a.len, p.g));
+  };
+  place now;
+  now.g = __builtin_amdgcn_readfirstlane(found[0]);
+  enter(now);
+  const int inside = __builtin_amdgcn_readfirstlane(found[1]);
+  now.head = inside / (now.k.steps * now.k.tiles);
+  now.tile = (inside - now.head * now.k.steps * now.k.tiles) / now.k.steps;
+  now.step = inside % now.k.steps;
+  auto advance = [&](place &p) {
+    if (++p.step < p.k.steps) return;
+    p.step = 0;
+    if (++p.tile < p.k.tiles) return;
+    p.tile = 0;
+    if (++p.head < Hkv) return;
+    p.head = 0;
+    do {
+      if (++p.g >= a.n_groups) return;                         // (only behind the last step of all)
+      enter(p);
+    } while (p.k.steps == 0);
+  };
+
+  // ---- one slab of one wave in registers ------------------------------------------------------------------
+  const size_t head_bytes = page_head_bytes(Q8 ? A3_PAGES_Q8 : A3_PAGES_PLAIN, sizeof(T), 1 << a.p.page_shift, D);
+  uint32_t koff[F::KB], voff;
 #pragma unroll
-  for (int e = 0; e < E; ++e) ((T *)a.out)[at + e] = (T)(some ? y[e] / sum : 0.f);
+  for (int b = 0; b < F::KB; ++b) koff[b] = (SK == 16 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3)) * F::kRow + 16 * lg;
+  voff = (uint32_t)(F::NS * lg * F::kRow + F::kVWords * 4 * l16);
+  auto slot_of = [&](const place &p) { return p.step * F::kStep + SK * wsl; };
+  uint4 sk[F::KB][F::NK];
+  uint32_t sv[F::NS][F::NP][F::kVWords];
+  f32x4 ks[Q8 ? 2 : 1], vs[Q8 ? 2 : 1];
+  struct where { size_t block; int at, n; };                   // n: its slots up to the tree's end (<= 0: none of them counts)
+  auto find = [&](const place &p, bool more) {
+    const int slot = slot_of(p);
+    where x{0, 0, 0};
+    if (!more || slot >= p.k.end) return x;
+    const int page = scalar_at(a.p.table, (size_t)p.k.req * a.p.max_pages + (slot >> a.p.page_shift));
+    if (page < 0 || page >= a.p.n_pages) return x;
+    x.block = ((size_t)page * Hkv + p.head) * head_bytes;
+    x.at = slot & ((1 << a.p.page_shift) - 1);
+    x.n = p.k.end - slot;
+    return x;
+  };
+  auto load_k = [&](const where &x) {
+    const char *kb = a.p.k_pool + x.block + x.at * F::kRow;
+#pragma unroll
+    for (int b = 0; b < F::KB; ++b)
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i) {
+        const uint4 *at = reinterpret_cast<const uint4 *>(kb + koff[b] + 64 * i);
+        sk[b][i] = F::kOnce ? a3_nt_load(at) : *at;
+      }
+    if constexpr (Q8) {
+      const char *sc = a.p.k_pool + x.block + ((size_t)D << a.p.page_shift) + 4 * x.at + 32 * lg;
+      ks[0] = *reinterpret_cast<const f32x4 *>(sc);
+      ks[1] = *reinterpret_cast<const f32x4 *>(sc + 16);
+    }
+  };
+  auto load_v = [&](const where &x) {
+    const char *vb = a.p.v_pool + x.block + x.at * F::kRow;
+#pragma unroll
+    for (int i = 0; i < F::NS; ++i)
+#pragma unroll
+      for (int j = 0; j < F::NP; ++j) {
+        typedef uint32_t words __attribute__((ext_vector_type(F::kVWords == 1 ? 1 : F::kVWords)));
+        const words *at = reinterpret_cast<const words *>(vb + voff + i * F::kRow + j * 64 * F::kVWords);
+        const words y = F::kOnce ? __builtin_nontemporal_load(at) : *at;
+#pragma unroll
+        for (int u = 0; u < F::kVWords; ++u) sv[i][j][u] = y[u];
+      }
+    if constexpr (Q8) {
+      const char *sc = a.p.v_pool + x.block + ((size_t)D << a.p.page_shift) + 4 * x.at + 32 * lg;
+      vs[0] = *reinterpret_cast<const f32x4 *>(sc);
+      vs[1] = *reinterpret_cast<const f32x4 *>(sc + 16);
+    }
+  };
+
+  // ---- the item's columns: their rows and the queries, operand of S^T ----------------------------------------------------
+  constexpr int NQ = F::kF32 ? F::NK : D / 32;
+  f32x4 qf[F::kF32 ? NB : 1][F::kF32 ? NQ : 1];
+  bf16x8 qb[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kQParts][F::kF32 ? 1 : NQ];
+  int row[NB];                                                 // of the group
+  auto load_queries = [&](const place &p) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      // (columns past the last repeat it: nothing of them is stored)
+      const int m = min(p.tile * F::TC + (wc * NB + nb) * 16 + l16, p.k.rows * G - 1);
+      row[nb] = m / G;
+      const T *q = (const T *)a.q + ((size_t)(p.k.first + row[nb]) * a.p.Hq + p.head * G + (m - row[nb] * G)) * D;
+      if constexpr (F::kF32) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) qf[nb][i] = *reinterpret_cast<const f32x4 *>(q + 16 * i + 4 * lg);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          const T *at = q + (Q8 ? 64 * (i >> 1) + 16 * lg + 8 * (i & 1) : 32 * i + 8 * lg);
+          if constexpr (sizeof(T) == 2) {
+            qb[nb][0][i] = *reinterpret_cast<const bf16x8 *>(at);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {                      // x as the sum of three bf16
+              float x = at[e];
+#pragma unroll
+              for (int k = 0; k < F::kQParts; ++k) {
+                const bf16_t h = a3_f2bf(x);
+                qb[nb][k][i][e] = h;
+                x -= a3_bf2f(h);
+                if (!(fabsf(x) < INFINITY)) x = 0.f;           // an infinity has no remainder
+              }
+            }
+          }
+        }
+      }
+    }
+  };
+
+  // ---- running state of the item --------------------------------------------------------------------------
+  f32x4 o[NB][D / 16];
+  float m[NB], l[NB];
+  int seen;                                                    // bit nb: the lane's column of block nb has seen a slot of the lane's
+  bool odd;                                                    // a value that is not finite was taken out
+  auto clear = [&]() {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[nb][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[nb] = -INFINITY;
+      l[nb] = 0.f;
+    }
+    seen = 0;
+    odd = false;
+  };
+
+  // Bits of the lane's slots (t0 .. t0 + NS - 1 of the tree; committed ones below 0) that row j sees.
+  auto seen_slots = [&](const place &p, int t0, int j) -> uint32_t {
+    constexpr uint32_t kAll = (1u << F::NS) - 1;
+    if (t0 + F::NS <= 0) return kAll;
+    const int top = p.k.end - p.k.len - t0;                    // slots in front of the tree's end
+    uint32_t bits;
+    if (a.mask) {
+      const int lo = max(t0, 0), word = lo >> 5;
+      const int *w = a.mask + (size_t)(p.k.first + j) * a.mask_words;
+      const uint64_t two = (word < a.mask_words ? (uint64_t)(uint32_t)w[word] : 0) | (word + 1 < a.mask_words ? (uint64_t)(uint32_t)w[word + 1] << 32 : 0);
+      bits = (uint32_t)(two >> (lo & 31));
+      if (t0 < 0) bits = (bits << -t0) | ((1u << -t0) - 1);
+    } else {
+      const int n = j + 1 - t0;
+      bits = n >= F::NS ? kAll : n <= 0 ? 0u : (1u << n) - 1;
+    }
+    return bits & (top >= F::NS ? kAll : top <= 0 ? 0u : (1u << top) - 1);
+  };
+
+  // One slab: `cur` is in the registers, `next` is asked for meanwhile.
+  auto work = [&](const where &cur, const where &next, const place &p) {
+    const int t0 = slot_of(p) + F::NS * lg - p.k.len;
+    const bool masked = cur.n < SK || slot_of(p) + SK > p.k.len;     // (uniform)
+    f32x4 acc[NB][F::KB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int b = 0; b < F::KB; ++b) acc[nb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (F::kF32) {
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i) {
+        const f32x4 kf = __builtin_bit_cast(f32x4, sk[0][i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) acc[nb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[nb][i][e], acc[nb][0], 0, 0, 0);
+      }
+    } else if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int b = 0; b < F::KB; ++b) {
+            const uint32_t x[2] = {u ? sk[b][i].z : sk[b][i].x, u ? sk[b][i].w : sk[b][i].y};
+            const bf16x8 kf = codes8(x);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int k = 0; k < F::kQParts; ++k)
+                acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][k][2 * i + u], acc[nb][b], 0, 0, 0);
+          }
+    } else {
+#pragma unroll
+      for (int i = 0; i < F::NK; ++i)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int b = 0; b < F::KB; ++b)
+            acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, sk[b][i]), qb[nb][0][i], acc[nb][b], 0, 0, 0);
+    }
+    if constexpr (Q8) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[nb][b] *= ks[b];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(next);
+    __builtin_amdgcn_sched_barrier(0);
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i) {
+        const bool none = F::NS * lg + i >= cur.n;             // behind the tree: anything
+        if constexpr (Q8) {
+          if (none) vs[i >> 2][i & 3] = 0.f;
+        } else {
+#pragma unroll
+          for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+            for (int u = 0; u < F::kVWords; ++u) {
+              uint32_t x = none ? 0u : sv[i][j][u];
+              if constexpr (sizeof(T) == 4) {
+                if ((x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
+              } else {
+                if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+                if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+              }
+              sv[i][j][u] = x;
+            }
+        }
+      }
+    }
+    // V^T operands
+    bf16x8 vf[F::kF32 ? 1 : D / 16];
+    float vw[F::kF32 ? 4 : 1][F::kF32 ? D / 16 : 1];
+    f32x4 vscale[Q8 ? 2 : 1];
+    if constexpr (F::kF32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) vw[i][c] = __builtin_bit_cast(float, sv[i][c >> 2][c & 3]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (Q8)
+            x[i] = pack_codes((float)(signed char)(sv[2 * i][0][c >> 2] >> 8 * (c & 3)), (float)(signed char)(sv[2 * i + 1][0][c >> 2] >> 8 * (c & 3)));
+          else
+            x[i] = __builtin_amdgcn_perm(sv[2 * i + 1][0][c >> 1], sv[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+        }
+        vf[c] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+      }
+    }
+    if constexpr (Q8) { vscale[0] = vs[0]; vscale[1] = vs[1]; }
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(next);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float w[F::NS];
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i) w[i] = acc[nb][i >> 2][i & 3] * a.scale;
+      uint32_t vis = ~0u;
+      if (masked) {
+        vis = cur.n <= 0 ? 0u : seen_slots(p, t0, row[nb]);
+#pragma unroll
+        for (int i = 0; i < F::NS; ++i)
+          if (!(vis >> i & 1)) w[i] = -INFINITY;
+      }
+      if (vis) seen |= 1 << nb;
+      float top = w[0];
+#pragma unroll
+      for (int i = 1; i < F::NS; ++i) top = fmaxf(top, w[i]);
+      if (__any(top > m[nb] + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float up = fmaxf(m[nb], top), f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - up);
+        m[nb] = up;
+        l[nb] *= f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
+      }
+      const float ref = m[nb] == -INFINITY ? 0.f : m[nb];
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(w[i] - ref);
+        l[nb] += w[i];
+        if constexpr (Q8) w[i] = vis >> i & 1 ? w[i] * vscale[i >> 2][i & 3] : 0.f;
+      }
+      if constexpr (F::kF32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw[i][c], w[i], o[nb][c], 0, 0, 0);
+      } else {
+        bf16x8 pf[F::kPParts];
+#pragma unroll
+        for (int k = 0; k < F::kPParts; ++k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (k == F::kPParts - 1) { pf[k][i] = a3_f2bf(w[i]); continue; }
+            const uint32_t h = __builtin_elementwise_sub_sat(__float_as_uint(w[i]), 1u) & 0xffff0000u;
+            pf[k][i] = __builtin_bit_cast(bf16_t, (unsigned short)(h >> 16));
+            w[i] -= __uint_as_float(h);
+          }
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+          for (int k = 0; k < F::kPParts; ++k) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], pf[k], o[nb][c], 0, 0, 0);
+      }
+    }
+  };
+
+  // Rare: the values that are not finite, of the tree's slots that row j sees, into coordinates d .. d + 3 (of several pieces, each adds them all).
+  auto add_odd = [&](const place &p, int j, int d, f32x4 &sum) {
+    for (int slot = p.k.len; slot < p.k.end; ++slot) {
+      const int page = a.p.table[(size_t)p.k.req * a.p.max_pages + (slot >> a.p.page_shift)], t = slot - p.k.len;
+      if (page < 0 || page >= a.p.n_pages) continue;
+      if (a.mask ? !(a.mask[(size_t)(p.k.first + j) * a.mask_words + (t >> 5)] >> (t & 31) & 1) : t > j) continue;
+      const T *v = (const T *)(a.p.v_pool + ((size_t)page * Hkv + p.head) * head_bytes) + (size_t)(slot & ((1 << a.p.page_shift) - 1)) * D + d;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float x = (float)v[u];
+        if (!(fabsf(x) < INFINITY)) sum[u] += x;
+      }
+    }
+  };
+
+  // ---- an item, or this workgroup's part of one, is done: join the waves that share columns ---------------------------------
+  auto finish = [&](const place &p, bool begins, bool ends) {
+    const bool whole = begins && ends;
+    const int slot = 2 * w + (begins ? 1 : 0);
+    const int some_odd = __any(odd);
+    if (lane == 0) scan[wave] = some_odd;                      // (the sums of steps are not needed any more)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      l[nb] += __shfl_xor(l[nb], 16);
+      l[nb] += __shfl_xor(l[nb], 32);
+      int any = seen >> nb & 1;
+      any |= __shfl_xor(any, 16);
+      any |= __shfl_xor(any, 32);
+      if (lg == 0) { ml[wave][l16] = make_float2(m[nb], l[nb]); sees[wave][l16] = any; }
+      A3_LDS_BARRIER();
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < WS; ++x) top = fmaxf(top, ml[x * WC + wc][l16].x);
+      const float f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - top);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+          for (int c = 0; c < F::E; c += 4) {
+            const int b = j * F::E + c;
+            *reinterpret_cast<f32x4 *>(&os[wave][l16][16 * F::E * j + F::E * (4 * lg + r) + c]) =
+                f32x4{o[nb][b][r], o[nb][b + 1][r], o[nb][b + 2][r], o[nb][b + 3][r]} * f;
+          }
+      A3_LDS_BARRIER();
+      for (int e = tid; e < WC * 16 * (D / 4); e += 256) {
+        const int col = e / (D / 4), d = 4 * (e % (D / 4)), cw = col >> 4, ci = col & 15;
+        const int in = (cw * NB + nb) * 16 + ci, at = p.tile * F::TC + in;   // its number in the item, and among the group's columns
+        if (at >= p.k.rows * G) continue;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float M = -INFINITY, L = 0.f;
+        int some = 0;
+#pragma unroll
+        for (int x = 0; x < WS; ++x) {
+          sum += *reinterpret_cast<const f32x4 *>(&os[x * WC + cw][ci][d]);
+          M = fmaxf(M, ml[x * WC + cw][ci].x);
+          some |= sees[x * WC + cw][ci];
+        }
+#pragma unroll
+        for (int x = 0; x < WS; ++x) {
+          const float2 y = ml[x * WC + cw][ci];
+          L += y.x == -INFINITY ? 0.f : y.y * __builtin_amdgcn_exp2f(y.x - M);
+        }
+        const int j = at / G;
+        if constexpr (!Q8)
+          if (scan[0] | scan[1] | scan[2] | scan[3]) add_odd(p, j, d, sum);
+        if (whole) {
+          typedef T vec4 __attribute__((ext_vector_type(4)));
+          vec4 y;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) y[u] = (T)(some ? sum[u] / L : 0.f);
+          *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D + d) = y;
+        } else {
+          *reinterpret_cast<f32x4 *>(a.part_o + ((size_t)slot * F::TC + in) * D + d) = sum;
+          if (d == 0) a.part_ml[(size_t)slot * F::TC + in] = make_float2(M, some ? L : -1.f);
+        }
+      }
+      A3_LDS_BARRIER();
+    }
+  };
+
+  // ---- the run of steps ------------------------------------------------------------------------------------------
+  place ahead = now;
+  bool begins = now.step == 0;
+  where cur = find(now, true);
+  load_k(cur);
+  load_v(cur);
+  load_queries(now);
+  clear();
+  for (int i = 0; i < n_steps; ++i) {
+    const bool more = i + 1 < n_steps, ends = now.step == now.k.steps - 1;
+    if (more) advance(ahead);
+    const where next = find(ahead, more);
+    work(cur, next, now);
+    cur = next;
+    if (!ends && more) {
+      ++now.step;
+      continue;
+    }
+    finish(now, begins, ends);
+    if (begins && tid == 0) {
+      int pieces = 1;
+      if (!ends) {                                             // goes on in the workgroups behind: how many of them
+        // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+        const int last = first + i + now.k.steps - 1 - now.step, fat = rest * (each + 1);
+        pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+      }
+      if (a.by_item) a.cut[((size_t)now.g * Hkv + now.head) * a.tiles + now.tile] = make_int4(now.g, now.head, w, pieces);
+      else if (!ends) a.cut[w] = make_int4(now.g, now.head | now.tile << 16, w, pieces);
+    }
+    begins = true;
+    clear();
+    if (more) {
+      now = ahead;
+      load_queries(now);
+    }
+  }
+}
+
+// Joins the pieces of an item that is cut, kUnits columns' four coordinates a workgroup: of item blockIdx.x (by_item: few of them), or of
+// the one that goes on after workgroup blockIdx.x.  A thread sums its coordinates over every kth piece, the loads of eight pieces on their
+// way together; then the k partial sums are joined.
+constexpr int kJoinThreads = 256;
+template <typename T, int D, int TC>
+__global__ void __launch_bounds__(kJoinThreads)
+tree_join_kernel(tree_args a) {
+  __shared__ f32x4 os[kJoinThreads];
+  __shared__ float2 mls[kJoinThreads];
+  const int tid = threadIdx.x, G = a.p.Hq / a.p.Hkv, groups = kJoinThreads / a.units;
+  int g, head, tile;
+  if (a.by_item) {
+    g = blockIdx.x / (a.p.Hkv * a.tiles);
+    head = blockIdx.x / a.tiles % a.p.Hkv;
+    tile = blockIdx.x % a.tiles;
+  } else {
+    const int4 c = a.cut[blockIdx.x];
+    if (c.x < 0) return;
+    g = c.x;
+    head = c.y & 0xffff;
+    tile = c.y >> 16;
+  }
+  const group_work k = work_of<1, TC>(a, a.start[g], a.start[g + 1], a.req ? a.req[g] : g, a.len[g]);
+  if (k.steps == 0 || tile >= k.tiles) return;                 // (no such item: `cut` says nothing)
+  const int4 c = a.cut[blockIdx.x];
+  const int w = c.z, n = c.w;
+  if (n < 2) return;
+  const int gr = tid / a.units, v = tid - gr * a.units, u = blockIdx.y * a.units + v, in = u / (D / 4), at = tile * TC + in;
+  const bool on = gr < groups && in < TC && at < k.rows * G;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = -1.f;                               // l < 0: nothing seen
+  auto take = [](f32x4 &o, float &m, float &l, const f32x4 &x, float2 ml, float top) {
+    if (ml.y < 0.f) return;
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+    o += x * f;                                                // (a piece whose logits are all NaN has no maximum, and its NaN stays one times 0)
+    l = (l < 0.f ? 0.f : l) + ml.y * f;
+  };
+  constexpr int K = 8;
+  if (on)
+    for (int i = gr; i < n; i += K * groups) {
+      f32x4 x[K];
+      float2 ml[K];
+#pragma unroll
+      for (int q = 0; q < K; ++q) {
+        const int p = min(i + q * groups, n - 1), slot = p == 0 ? 2 * w + 1 : 2 * (w + p);
+        x[q] = *reinterpret_cast<const f32x4 *>(a.part_o + (size_t)slot * TC * D + 4 * u);
+        ml[q] = a.part_ml[(size_t)slot * TC + in];
+      }
+      float top = m;
+#pragma unroll
+      for (int q = 0; q < K; ++q) {
+        if (i + q * groups >= n) ml[q] = make_float2(-INFINITY, -1.f);
+        top = fmaxf(top, ml[q].x);
+      }
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      if (!(l < 0.f)) { o *= f; l *= f; }
+      m = top;
+#pragma unroll
+      for (int q = 0; q < K; ++q) take(o, m, l, x[q], ml[q], top);
+    }
+  os[tid] = o;
+  mls[tid] = make_float2(m, l);
+  __syncthreads();
+  if (gr != 0 || !on) return;
+  for (int q = 1; q < groups; ++q) m = fmaxf(m, mls[q * a.units + v].x);
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  l = -1.f;
+  for (int q = 0; q < groups; ++q) take(o, m, l, os[q * a.units + v], mls[q * a.units + v], m);
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  vec4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (T)(l < 0.f ? 0.f : o[e] / l);
+  const int j = at / G;
+  *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(k.first + j) * a.p.Hq + head * G + (at - j * G)) * D + 4 * (u % (D / 4))) = y;
 }
 
 constexpr int kMaxRows = 1024;
+
+// What a call runs in: blocks of columns a wave, waves beside each other, workgroups at most.
+struct tree_shape { int nb, wc, wgs; };
+tree_shape shape_of(const a3_pages *P, int max_rows) {
+  const int cols = max_rows * (P->n_q_heads / P->n_kv_heads);
+  if (cols <= 16) return {1, 1, 512};
+  if (cols <= 32) return {2, 1, P->dtype == A3_F32 && P->head_dim == 128 ? 256 : 512};
+  if (P->dtype == A3_F32) return {2, cols <= 64 ? 2 : 4, P->head_dim == 64 ? 512 : 256};
+  return cols <= 64 ? tree_shape{4, 1, 256} : cols <= 128 ? tree_shape{4, 2, 256} : tree_shape{4, 4, 256};
+}
+template <typename T, int D, bool Q8, class F>
+void with_shape(tree_shape s, F f) {
+  if (s.nb == 1) f(tree_form<T, D, Q8, 1, 1>{});
+  else if (s.nb == 2 && s.wc == 1) f(tree_form<T, D, Q8, 2, 1>{});
+  else if constexpr (sizeof(T) == 4) {
+    if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2>{});
+    else f(tree_form<T, D, Q8, 2, 4>{});
+  } else {
+    if (s.wc == 1) f(tree_form<T, D, Q8, 4, 1>{});
+    else if (s.wc == 2) f(tree_form<T, D, Q8, 4, 2>{});
+    else f(tree_form<T, D, Q8, 4, 4>{});
+  }
+}
+struct tree_plan { tree_shape s; int tc, tiles, shares; long long items, steps; };
+tree_plan plan_of(const a3_pages *P, int n_groups, int max_rows) {
+  tree_plan p;
+  p.s = shape_of(P, max_rows);
+  p.tc = 16 * p.s.nb * p.s.wc;
+  p.tiles = (max_rows * (P->n_q_heads / P->n_kv_heads) + p.tc - 1) / p.tc;
+  const int step = 4 / p.s.wc * (P->dtype == A3_F32 && P->format == A3_PAGES_PLAIN ? 16 : 32);
+  p.items = (long long)n_groups * P->n_kv_heads * p.tiles;
+  p.steps = ((long long)P->max_pages * P->page_size + step - 1) / step * p.items;
+  p.shares = p.steps < p.s.wgs ? (int)p.steps : p.s.wgs;
+  return p;
+}
+// workspace; base NULL: only its size
+size_t tree_ws(const a3_pages *P, const tree_plan &p, void *base, tree_args *a) {
+  a3_ws_cursor cur(base, 0);
+  const size_t n = (size_t)p.shares;
+  float *o = (float *)cur.take(2 * n * p.tc * P->head_dim * sizeof(float));
+  float2 *ml = (float2 *)cur.take(2 * n * p.tc * sizeof(float2));
+  int4 *cut = (int4 *)cur.take(n * sizeof(int4));
+  if (a) { a->part_o = o; a->part_ml = ml; a->cut = cut; }
+  return cur.off;
+}
 
 }  // namespace
 
 extern "C" size_t a3_tree_attention_ws_bytes(const a3_pages *P, int n_groups, int max_rows) {
   if (check_pages(P, "a3_tree_attention_ws_bytes", false) != A3_OK || n_groups < 0 || max_rows < 1 || max_rows > kMaxRows) return 0;
-  return 256;
+  size_t most = 0;                                             // (fewer rows may take another shape, fewer groups fewer workgroups)
+  const int G = P->n_q_heads / P->n_kv_heads;
+  for (int cols : {16, 32, 64, 128, kMaxRows * 16}) {
+    const int rows = cols / G < max_rows ? cols / G : max_rows;
+    if (rows < 1) continue;
+    const size_t n = tree_ws(P, plan_of(P, n_groups > 0 ? n_groups : 1, rows), nullptr, nullptr);
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 extern "C" a3_status a3_tree_attention(const a3_pages *P, const void *q, int n_groups, const int *group_start, const int *group_req,
@@ -116,10 +714,22 @@ extern "C" a3_status a3_tree_attention(const a3_pages *P, const void *q, int n_g
              ws ? ws_bytes : 0, need);
   tree_args a{args_of(P), q, out, group_start, group_req, group_len, mask, n_groups, n_rows, max_rows, mask_words,
               (float)((P->sm_scale != 0.f ? (double)P->sm_scale : 1.0 / sqrt((double)P->head_dim)) * 1.4426950408889634074)};
-  A3_REQUIRE((long long)n_groups * max_rows < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_tree_attention: too many groups");
+  const tree_plan plan = plan_of(P, n_groups, max_rows);
+  A3_REQUIRE(plan.steps < (1LL << 31) - 1024 && (long long)n_rows * P->n_q_heads < (1LL << 31), A3_ERR_UNSUPPORTED,
+             "a3_tree_attention: too many groups for a page table of this width");
+  a.shares = plan.shares;
+  a.tiles = plan.tiles;
+  a.by_item = plan.items <= plan.shares;
+  tree_ws(P, plan, ws, &a);
+  a.units = 64;
+  const dim3 join((unsigned)(a.by_item ? plan.items : plan.shares), (unsigned)(plan.tc * (P->head_dim / 4) / a.units));
   with_format(P, [&](auto elem, auto d, auto q8) {
-    hipLaunchKernelGGL((tree_attention_kernel<decltype(elem), d.value, q8.value>), dim3((unsigned)(n_groups * max_rows), (unsigned)P->n_q_heads),
-                       dim3(256), 0, (hipStream_t)stream, a);
+    typedef decltype(elem) T;
+    with_shape<T, d.value, q8.value>(plan.s, [&](auto form) {
+      typedef decltype(form) F;
+      hipLaunchKernelGGL((tree_attention_kernel<F, T, d.value, q8.value>), dim3((unsigned)plan.shares), dim3(256), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((tree_join_kernel<T, d.value, F::TC>), join, dim3(kJoinThreads), 0, (hipStream_t)stream, a);
+    });
   });
   A3_CHECK_LAUNCH("a3_tree_attention");
   return A3_OK;
