@@ -1,20 +1,11 @@
 // What follows several candidates of a request: the accepted path of a drafted tree, cache rows moved to other slots, and the best
 // continuations of beams.
+#include "a3_choose.h"
 #include "a3_pages.h"
 
 namespace {
 
 constexpr int kMaxRows = 1024, kMaxPath = 64, kMaxSet = 64, kMaxBeams = 64, kMaxBest = 64;
-
-// Order of logits as one number: larger, then lower index; -0 equals 0, NaN below everything.
-__device__ __forceinline__ unsigned long long logit_key(float x, int v) {
-  const uint32_t b = __float_as_uint(x + 0.f), o = x != x ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return ((unsigned long long)o << 32) | (uint32_t)~v;
-}
-__device__ __forceinline__ unsigned long long wave_max_key(unsigned long long k) {
-  for (int o = 32; o; o >>= 1) { const unsigned long long x = __shfl_xor(k, o); k = x > k ? x : k; }
-  return k;
-}
 
 // ---------------------------------------------------------------------------------------
 // the accepted path
@@ -27,58 +18,139 @@ struct accept_args {
   const int *tokens, *parent, *start, *len;
   int n_groups, n_rows, max_rows, max_path;
   int *count, *path, *next, *src, *dst;
+  int slices;                          // of a row
+  unsigned long long *part;            // [n_rows, slices] largest keys
 };
 
-template <typename T>
-__global__ void __launch_bounds__(256)
-pick_kernel(accept_args a) {
-  __shared__ unsigned long long best[4];
-  const int tid = threadIdx.x;
-  const T *x = (const T *)a.x + (size_t)blockIdx.x * a.ld;
-  unsigned long long k = 0;
-  for (int v = tid; v < a.vocab; v += 256) { const unsigned long long y = logit_key((float)x[v], v); k = y > k ? y : k; }
-  k = wave_max_key(k);
-  if ((tid & 63) == 0) best[tid >> 6] = k;
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < 4; ++w) k = best[w] > k ? best[w] : k;
-    a.picked[blockIdx.x] = (int)~(uint32_t)k;
-  }
+// The largest key of 2^k neighbouring lanes, in all of them.
+__device__ __forceinline__ unsigned long long max_of_lanes(unsigned long long k, int lanes) {
+  for (int o = lanes >> 1; o; o >>= 1) { const unsigned long long x = __shfl_xor(k, o); k = x > k ? x : k; }
+  return k;
 }
 
-// One wave a group: every step looks for the first child of the last row among 64 rows at a time.
-__global__ void __launch_bounds__(64)
+// The largest logit of a slice of a row.  A thread keeps the maximum of its values and the chunk of 32 that it came from: one instruction a
+// value, so that reading is all that counts.  Its key is found in that chunk afterwards.  (A maximum of -inf says nothing: all may be NaN.)
+template <typename T>
+__global__ void __launch_bounds__(kLpThreads)
+pick_kernel(accept_args a) {
+  typedef lp_row<T> R;
+  constexpr int V = R::V, U = R::U, kChunk = R::kChunk;
+  __shared__ unsigned long long best[4];
+  const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x;
+  R r;
+  r.x = (const T *)a.x + (size_t)row * a.ld;
+  r.vocab = a.vocab;
+  r.skew = (int)(((uintptr_t)r.x & 15) / sizeof(T));
+  const int n_vec = (int)(((long long)a.vocab + r.skew + V - 1) / V), per = n_vec / a.slices, rest = n_vec - per * a.slices;
+  r.v0 = slice * per + min(slice, rest);
+  r.v1 = r.v0 + per + (slice < rest ? 1 : 0);
+  float m = -INFINITY;
+  int from = -1;
+  for (int c = r.v0; c < r.v1; c += kChunk) {
+    typename R::vec_t raw[U];
+    if (c * V >= r.skew && c + kChunk <= r.v1 && (long long)(c + kChunk) * V - r.skew <= r.vocab) {
+      const T *x = r.x + ((long long)c * V - r.skew);
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const typename R::vec_t *>(x + (u * kLpThreads + tid) * V);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = r.vec(c + u * kLpThreads + tid);
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kLpValues; ++i) top = fmaxf(top, (float)raw[i / V][i % V]);
+    if (top > m) { m = top; from = c; }
+  }
+  unsigned long long k = 0;
+  const bool all = __syncthreads_and(m == -INFINITY);          // nothing but -inf and NaN: every value is looked at
+  for (int c = all ? r.v0 : from; c >= 0 && c < r.v1; c = all ? c + kChunk : -1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = c + u * kLpThreads + tid;
+      const typename R::vec_t raw = r.vec(v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) { const unsigned long long x = r.key(v, i, (float)raw[i]); k = x > k ? x : k; }
+    }
+  k = max_of_lanes(k, 64);
+  if ((tid & 63) == 0) best[tid >> 6] = k;
+  __syncthreads();
+  if (tid != 0) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) k = best[w] > k ? best[w] : k;
+  a.part[blockIdx.x] = k;
+}
+
+// Workgroup g < n_groups follows the tree of group g; the others write the picks of 64 rows each (rows may be in no group).
+// A chain of latencies: the slices' keys and the tree in one round trip, then a look at LDS for every row of the path.
+__global__ void __launch_bounds__(256)
 follow_kernel(accept_args a) {
-  const int g = blockIdx.x, lane = threadIdx.x;
-  const int first = a.start[g], end = a.start[g + 1];
+  __shared__ int picked[kMaxRows], parent[kMaxRows], token[kMaxRows];
+  const int tid = threadIdx.x, g = blockIdx.x;
+  // picks of rows first .. first + n - 1 into `to`: as many lanes a row as there are threads for
+  auto join = [&](int first, int n, int *to) {
+    int lanes = 64;
+    while (lanes > 1 && lanes * n > 256) lanes >>= 1;
+    for (int r0 = 0; r0 < n; r0 += 256 / lanes) {
+      const int r = r0 + tid / lanes;
+      unsigned long long k = 0;
+      if (r < n) {
+        const unsigned long long *p = a.part + (size_t)(first + r) * a.slices;
+#pragma unroll 4
+        for (int s = tid % lanes; s < a.slices; s += lanes) k = p[s] > k ? p[s] : k;
+      }
+      k = max_of_lanes(k, lanes);
+      if (r < n && tid % lanes == 0) to[r] = (int)~(uint32_t)k;
+    }
+  };
+  if (g >= a.n_groups) {
+    const int first = (g - a.n_groups) * 64;
+    join(first, min(64, a.n_rows - first), a.picked + first);
+    return;
+  }
+  const int first = a.start[g], end = a.start[g + 1], L = a.len ? a.len[g] : 0;
   const int n = first < 0 || end > a.n_rows || end < first ? 0 : min(end - first, a.max_rows);
+  for (int i = tid; i < n; i += 256) {
+    parent[i] = a.parent[first + i];
+    token[i] = a.tokens[first + i];
+    if (!a.x) picked[i] = a.picked[first + i];
+  }
+  if (a.x) join(first, n, picked);
+  __syncthreads();
+  if (tid >= 64) return;
   int mine = -1, count = 0, last = 0;                          // lane m keeps path[m]
   while (n > 0) {
-    if (lane == count) mine = last;
+    if (tid == count) mine = last;
     if (++count == a.max_path) break;
-    const int tok = a.picked[first + last];
+    const int tok = picked[last];
     int child = -1;
     for (int c0 = last + 1; c0 < n && child < 0; c0 += 64) {
-      const int c = c0 + lane;
-      const unsigned long long hit = __ballot(c < n && a.parent[first + min(c, n - 1)] == last && a.tokens[first + min(c, n - 1)] == tok);
+      const int c = min(c0 + tid, n - 1);
+      const unsigned long long hit = __ballot(c0 + tid < n && parent[c] == last && token[c] == tok);
       if (hit) child = c0 + __builtin_ctzll(hit);
     }
     if (child < 0) break;
     last = child;
   }
-  if (lane == 0) {
+  if (tid == 0) {
     a.count[g] = count;
-    a.next[g] = n > 0 ? a.picked[first + last] : -1;
+    a.next[g] = n > 0 ? picked[last] : -1;
   }
-  if (lane < a.max_path) {
-    const size_t i = (size_t)g * a.max_path + lane;
-    a.path[i] = lane < count ? mine : -1;
+  if (tid < a.max_path) {
+    const size_t i = (size_t)g * a.max_path + tid;
+    a.path[i] = tid < count ? mine : -1;
     if (a.src) {
-      const int L = a.len[g];
-      a.src[i] = lane < count ? L + mine : -1;
-      a.dst[i] = lane < count ? L + lane : -1;
+      a.src[i] = tid < count ? L + mine : -1;
+      a.dst[i] = tid < count ? L + tid : -1;
     }
   }
+}
+
+// Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of no less than a vector a thread.
+constexpr int kPickPieces = 2048;
+int pick_slices(int n_rows, int vocab, int elem) {
+  const int by_rows = n_rows >= kPickPieces ? 1 : (kPickPieces + n_rows - 1) / n_rows;
+  const long long by_size = (long long)vocab * elem / (16 * kLpThreads);
+  return by_size < 1 ? 1 : by_size < by_rows ? (int)by_size : by_rows < 128 ? by_rows : 128;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -90,127 +162,258 @@ struct move_args {
   char *pools[2 * kLayersAtOnce];      // K and V of every layer
   const int *src_req, *src_slot, *dst_req, *dst_slot, *n_slots;
   int max_slots, set_size, row_bytes, q8;
+  int row_shift, slot_shift, groups;   // a workgroup: 2^row_shift vectors of a row, 2^slot_shift slots, 256 >> both KV heads; groups of those
   size_t head_bytes;
 };
 
-__device__ __forceinline__ long long slot_of(const pages_args &p, int req, long long slot) {
-  if (req < 0 || req >= p.n_req || slot < 0 || slot >= p.slots) return -1;
-  const int page = p.table[(size_t)req * p.max_pages + (slot >> p.page_shift)];
-  return page < 0 || page >= p.n_pages ? -1 : ((long long)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1));
+// The physical slot of a request's, -1 where there is none.  (Everything is looked up, whether it is needed or not: the moves of a set are
+// on their way together.)
+__device__ __forceinline__ long long place_of(const pages_args &p, int req, int first, int o) {
+  const long long slot = (long long)first + o;
+  const bool in = req >= 0 && req < p.n_req && first >= 0 && slot < p.slots;
+  const int page = p.table[in ? (size_t)req * p.max_pages + (size_t)(slot >> p.page_shift) : 0];
+  return in && page >= 0 && page < p.n_pages ? ((long long)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1)) : -1;
 }
 
-// A thread has four bytes of one KV head at one o, of all moves of its set: it reads them all, then writes them all.
+// A thread has 16 bytes of one KV head at one slot o of the runs, of all N moves of its set: it reads them all, then writes them all, and no
+// other thread touches what it does, so that a set needs neither a barrier nor a copy in between.  8-bit pages: then the scales, four bytes
+// a slot.  Bound by memory (reading and writing the rows that change their place).
 template <int N>
 __global__ void __launch_bounds__(256)
 move_kernel(move_args a) {
-  const int set = blockIdx.y, words = a.row_bytes / 4 + a.q8, per_o = a.p.Hkv * words;
-  char *pool = a.pools[blockIdx.z];
-  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (long long)a.max_slots * per_o; u += (long long)gridDim.x * 256) {
-    const int o = (int)(u / per_o), rest = (int)(u - (long long)o * per_o), h = rest / words, c = rest - h * words;
-    auto where = [&](long long at) {
-      const long long page = at >> a.p.page_shift, in = at & ((1 << a.p.page_shift) - 1);
-      return ((size_t)page * a.p.Hkv + h) * a.head_bytes + (4 * c < a.row_bytes ? in * a.row_bytes + 4 * c : ((size_t)a.row_bytes << a.p.page_shift) + 4 * in);
-    };
-    uint32_t x[N];
-    long long to[N];
+  const int set = blockIdx.y, tid = threadIdx.x, pool_no = blockIdx.z / a.groups, group = blockIdx.z - pool_no * a.groups;
+  char *pool = a.pools[pool_no];
+  struct one { int from, to, n, sr, dr; };
+  __shared__ one list[N];
+  if (tid < N) {
+    const size_t i = (size_t)set * a.set_size + min(tid, a.set_size - 1);
+    list[tid] = {a.src_slot[i], a.dst_slot[i], tid < a.set_size ? min(a.n_slots ? a.n_slots[i] : 1, a.max_slots) : 0, a.src_req ? a.src_req[i] : set,
+                 a.dst_req ? a.dst_req[i] : set};
+  }
+  __syncthreads();
+  int most = 0;
+#pragma unroll 8
+  for (int m = 0; m < N; ++m) most = max(most, list[m].n);
+  // Moves words W of KV head h at slot o: the lane's `at` bytes into the slot's `width` bytes, `begin` bytes into the head's page.
+  auto move = [&](auto word, int o, int h, size_t begin, int width, int at) {
+    typedef decltype(word) W;
+    W x[N];
+    long long dst[N];
 #pragma unroll
     for (int m = 0; m < N; ++m) {
-      to[m] = -1;
-      if (m >= a.set_size) continue;
-      const int i = set * a.set_size + m;
-      if (o >= (a.n_slots ? a.n_slots[i] : 1) || a.src_slot[i] < 0 || a.dst_slot[i] < 0) continue;
-      const long long from = slot_of(a.p, a.src_req ? a.src_req[i] : set, (long long)a.src_slot[i] + o);
-      to[m] = slot_of(a.p, a.dst_req ? a.dst_req[i] : set, (long long)a.dst_slot[i] + o);
-      if (from < 0 || from == to[m]) to[m] = -1;
-      if (to[m] >= 0) x[m] = *reinterpret_cast<const uint32_t *>(pool + where(from));
+      const one l = list[m];
+      const long long from = place_of(a.p, l.sr, l.from, o), to = place_of(a.p, l.dr, l.to, o);
+      const bool on = o < l.n && from >= 0 && to >= 0 && from != to && h < a.p.Hkv;
+      auto where = [&](long long place) {
+        return (long long)(((size_t)(place >> a.p.page_shift) * a.p.Hkv + h) * a.head_bytes + begin +
+                           (size_t)(place & ((1 << a.p.page_shift) - 1)) * width + at);
+      };
+      x[m] = *reinterpret_cast<const W *>(pool + (on ? where(from) : 0));
+      dst[m] = on ? where(to) : -1;
     }
 #pragma unroll
     for (int m = 0; m < N; ++m)
-      if (to[m] >= 0) *reinterpret_cast<uint32_t *>(pool + where(to[m])) = x[m];
+      if (dst[m] >= 0) *reinterpret_cast<W *>(pool + dst[m]) = x[m];
+  };
+  const int heads = 256 >> (a.row_shift + a.slot_shift), slots = 1 << a.slot_shift;
+  const int c = tid & ((1 << a.row_shift) - 1), so = (tid >> a.row_shift) & (slots - 1), h = group * heads + (tid >> (a.row_shift + a.slot_shift));
+  for (int o0 = blockIdx.x * slots; o0 < most; o0 += gridDim.x * slots) {
+    move(a3_u32x4{}, o0 + so, h, 0, a.row_bytes, 16 * c);
+    if (a.q8 && tid < slots * heads) move(uint32_t{}, o0 + (tid & (slots - 1)), group * heads + (tid >> a.slot_shift), (size_t)a.row_bytes << a.p.page_shift, 4, 0);
   }
 }
 
 // ---------------------------------------------------------------------------------------
 // beams
 // ---------------------------------------------------------------------------------------
+// A workgroup reads a row, or a slice of one, as the log probabilities do (a3_logits.hip): maximum and sum of a thread's own values, the
+// maxima of its chunks of 32 noted, and the best n_best values chosen when all have been read.  Its vectors lie as the row stands, wherever
+// that starts, so that beams that are the same have the same sums.  A chunk's 32 exponentials are summed in float, chunks in double.
+// A second kernel, one workgroup a group, makes worths of its lists (one of every slice of every beam, best first) in double and puts
+// them together: the n_best-th of the lists' heads (or of their first few, where there are fewer lists) bounds what can be among the best,
+// what reaches it is gathered, at most n_best values of n_best lists, and ranked by counting.
 struct beam_args {
   const void *x;
   long long ld;
-  int vocab, n_beams, n_best, end;
+  int vocab, n_beams, n_best, end, slices;
   const float *score;
   const int *done;
   float *best_score;
   int *best_row, *best_token;
-  double *base;            // [rows] score - m - log Z: what a logit is added to; -inf: the beam goes on with nothing
+  double2 *part;                       // [rows, slices] maximum and sum of a slice
+  unsigned long long *part_top;        // [rows, slices, n_best] its best values, best first (0: none)
 };
 
 template <typename T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kLpThreads)
 beam_row_kernel(beam_args a) {
-  __shared__ float top[4];
+  typedef lp_row<T, true> R;
+  constexpr int V = R::V, U = R::U, kChunk = R::kChunk;
+  __shared__ lp_shared s;
+  __shared__ float noted[kLpChunks][kLpThreads];
   __shared__ double sums[4];
-  const int row = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
-  const T *x = (const T *)a.x + (size_t)row * a.ld;
+  const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x;
+  if (a.done && a.done[row]) return;                           // (its logits are not looked at, nor what would be left of them)
+  R r;
+  r.x = (const T *)a.x + (size_t)row * a.ld;
+  r.vocab = a.vocab;
+  r.skew = 0;
+  const int n_vec = (a.vocab + V - 1) / V, per = n_vec / a.slices, rest = n_vec - per * a.slices;
+  r.v0 = slice * per + min(slice, rest);
+  r.v1 = r.v0 + per + (slice < rest ? 1 : 0);
+  typename R::vec_t raw[U];
+  auto load = [&](int c) {
+    if (c + kChunk <= r.v1 && (long long)(c + kChunk) * V <= r.vocab) {
+      const T *x = r.x + (long long)c * V;
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const typename R::vec_any *>(x + (u * kLpThreads + tid) * V);
+      return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = r.vec(c + u * kLpThreads + tid);
+  };
+  load(r.v0);
+  for (int j = tid; j < a.n_best; j += kLpThreads) s.list[j] = 0;
   float m = -INFINITY;
-  bool nan = false;
-  for (int v = tid; v < a.vocab; v += 256) { const float y = (float)x[v]; m = fmaxf(m, y); nan |= y != y; }
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((tid & 63) == 0) top[wave] = m;
-  nan = __syncthreads_or(nan);
-  m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   double z = 0.0;
-  for (int v = tid; v < a.vocab; v += 256) z += (double)expf((float)x[v] - m);
+  for (int g0 = r.v0; g0 < r.v1; g0 += kLpChunks * kChunk) {   // chunks between two choices of the best
+    const int g1 = min(r.v1, g0 + kLpChunks * kChunk);
+    float most = -INFINITY, second = -INFINITY;
+    for (int c = g0; c < g1; c += kChunk) {
+      float y[kLpValues];
+#pragma unroll
+      for (int i = 0; i < kLpValues; ++i) y[i] = (float)raw[i / V][i % V];
+      if (c + kChunk < r.v1) load(c + kChunk);                 // on its way while this chunk is worked on
+      float top = fmaxf(-INFINITY, y[0]), half = fmaxf(-INFINITY, y[1]);   // (halves of nothing but NaN: -inf)
+#pragma unroll
+      for (int i = 2; i < kLpValues; i += 2) { top = fmaxf(top, y[i]); half = fmaxf(half, y[i + 1]); }
+      second = fmaxf(second, fmaxf(fminf(top, half), fminf(most, fmaxf(top, half))));
+      top = fmaxf(top, half);
+      noted[(c - g0) / kChunk][tid] = top;
+      most = fmaxf(most, top);
+      if (top > m) {
+        z *= (double)__builtin_amdgcn_exp2f(lp_shift(m, top));
+        m = top;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kLpValues; ++i) sum[i & 3] += __builtin_amdgcn_exp2f((y[i] - ref) * kLog2e);
+      z += (double)((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    }
+    __syncthreads();                                           // (the list: cleared, or of the last choice)
+    lp_choose(s, r, noted, a.n_best, g0, g1, g0 + tid >= g1 || (most == -INFINITY && z != z) ? 0u : top_order(most),
+              second == -INFINITY ? 0u : top_order(second));
+  }
+  const float mw = wave_max(m);
+  z *= (double)__builtin_amdgcn_exp2f(lp_shift(m, mw));
   for (int o = 32; o; o >>= 1) z += __shfl_xor(z, o);
-  if ((tid & 63) == 0) sums[wave] = z;
   __syncthreads();
-  if (tid != 0) return;
-  const float s = a.score[row];
-  const bool on = !nan && m > -INFINITY && m < INFINITY && s > -INFINITY && s < INFINITY;
-  a.base[row] = on ? (double)s - (double)m - log(sums[0] + sums[1] + sums[2] + sums[3]) : -INFINITY;
+  if ((tid & 63) == 0) { s.red[tid >> 6][0] = mw; sums[tid >> 6] = z; }
+  __syncthreads();
+  if (tid == 0) {
+    const float top = fmaxf(fmaxf(s.red[0][0], s.red[1][0]), fmaxf(s.red[2][0], s.red[3][0]));
+    double all = 0.0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) all += sums[w] * (double)__builtin_amdgcn_exp2f(lp_shift(s.red[w][0], top));
+    a.part[blockIdx.x] = make_double2((double)top, all);
+  }
+  for (int j = tid; j < a.n_best; j += kLpThreads) a.part_top[(size_t)blockIdx.x * a.n_best + j] = s.list[j];
 }
 
-template <typename T>
-__global__ void __launch_bounds__(1024)
-beam_choose_kernel(beam_args a) {
-  __shared__ double value[16];
-  __shared__ unsigned long long where[16];
-  const int g = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
-  double last = INFINITY;
-  unsigned long long at = 0;
-  for (int j = 0; j < a.n_best; ++j) {
-    double v = -INFINITY;
-    unsigned long long w = ~0ull;
-    auto offer = [&](double y, unsigned long long i) {
-      if (y > -INFINITY && (y < last || (y == last && i > at)) && (y > v || (y == v && i < w))) { v = y; w = i; }
-    };
-    for (int b = 0; b < a.n_beams; ++b) {
-      const int row = g * a.n_beams + b;
-      if (a.done && a.done[row]) {
-        const float s = a.score[row];
-        if (tid == 0 && s < INFINITY) offer((double)s, ((unsigned long long)b << 32) | (uint32_t)a.end);
-        continue;
-      }
-      const double base = a.base[row];
-      const T *x = (const T *)a.x + (size_t)row * a.ld;
-      if (base > -INFINITY)
-        for (int t = tid; t < a.vocab; t += 1024) offer(base + (double)(float)x[t], ((unsigned long long)b << 32) | (uint32_t)t);
+// Larger worth, then lower beam, then lower token; worth -inf: no candidate.
+struct candidate { double worth; unsigned long long id; };
+__device__ __forceinline__ bool before(const candidate &a, const candidate &b) { return a.worth > b.worth || (a.worth == b.worth && a.id < b.id); }
+
+constexpr int kBeamLists = 512, kBeamHeads = kBeamLists + kMaxBest;
+__global__ void __launch_bounds__(256)
+beam_join_kernel(beam_args a) {
+  extern __shared__ candidate gathered[];                      // [n_best * n_best]
+  __shared__ candidate head[kBeamHeads], bound;
+  __shared__ double base[kMaxBeams];
+  __shared__ unsigned char kind[kMaxBeams];                    // 0: no candidates, 1: logits, 2: has ended
+  __shared__ int count;
+  const int g = blockIdx.x, tid = threadIdx.x, lists = a.n_beams * a.slices, first = g * a.n_beams;
+  // worth of a logit: base + x
+  for (int b = tid; b < a.n_beams; b += 256) {
+    const float s = a.score[first + b];
+    const bool ended = a.done && a.done[first + b];
+    int k = !(fabsf(s) < INFINITY) ? 0 : ended ? 2 : 1;
+    double M = -INFINITY, Z = 0.0;
+    if (k == 1) {
+      const double2 *p = a.part + (size_t)(first + b) * a.slices;
+      for (int i = 0; i < a.slices; ++i) M = fmax(M, p[i].x);
+      for (int i = 0; i < a.slices; ++i) Z += p[i].x == -INFINITY && p[i].y == 0.0 ? 0.0 : p[i].y * exp(p[i].x - M);
+      if (!(Z > 0.0 && Z < INFINITY && fabs(M) < INFINITY)) k = 0;
     }
-    auto join = [&](double y, unsigned long long i) { if (y > v || (y == v && i < w)) { v = y; w = i; } };
-    for (int o = 32; o; o >>= 1) join(__shfl_xor(v, o), __shfl_xor(w, o));
-    __syncthreads();
-    if ((tid & 63) == 0) { value[wave] = v; where[wave] = w; }
-    __syncthreads();
-    for (int i = 0; i < 16; ++i) join(value[i], where[i]);
-    const bool none = !(v > -INFINITY);
-    if (tid == 0) {
-      a.best_score[(size_t)g * a.n_best + j] = none ? -INFINITY : (float)v;
-      a.best_row[(size_t)g * a.n_best + j] = none ? -1 : g * a.n_beams + (int)(w >> 32);
-      a.best_token[(size_t)g * a.n_best + j] = none ? -1 : (int)(uint32_t)w;
-    }
-    if (none) { v = -INFINITY; w = ~0ull; }
-    last = v;
-    at = w;
+    kind[b] = (unsigned char)k;
+    base[b] = k == 2 ? (double)s : (double)s - M - log(Z);
   }
+  if (tid == 0) count = 0;
+  __syncthreads();
+  auto at = [&](int list, int j) {                             // the jth of a list
+    const int b = list / a.slices;
+    const unsigned long long id = (unsigned long long)b << 32;
+    if (kind[b] == 0) return candidate{-INFINITY, 0};
+    if (kind[b] == 2) return list == b * a.slices && j == 0 ? candidate{base[b], id | (uint32_t)a.end} : candidate{-INFINITY, 0};
+    const unsigned long long k = a.part_top[((size_t)first * a.slices + list) * a.n_best + j];
+    return k ? candidate{base[b] + (double)top_value(k), id | (uint32_t)~(uint32_t)k} : candidate{-INFINITY, 0};
+  };
+  const int deep = (a.n_best + lists - 1) / lists, heads = lists * deep;      // at least n_best of them
+  for (int i = tid; i < heads; i += 256) head[i] = at(i / deep, i % deep);
+  if (tid == 0) bound = candidate{-INFINITY, 0};
+  __syncthreads();
+  for (int i = tid; i < heads; i += 256) {
+    const candidate c = head[i];
+    int rank = 0;
+#pragma unroll 4
+    for (int o = 0; o < heads; ++o) rank += before(head[o], c);
+    if (rank == a.n_best - 1 && c.worth > -INFINITY) bound = c;
+  }
+  __syncthreads();
+  const candidate last = bound;                                // (none: all there are)
+  for (int i = tid; i < lists; i += 256)
+    for (int j = 0; j < a.n_best; ++j) {
+      const candidate c = at(i, j);
+      if (!(c.worth > -INFINITY) || (last.worth > -INFINITY && before(last, c))) break;
+      gathered[atomicAdd(&count, 1)] = c;
+    }
+  __syncthreads();
+  const int n = count;
+  for (int i = tid; i < n; i += 256) {
+    const candidate c = gathered[i];
+    int rank = 0;
+#pragma unroll 4
+    for (int o = 0; o < n; ++o) rank += before(gathered[o], c);
+    if (rank < a.n_best) {
+      const size_t to = (size_t)g * a.n_best + rank;
+      a.best_score[to] = (float)c.worth;
+      a.best_row[to] = first + (int)(c.id >> 32);
+      a.best_token[to] = (int)(uint32_t)c.id;
+    }
+  }
+  for (int j = n + tid; j < a.n_best; j += 256) {
+    const size_t to = (size_t)g * a.n_best + j;
+    a.best_score[to] = -INFINITY;
+    a.best_row[to] = a.best_token[to] = -1;
+  }
+}
+
+// Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of no less than two vectors a thread, and
+// so that a group has no more lists than kBeamLists.
+constexpr int kBeamPieces = 1024;
+int beam_slices(long long rows, int n_beams, int vocab, int elem) {
+  const long long by_size = (long long)vocab * elem / (16 * 2 * kLpThreads), by_rows = rows >= kBeamPieces ? 1 : (kBeamPieces + rows - 1) / rows;
+  long long n = by_rows < kBeamLists / n_beams ? by_rows : kBeamLists / n_beams;
+  if (by_size < n) n = by_size;
+  return n < 1 ? 1 : (int)n;
+}
+size_t beam_ws(size_t pieces, int n_best, void *base, beam_args *a) {
+  a3_ws_cursor cur(base, 0);
+  double2 *part = (double2 *)cur.take(pieces * sizeof(double2));
+  unsigned long long *top = (unsigned long long *)cur.take(pieces * n_best * sizeof(unsigned long long));
+  if (a) { a->part = part; a->part_top = top; }
+  return cur.off;
 }
 
 template <class F>
@@ -223,7 +426,9 @@ void with_dtype(int dtype, F f) {
 
 extern "C" size_t a3_tree_accept_ws_bytes(int n_rows, int vocab) {
   if (n_rows < 0 || vocab <= 0) return 0;
-  return 256;
+  // (r rows are r min(128, ceil(2048 / r)) pieces at most: below 2048 + r, and r from r = 2048 on)
+  const size_t r = n_rows < kPickPieces ? n_rows : kPickPieces - 1, some = r * 128 < kPickPieces + r ? r * 128 : kPickPieces + r;
+  return ((size_t)n_rows > some ? (size_t)n_rows : some) * sizeof(unsigned long long) + 256;
 }
 
 extern "C" a3_status a3_tree_accept(int dtype, const void *logits, int vocab, long long ld, int *picked, const int *tokens, const int *parent,
@@ -247,10 +452,15 @@ extern "C" a3_status a3_tree_accept(int dtype, const void *logits, int vocab, lo
   A3_REQUIRE(logits == nullptr || (ws && a3_aligned16(ws) && ws_bytes >= need), A3_ERR_WORKSPACE,
              "a3_tree_accept: workspace %zu bytes (16-byte aligned), need %zu", ws ? ws_bytes : 0, need);
   accept_args a{logits, ld, vocab, picked, tokens, parent, group_start, group_len, n_groups, n_rows, max_rows, max_path,
-                count, path, next_token, src_slot, dst_slot};
+                count, path, next_token, src_slot, dst_slot, n_rows ? pick_slices(n_rows, vocab, dtype == A3_BF16 ? 2 : 4) : 1,
+                (unsigned long long *)ws};
+  const int more = logits ? (int)(((long long)n_rows + 63) / 64) : 0;
+  A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31) && (long long)n_groups + more < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_tree_accept: too many rows");
   if (logits && n_rows)
-    with_dtype(dtype, [&](auto e) { hipLaunchKernelGGL(pick_kernel<decltype(e)>, dim3((unsigned)n_rows), dim3(256), 0, (hipStream_t)stream, a); });
-  if (n_groups) hipLaunchKernelGGL(follow_kernel, dim3((unsigned)n_groups), dim3(64), 0, (hipStream_t)stream, a);
+    with_dtype(dtype, [&](auto e) {
+      hipLaunchKernelGGL(pick_kernel<decltype(e)>, dim3((unsigned)(n_rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
+    });
+  hipLaunchKernelGGL(follow_kernel, dim3((unsigned)(n_groups + more)), dim3(256), 0, (hipStream_t)stream, a);
   A3_CHECK_LAUNCH("a3_tree_accept");
   return A3_OK;
 }
@@ -285,18 +495,30 @@ extern "C" a3_status a3_paged_move(const a3_pages *layers, int n_layers, const i
   a.row_bytes = layers->head_dim * (q8 ? 1 : elem_bytes(layers));
   a.q8 = q8;
   a.head_bytes = page_head_bytes(layers->format, elem_bytes(layers), layers->page_size, layers->head_dim);
-  const long long units = (long long)a.max_slots * layers->n_kv_heads * (a.row_bytes / 4 + a.q8), blocks = (units + 255) / 256;
-  for (int l0 = 0; l0 < n_layers; l0 += kLayersAtOnce) {
-    const int n = n_layers - l0 < kLayersAtOnce ? n_layers - l0 : kLayersAtOnce;
+  a.row_shift = __builtin_ctz((unsigned)(a.row_bytes / 16));
+  a.slot_shift = 0;
+  while (a.slot_shift < 8 - a.row_shift && (1 << a.slot_shift) < a.max_slots) ++a.slot_shift;
+  const int heads = 256 >> (a.row_shift + a.slot_shift);
+  a.groups = (layers->n_kv_heads + heads - 1) / heads;
+  const int at_once = 65535 / (2 * a.groups) < kLayersAtOnce ? 65535 / (2 * a.groups) : kLayersAtOnce;
+  A3_REQUIRE(at_once >= 1, A3_ERR_UNSUPPORTED, "a3_paged_move: %d KV heads", layers->n_kv_heads);
+  // (the runs may be shorter than max_slots says: some workgroups that go on along them, not one for each piece that there might be)
+  const long long tiles = ((long long)a.max_slots + (1 << a.slot_shift) - 1) >> a.slot_shift;
+  for (int l0 = 0; l0 < n_layers; l0 += at_once) {
+    const int n = n_layers - l0 < at_once ? n_layers - l0 : at_once;
     for (int l = 0; l < n; ++l) {
       a.pools[2 * l] = (char *)layers[l0 + l].k_pool;
       a.pools[2 * l + 1] = (char *)layers[l0 + l].v_pool;
     }
-    const dim3 grid((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)n_sets, (unsigned)(2 * n));
-    if (set_size <= 4) hipLaunchKernelGGL(move_kernel<4>, grid, dim3(256), 0, (hipStream_t)stream, a);
-    else if (set_size <= 8) hipLaunchKernelGGL(move_kernel<8>, grid, dim3(256), 0, (hipStream_t)stream, a);
-    else if (set_size <= 16) hipLaunchKernelGGL(move_kernel<16>, grid, dim3(256), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(move_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    const long long others = (long long)n_sets * 2 * n * a.groups, want = (8192 + others - 1) / others;
+    const dim3 grid((unsigned)(tiles < want ? tiles : want), (unsigned)n_sets, (unsigned)(2 * n * a.groups));
+    auto launch = [&](auto size) { hipLaunchKernelGGL(move_kernel<size.value>, grid, dim3(256), 0, (hipStream_t)stream, a); };
+    if (set_size <= 2) launch(std::integral_constant<int, 2>{});
+    else if (set_size <= 4) launch(std::integral_constant<int, 4>{});
+    else if (set_size <= 8) launch(std::integral_constant<int, 8>{});
+    else if (set_size <= 16) launch(std::integral_constant<int, 16>{});
+    else if (set_size <= 32) launch(std::integral_constant<int, 32>{});
+    else launch(std::integral_constant<int, 64>{});
     A3_CHECK_LAUNCH("a3_paged_move");
   }
   return A3_OK;
@@ -304,7 +526,10 @@ extern "C" a3_status a3_paged_move(const a3_pages *layers, int n_layers, const i
 
 extern "C" size_t a3_beam_select_ws_bytes(int n_groups, int n_beams, int vocab, int n_best) {
   if (n_groups < 0 || n_beams < 1 || n_beams > kMaxBeams || vocab <= 0 || n_best < 1 || n_best > kMaxBest) return 0;
-  return a3_align_up((size_t)n_groups * n_beams * sizeof(double), 256) + 256;
+  // (r rows are r min(s, ceil(1024 / r)) pieces at most: below 1024 + r, and r from r = 1024 on)
+  const size_t rows = (size_t)n_groups * n_beams, s = beam_slices(1, n_beams, vocab, 4), r = rows < kBeamPieces ? rows : kBeamPieces - 1;
+  const size_t some = r * s < kBeamPieces + r ? r * s : kBeamPieces + r;
+  return beam_ws(rows > some ? rows : some, n_best, nullptr, nullptr) + 256;
 }
 
 extern "C" a3_status a3_beam_select(int dtype, const void *logits, int n_groups, int n_beams, int vocab, long long ld, const float *score,
@@ -324,11 +549,19 @@ extern "C" a3_status a3_beam_select(int dtype, const void *logits, int n_groups,
   const size_t need = a3_beam_select_ws_bytes(n_groups, n_beams, vocab, n_best);
   A3_REQUIRE(ws && a3_aligned16(ws) && ws_bytes >= need, A3_ERR_WORKSPACE, "a3_beam_select: workspace %zu bytes (16-byte aligned), need %zu",
              ws ? ws_bytes : 0, need);
-  beam_args a{logits, ld, vocab, n_beams, n_best, end_token, score, done, best_score, best_row, best_token, (double *)ws};
+  const int rows = n_groups * n_beams;
+  beam_args a{logits, ld, vocab, n_beams, n_best, end_token, beam_slices(rows, n_beams, vocab, dtype == A3_BF16 ? 2 : 4), score, done, best_score,
+              best_row, best_token, nullptr, nullptr};
+  beam_ws((size_t)rows * a.slices, n_best, ws, &a);
   with_dtype(dtype, [&](auto e) {
-    hipLaunchKernelGGL(beam_row_kernel<decltype(e)>, dim3((unsigned)(n_groups * n_beams)), dim3(256), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL(beam_choose_kernel<decltype(e)>, dim3((unsigned)n_groups), dim3(1024), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(beam_row_kernel<decltype(e)>, dim3((unsigned)(rows * a.slices)), dim3(kLpThreads), 0, (hipStream_t)stream, a);
   });
+  static a3_once_per_device lds_once;
+  if (a3_once(lds_once, [&]() {
+        return hipFuncSetAttribute((const void *)beam_join_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kMaxBest * kMaxBest * sizeof(candidate)));
+      }) != hipSuccess)
+    return a3_fail(A3_ERR_HIP, "a3_beam_select: cannot raise the dynamic LDS limit");
+  hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)n_groups), dim3(256), (size_t)n_best * n_best * sizeof(candidate), (hipStream_t)stream, a);
   A3_CHECK_LAUNCH("a3_beam_select");
   return A3_OK;
 }
