@@ -43,9 +43,9 @@ struct tree_args {
 // is not seen has weight 0.  0 times a value that is not finite would be NaN in the rows that do not see it, so there such values are taken out
 // of the product and, where there are any, added to the rows that see them when the item is put together (its result there is not finite
 // whatever the weights are).
-template <typename T, int D, bool Q8, int NB_, int WC_>
+template <typename T, int D, bool Q8, int NB_, int WC_, int W_>
 struct tree_form {
-  static constexpr int NB = NB_, WC = WC_, WS = 4 / WC_;
+  static constexpr int NB = NB_, WC = WC_, W = W_, WS = W_ / WC_;
   static constexpr bool kF32 = sizeof(T) == 4 && !Q8;          // fp32 matrix instructions
   static constexpr int SK = kF32 ? 16 : 32;                    // slots of a wave's slab
   static constexpr int KB = SK / 16;                           // row blocks of S^T
@@ -76,32 +76,35 @@ __device__ __forceinline__ group_work work_of(const tree_args &a, int start, int
 }
 
 template <class F, typename T, int D, bool Q8>
-__global__ void __launch_bounds__(256, F::NB == 1 || (F::NB == 2 && (sizeof(T) == 2 || D == 64)) ? 2 : 1)
+__global__ void __launch_bounds__(64 * F::W, F::W == 4 && !(sizeof(T) == 4 && D == 128 && F::NB == 2) ? 2 : 1)
 tree_attention_kernel(tree_args a) {
-  constexpr int SK = F::SK, NB = F::NB, WS = F::WS, WC = F::WC, kOS = D + 4;
-  __shared__ int scan[8], found[2];
-  __shared__ float2 ml[4][16];
-  __shared__ int sees[4][16];
-  __shared__ __align__(16) float os[4][16][kOS];
+  constexpr int SK = F::SK, NB = F::NB, WS = F::WS, WC = F::WC, W = F::W, kOS = D + 4;
+  __shared__ int scan[2][W], found[2], odd_waves[W];
+  __shared__ float2 ml[W][16];
+  __shared__ int sees[W][16];
+  __shared__ __align__(16) float os[W][16][kOS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, lg = lane >> 4, G = a.p.Hq / a.p.Hkv, Hkv = a.p.Hkv, wc = wave % WC, wsl = wave / WC;
 
   // ---- this workgroup's run of steps -----------------------------------------------------------------------
-  // Up to 256 groups: one thread a group.  More: the groups' sum first, then blocks of 256 up to the one the run begins in.
+  // Up to as many groups as threads: one thread a group.  More: the groups' sum first, then blocks of them up to the one the run begins in.
   auto steps_of = [&](int g) {
     if (g >= a.n_groups) return 0;
     const group_work w = work_of<F::kStep, F::TC>(a, a.start[g], a.start[g + 1], a.req ? a.req[g] : g, a.len[g]);
     return w.steps * w.tiles;
   };
   int st = steps_of(tid), incl = a3_wave_prefix(st), sum = incl;
-  if (a.n_groups > 256) {
+  if (a.n_groups > 64 * W) {
     int mine = st;
-    for (int g = tid + 256; g < a.n_groups; g += 256) mine += steps_of(g);
+    for (int g = tid + 64 * W; g < a.n_groups; g += 64 * W) mine += steps_of(g);
     sum = a3_wave_prefix(mine);
   }
-  if (lane == 63) { scan[wave] = sum; scan[4 + wave] = incl; }
+  if (lane == 63) { scan[0][wave] = sum; scan[1][wave] = incl; }
   __syncthreads();
-  const int total = (scan[0] + scan[1] + scan[2] + scan[3]) * Hkv;
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) total += scan[0][i];
+  total *= Hkv;
   // neighbouring runs, which may read the same slots for other columns, on one of the eight dies (workgroups are dealt out in turn)
   const int w = a.shares % 8 == 0 ? (int)(blockIdx.x % 8) * (a.shares / 8) + blockIdx.x / 8 : blockIdx.x;
   const int each = total / a.shares, rest = total - each * a.shares;      // the first `rest` workgroups take one more
@@ -110,16 +113,17 @@ tree_attention_kernel(tree_args a) {
   if (n_steps == 0) return;
   for (int g0 = 0, before = 0;;) {                             // before: steps of the groups in front of this block
     int base = before;
-    for (int i = 0; i < wave; ++i) base += scan[4 + i];
+    for (int i = 0; i < wave; ++i) base += scan[1][i];
     const int lo = (base + incl - st) * Hkv, hi = (base + incl) * Hkv;
     if (first >= lo && first < hi) { found[0] = g0 + tid; found[1] = first - lo; }
-    before += scan[4] + scan[5] + scan[6] + scan[7];
+#pragma unroll
+    for (int i = 0; i < W; ++i) before += scan[1][i];
     if (before * Hkv > first) break;
-    g0 += 256;
+    g0 += 64 * W;
     st = steps_of(g0 + tid);
     incl = a3_wave_prefix(st);
     __syncthreads();
-    if (lane == 63) scan[4 + wave] = incl;
+    if (lane == 63) scan[1][wave] = incl;
     __syncthreads();
   }
   __syncthreads();
@@ -151,57 +155,66 @@ tree_attention_kernel(tree_args a) {
 
   // ---- one slab of one wave in registers ------------------------------------------------------------------
   const size_t head_bytes = page_head_bytes(Q8 ? A3_PAGES_Q8 : A3_PAGES_PLAIN, sizeof(T), 1 << a.p.page_shift, D);
-  uint32_t koff[F::KB], voff;
-#pragma unroll
-  for (int b = 0; b < F::KB; ++b) koff[b] = (SK == 16 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3)) * F::kRow + 16 * lg;
-  voff = (uint32_t)(F::NS * lg * F::kRow + F::kVWords * 4 * l16);
+  // (buffer loads: the page in four scalars, a lane's place in one register)
+  const uint32_t koff = (SK == 16 ? l16 : 8 * (l16 >> 2) + (l16 & 3)) * F::kRow + 16 * lg;
+  const uint32_t voff = (uint32_t)(F::NS * lg * F::kRow + F::kVWords * 4 * l16);
   auto slot_of = [&](const place &p) { return p.step * F::kStep + SK * wsl; };
   uint4 sk[F::KB][F::NK];
   uint32_t sv[F::NS][F::NP][F::kVWords];
   f32x4 ks[Q8 ? 2 : 1], vs[Q8 ? 2 : 1];
   struct where { size_t block; int at, n; };                   // n: its slots up to the tree's end (<= 0: none of them counts)
-  auto find = [&](const place &p, bool more) {
-    const int slot = slot_of(p);
-    where x{0, 0, 0};
-    if (!more || slot >= p.k.end) return x;
-    const int page = scalar_at(a.p.table, (size_t)p.k.req * a.p.max_pages + (slot >> a.p.page_shift));
-    if (page < 0 || page >= a.p.n_pages) return x;
-    x.block = ((size_t)page * Hkv + p.head) * head_bytes;
-    x.at = slot & ((1 << a.p.page_shift) - 1);
-    x.n = p.k.end - slot;
+  auto page_at = [&](const place &p, int slot) {               // its number; behind the tree any
+    return scalar_at(a.p.table, (size_t)p.k.req * a.p.max_pages + (min(slot, p.k.end - 1) >> a.p.page_shift));
+  };
+  auto on_page = [&](const place &p, int slot, int page) {
+    const bool none = slot >= p.k.end || page < 0 || page >= a.p.n_pages;
+    where x;
+    x.block = none ? 0 : ((size_t)page * Hkv + p.head) * head_bytes;
+    x.at = none ? 0 : slot & ((1 << a.p.page_shift) - 1);
+    x.n = none ? 0 : p.k.end - slot;
     return x;
   };
+  auto find = [&](const place &p) { return on_page(p, slot_of(p), page_at(p, slot_of(p))); };
+  constexpr int kAux = F::kOnce ? 2 : 0;                       // nontemporal
+  auto page_of = [&](const char *pool, const where &x) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pool) + x.block, 0, (int)head_bytes, 0x00020000);
+  };
   auto load_k = [&](const where &x) {
-    const char *kb = a.p.k_pool + x.block + x.at * F::kRow;
+    const auto page = page_of(a.p.k_pool, x);
+    const int at = x.at * F::kRow;
 #pragma unroll
     for (int b = 0; b < F::KB; ++b)
 #pragma unroll
-      for (int i = 0; i < F::NK; ++i) {
-        const uint4 *at = reinterpret_cast<const uint4 *>(kb + koff[b] + 64 * i);
-        sk[b][i] = F::kOnce ? a3_nt_load(at) : *at;
-      }
+      for (int i = 0; i < F::NK; ++i)
+        sk[b][i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(page, koff + 4 * b * F::kRow + 64 * i, at, kAux));
     if constexpr (Q8) {
-      const char *sc = a.p.k_pool + x.block + ((size_t)D << a.p.page_shift) + 4 * x.at + 32 * lg;
-      ks[0] = *reinterpret_cast<const f32x4 *>(sc);
-      ks[1] = *reinterpret_cast<const f32x4 *>(sc + 16);
+      const int sc = (D << a.p.page_shift) + 4 * x.at;
+      ks[0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(page, 32 * lg, sc, 0));
+      ks[1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(page, 32 * lg + 16, sc, 0));
     }
   };
   auto load_v = [&](const where &x) {
-    const char *vb = a.p.v_pool + x.block + x.at * F::kRow;
+    const auto page = page_of(a.p.v_pool, x);
+    const int at = x.at * F::kRow;
 #pragma unroll
     for (int i = 0; i < F::NS; ++i)
 #pragma unroll
       for (int j = 0; j < F::NP; ++j) {
-        typedef uint32_t words __attribute__((ext_vector_type(F::kVWords == 1 ? 1 : F::kVWords)));
-        const words *at = reinterpret_cast<const words *>(vb + voff + i * F::kRow + j * 64 * F::kVWords);
-        const words y = F::kOnce ? __builtin_nontemporal_load(at) : *at;
-#pragma unroll
-        for (int u = 0; u < F::kVWords; ++u) sv[i][j][u] = y[u];
+        const uint32_t from = voff + i * F::kRow + j * 64 * F::kVWords;
+        if constexpr (F::kVWords == 4) {
+          const uint4 y = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(page, from, at, kAux));
+          sv[i][j][0] = y.x; sv[i][j][1] = y.y; sv[i][j][2] = y.z; sv[i][j][3] = y.w;
+        } else if constexpr (F::kVWords == 2) {
+          const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(page, from, at, kAux));
+          sv[i][j][0] = y.x; sv[i][j][1] = y.y;
+        } else {
+          sv[i][j][0] = __builtin_amdgcn_raw_buffer_load_b32(page, from, at, kAux);
+        }
       }
     if constexpr (Q8) {
-      const char *sc = a.p.v_pool + x.block + ((size_t)D << a.p.page_shift) + 4 * x.at + 32 * lg;
-      vs[0] = *reinterpret_cast<const f32x4 *>(sc);
-      vs[1] = *reinterpret_cast<const f32x4 *>(sc + 16);
+      const int sc = (D << a.p.page_shift) + 4 * x.at;
+      vs[0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(page, 32 * lg, sc, 0));
+      vs[1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(page, 32 * lg + 16, sc, 0));
     }
   };
 
@@ -210,7 +223,7 @@ tree_attention_kernel(tree_args a) {
   f32x4 qf[F::kF32 ? NB : 1][F::kF32 ? NQ : 1];
   bf16x8 qb[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kQParts][F::kF32 ? 1 : NQ];
   int row[NB];                                                 // of the group
-  auto load_queries = [&](const place &p) {
+  auto load_queries = [&](const place &p, int (&row)[NB]) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // (columns past the last repeat it: nothing of them is stored)
@@ -280,10 +293,11 @@ tree_attention_kernel(tree_args a) {
     return bits & (top >= F::NS ? kAll : top <= 0 ? 0u : (1u << top) - 1);
   };
 
-  // One slab: `cur` is in the registers, `next` is asked for meanwhile.
-  auto work = [&](const where &cur, const where &next, const place &p) {
-    const int t0 = slot_of(p) + F::NS * lg - p.k.len;
-    const bool masked = cur.n < SK || slot_of(p) + SK > p.k.len;     // (uniform)
+  // One slab: `cur` is in the registers, `next` is asked for meanwhile.  MASKED: it reaches behind the committed slots, or does not exist.
+  // Loads come back in order: the next item's queries are asked for in front of its first K, so that a wait for that K is one for them.
+  auto work = [&](auto with_mask, const where &cur, const where &next, const place &p, const place *to) {
+    constexpr bool MASKED = decltype(with_mask)::value;
+    int row_next[NB];
     f32x4 acc[NB][F::KB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -313,6 +327,10 @@ tree_attention_kernel(tree_args a) {
               for (int k = 0; k < F::kQParts; ++k)
                 acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][k][2 * i + u], acc[nb][b], 0, 0, 0);
           }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[nb][b] *= ks[b];
     } else {
 #pragma unroll
       for (int i = 0; i < F::NK; ++i)
@@ -322,47 +340,110 @@ tree_attention_kernel(tree_args a) {
           for (int b = 0; b < F::KB; ++b)
             acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, sk[b][i]), qb[nb][0][i], acc[nb][b], 0, 0, 0);
     }
-    if constexpr (Q8) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) acc[nb][b] *= ks[b];
-    }
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (MASKED) {
+      if (to) load_queries(*to, row_next);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     load_k(next);
     __builtin_amdgcn_sched_barrier(0);
-    if (masked) {
+    uint32_t vis[NB];
+    float top[NB];
+    bool far = false;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      vis[nb] = ~0u;
+      if constexpr (MASKED) {
+        vis[nb] = cur.n <= 0 ? 0u : seen_slots(p, slot_of(p) + F::NS * lg - p.k.len, row[nb]);
+#pragma unroll
+        for (int i = 0; i < F::NS; ++i)
+          if (!(vis[nb] >> i & 1)) acc[nb][i >> 2][i & 3] = -INFINITY;
+        if (vis[nb]) seen |= 1 << nb;
+      }
+      top[nb] = acc[nb][0][0];
+#pragma unroll
+      for (int i = 1; i < F::NS; ++i) top[nb] = fmaxf(top[nb], acc[nb][i >> 2][i & 3]);
+      far |= fmaf(top[nb], a.scale, -m[nb]) > 8.f;
+    }
+    if constexpr (!MASKED) seen = (1 << NB) - 1;
+    if (__builtin_expect(__any(far), 0)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float t = top[nb] * a.scale;
+        t = fmaxf(t, __shfl_xor(t, 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float up = fmaxf(m[nb], t), f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - up);
+        m[nb] = up;
+        l[nb] *= f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
+      }
+    }
+    // weights: their parts (fp32 pages: themselves)
+    bf16x8 pf[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kPParts];
+    float pw[F::kF32 ? NB : 1][F::kF32 ? 4 : 1];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
+      float w[F::NS];
 #pragma unroll
       for (int i = 0; i < F::NS; ++i) {
-        const bool none = F::NS * lg + i >= cur.n;             // behind the tree: anything
-        if constexpr (Q8) {
-          if (none) vs[i >> 2][i & 3] = 0.f;
-        } else {
+        w[i] = __builtin_amdgcn_exp2f(fmaf(acc[nb][i >> 2][i & 3], a.scale, ref));
+        l[nb] += w[i];
+      }
+      if constexpr (Q8) {
 #pragma unroll
-          for (int j = 0; j < F::NP; ++j)
+        for (int i = 0; i < F::NS; ++i) w[i] = !MASKED || vis[nb] >> i & 1 ? w[i] * vs[i >> 2][i & 3] : 0.f;
+      }
+      if constexpr (F::kF32) {
 #pragma unroll
-            for (int u = 0; u < F::kVWords; ++u) {
-              uint32_t x = none ? 0u : sv[i][j][u];
-              if constexpr (sizeof(T) == 4) {
-                if ((x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
-              } else {
-                if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
-                if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
-              }
-              sv[i][j][u] = x;
-            }
+        for (int i = 0; i < 4; ++i) pw[nb][i] = w[i];
+      } else {
+        // (cut off, not rounded: a remainder is never negative; weights are finite or NaN, and a NaN here stays one without its lower half)
+#pragma unroll
+        for (int k = 0; k < F::kPParts; ++k) {
+          uint32_t x[4];
+          if (k == F::kPParts - 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pf[nb][k][i] = a3_f2bf(w[i]);
+            continue;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(__float_as_uint(w[2 * i + 1]), __float_as_uint(w[2 * i]), 0x07060302u);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] -= __uint_as_float(__float_as_uint(w[i]) & 0xffff0000u);
+          pf[nb][k] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
         }
       }
     }
-    // V^T operands
-    bf16x8 vf[F::kF32 ? 1 : D / 16];
-    float vw[F::kF32 ? 4 : 1][F::kF32 ? D / 16 : 1];
-    f32x4 vscale[Q8 ? 2 : 1];
+    if constexpr (MASKED && !Q8) {
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i) {
+        const bool none = F::NS * lg + i >= cur.n;             // behind the tree: anything
+        const bool drafted = slot_of(p) + F::NS * lg + i >= p.k.len;      // (every row sees the committed ones)
+#pragma unroll
+        for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+          for (int u = 0; u < F::kVWords; ++u) {
+            uint32_t x = none ? 0u : sv[i][j][u];
+            if constexpr (sizeof(T) == 4) {
+              if (drafted && (x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
+            } else {
+              if (drafted && (x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+              if (drafted && (x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+            }
+            sv[i][j][u] = x;
+          }
+      }
+    }
     if constexpr (F::kF32) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) vw[i][c] = __builtin_bit_cast(float, sv[i][c >> 2][c & 3]);
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, sv[i][c >> 2][c & 3]), pw[nb][i], o[nb][c], 0, 0, 0);
     } else {
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
@@ -374,66 +455,20 @@ tree_attention_kernel(tree_args a) {
           else
             x[i] = __builtin_amdgcn_perm(sv[2 * i + 1][0][c >> 1], sv[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
         }
-        vf[c] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
-      }
-    }
-    if constexpr (Q8) { vscale[0] = vs[0]; vscale[1] = vs[1]; }
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(next);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      float w[F::NS];
-#pragma unroll
-      for (int i = 0; i < F::NS; ++i) w[i] = acc[nb][i >> 2][i & 3] * a.scale;
-      uint32_t vis = ~0u;
-      if (masked) {
-        vis = cur.n <= 0 ? 0u : seen_slots(p, t0, row[nb]);
-#pragma unroll
-        for (int i = 0; i < F::NS; ++i)
-          if (!(vis >> i & 1)) w[i] = -INFINITY;
-      }
-      if (vis) seen |= 1 << nb;
-      float top = w[0];
-#pragma unroll
-      for (int i = 1; i < F::NS; ++i) top = fmaxf(top, w[i]);
-      if (__any(top > m[nb] + 8.f)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float up = fmaxf(m[nb], top), f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - up);
-        m[nb] = up;
-        l[nb] *= f;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
-      }
-      const float ref = m[nb] == -INFINITY ? 0.f : m[nb];
-#pragma unroll
-      for (int i = 0; i < F::NS; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(w[i] - ref);
-        l[nb] += w[i];
-        if constexpr (Q8) w[i] = vis >> i & 1 ? w[i] * vscale[i >> 2][i & 3] : 0.f;
-      }
-      if constexpr (F::kF32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int c = 0; c < D / 16; ++c) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw[i][c], w[i], o[nb][c], 0, 0, 0);
-      } else {
-        bf16x8 pf[F::kPParts];
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
 #pragma unroll
         for (int k = 0; k < F::kPParts; ++k)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (k == F::kPParts - 1) { pf[k][i] = a3_f2bf(w[i]); continue; }
-            const uint32_t h = __builtin_elementwise_sub_sat(__float_as_uint(w[i]), 1u) & 0xffff0000u;
-            pf[k][i] = __builtin_bit_cast(bf16_t, (unsigned short)(h >> 16));
-            w[i] -= __uint_as_float(h);
-          }
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-          for (int k = 0; k < F::kPParts; ++k) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], pf[k], o[nb][c], 0, 0, 0);
+          for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[nb][k], o[nb][c], 0, 0, 0);
       }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(next);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (MASKED) {
+      if (to)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) row[nb] = row_next[nb];
     }
   };
 
@@ -457,7 +492,7 @@ tree_attention_kernel(tree_args a) {
     const bool whole = begins && ends;
     const int slot = 2 * w + (begins ? 1 : 0);
     const int some_odd = __any(odd);
-    if (lane == 0) scan[wave] = some_odd;                      // (the sums of steps are not needed any more)
+    if (lane == 0) odd_waves[wave] = some_odd;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       l[nb] += __shfl_xor(l[nb], 16);
@@ -482,7 +517,7 @@ tree_attention_kernel(tree_args a) {
                 f32x4{o[nb][b][r], o[nb][b + 1][r], o[nb][b + 2][r], o[nb][b + 3][r]} * f;
           }
       A3_LDS_BARRIER();
-      for (int e = tid; e < WC * 16 * (D / 4); e += 256) {
+      for (int e = tid; e < WC * 16 * (D / 4); e += 64 * W) {
         const int col = e / (D / 4), d = 4 * (e % (D / 4)), cw = col >> 4, ci = col & 15;
         const int in = (cw * NB + nb) * 16 + ci, at = p.tile * F::TC + in;   // its number in the item, and among the group's columns
         if (at >= p.k.rows * G) continue;
@@ -501,8 +536,12 @@ tree_attention_kernel(tree_args a) {
           L += y.x == -INFINITY ? 0.f : y.y * __builtin_amdgcn_exp2f(y.x - M);
         }
         const int j = at / G;
-        if constexpr (!Q8)
-          if (scan[0] | scan[1] | scan[2] | scan[3]) add_odd(p, j, d, sum);
+        if constexpr (!Q8) {
+          int odd_any = 0;
+#pragma unroll
+          for (int x = 0; x < W; ++x) odd_any |= odd_waves[x];
+          if (__builtin_expect(odd_any, 0)) add_odd(p, j, d, sum);
+        }
         if (whole) {
           typedef T vec4 __attribute__((ext_vector_type(4)));
           vec4 y;
@@ -518,41 +557,54 @@ tree_attention_kernel(tree_args a) {
     }
   };
 
-  // ---- the run of steps ------------------------------------------------------------------------------------------
-  place ahead = now;
-  bool begins = now.step == 0;
-  where cur = find(now, true);
+  // ---- the run of steps: of every item first those whose slots are all committed ------------------------------------------
+  where cur = find(now);
+  load_queries(now, row);
+  __builtin_amdgcn_sched_barrier(0);
   load_k(cur);
+  __builtin_amdgcn_sched_barrier(0);
   load_v(cur);
-  load_queries(now);
+  __builtin_amdgcn_sched_barrier(0);
   clear();
-  for (int i = 0; i < n_steps; ++i) {
-    const bool more = i + 1 < n_steps, ends = now.step == now.k.steps - 1;
-    if (more) advance(ahead);
-    const where next = find(ahead, more);
-    work(cur, next, now);
-    cur = next;
-    if (!ends && more) {
+  for (int left = n_steps; left > 0;) {                        // an item, or the part of it that is in this run
+    const bool begins = now.step == 0;
+    const int here = min(now.k.steps - now.step, left), begun = now.step;
+    const int plain = max(0, min(now.k.len / F::kStep, begun + here - 1) - begun);       // (the last one of the run's part is not among them)
+    int i = 0, page = page_at(now, slot_of(now) + F::kStep);
+    for (; i < plain && cur.n >= SK; ++i) {                    // (up to a page that does not exist)
+      const int slot = slot_of(now) + F::kStep, page2 = page_at(now, slot + F::kStep);     // a step ahead: a scalar load takes a while
+      const where next = on_page(now, slot, page);
+      work(std::false_type{}, cur, next, now, nullptr);
+      cur = next;
+      page = page2;
       ++now.step;
-      continue;
     }
-    finish(now, begins, ends);
-    if (begins && tid == 0) {
-      int pieces = 1;
-      if (!ends) {                                             // goes on in the workgroups behind: how many of them
-        // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
-        const int last = first + i + now.k.steps - 1 - now.step, fat = rest * (each + 1);
-        pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+    for (; i < here; ++i) {
+      place p = now;
+      if (i + 1 < here) ++p.step;
+      else if (left > here) advance(p);
+      const where next = i + 1 < here || left > here ? find(p) : where{0, 0, 0};
+      work(std::true_type{}, cur, next, now, i + 1 == here && left > here ? &p : nullptr);
+      cur = next;
+      if (i + 1 < here) now = p;
+      else {
+        const bool ends = now.step == now.k.steps - 1;
+        finish(now, begins, ends);
+        if (begins && tid == 0) {
+          int pieces = 1;
+          if (!ends) {                                         // goes on in the workgroups behind: how many of them
+            // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+            const int last = first + (n_steps - left) + now.k.steps - 1 - begun, fat = rest * (each + 1);
+            pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+          }
+          if (a.by_item) a.cut[((size_t)now.g * Hkv + now.head) * a.tiles + now.tile] = make_int4(now.g, now.head, w, pieces);
+          else if (!ends) a.cut[w] = make_int4(now.g, now.head | now.tile << 16, w, pieces);
+        }
+        clear();
+        now = p;
       }
-      if (a.by_item) a.cut[((size_t)now.g * Hkv + now.head) * a.tiles + now.tile] = make_int4(now.g, now.head, w, pieces);
-      else if (!ends) a.cut[w] = make_int4(now.g, now.head | now.tile << 16, w, pieces);
     }
-    begins = true;
-    clear();
-    if (more) {
-      now = ahead;
-      load_queries(now);
-    }
+    left -= here;
   }
 }
 
@@ -634,27 +686,23 @@ tree_join_kernel(tree_args a) {
 
 constexpr int kMaxRows = 1024;
 
-// What a call runs in: blocks of columns a wave, waves beside each other, workgroups at most.
-struct tree_shape { int nb, wc, wgs; };
+// What a call runs in: blocks of columns a wave, waves beside each other, waves, workgroups at most.
+struct tree_shape { int nb, wc, waves, wgs; };
 tree_shape shape_of(const a3_pages *P, int max_rows) {
   const int cols = max_rows * (P->n_q_heads / P->n_kv_heads);
-  if (cols <= 16) return {1, 1, 512};
-  if (cols <= 32) return {2, 1, P->dtype == A3_F32 && P->head_dim == 128 ? 256 : 512};
-  if (P->dtype == A3_F32) return {2, cols <= 64 ? 2 : 4, P->head_dim == 64 ? 512 : 256};
-  return cols <= 64 ? tree_shape{4, 1, 256} : cols <= 128 ? tree_shape{4, 2, 256} : tree_shape{4, 4, 256};
+  const bool wide = P->dtype == A3_F32 && P->head_dim == 128;  // (two blocks a wave: registers for one wave a SIMD)
+  if (cols <= 16) return {1, 1, 4, 512};
+  if (cols <= 32) return {2, 1, 4, wide ? 256 : 512};
+  if (wide) return {2, 4, 4, 256};
+  return {2, cols <= 64 ? 2 : 4, 8, 256};
 }
 template <typename T, int D, bool Q8, class F>
 void with_shape(tree_shape s, F f) {
-  if (s.nb == 1) f(tree_form<T, D, Q8, 1, 1>{});
-  else if (s.nb == 2 && s.wc == 1) f(tree_form<T, D, Q8, 2, 1>{});
-  else if constexpr (sizeof(T) == 4) {
-    if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2>{});
-    else f(tree_form<T, D, Q8, 2, 4>{});
-  } else {
-    if (s.wc == 1) f(tree_form<T, D, Q8, 4, 1>{});
-    else if (s.wc == 2) f(tree_form<T, D, Q8, 4, 2>{});
-    else f(tree_form<T, D, Q8, 4, 4>{});
-  }
+  if (s.nb == 1) f(tree_form<T, D, Q8, 1, 1, 4>{});
+  else if (s.wc == 1) f(tree_form<T, D, Q8, 2, 1, 4>{});
+  else if constexpr (sizeof(T) == 4 && D == 128) f(tree_form<T, D, Q8, 2, 4, 4>{});
+  else if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 8>{});
+  else f(tree_form<T, D, Q8, 2, 4, 8>{});
 }
 struct tree_plan { tree_shape s; int tc, tiles, shares; long long items, steps; };
 tree_plan plan_of(const a3_pages *P, int n_groups, int max_rows) {
@@ -662,7 +710,7 @@ tree_plan plan_of(const a3_pages *P, int n_groups, int max_rows) {
   p.s = shape_of(P, max_rows);
   p.tc = 16 * p.s.nb * p.s.wc;
   p.tiles = (max_rows * (P->n_q_heads / P->n_kv_heads) + p.tc - 1) / p.tc;
-  const int step = 4 / p.s.wc * (P->dtype == A3_F32 && P->format == A3_PAGES_PLAIN ? 16 : 32);
+  const int step = p.s.waves / p.s.wc * (P->dtype == A3_F32 && P->format == A3_PAGES_PLAIN ? 16 : 32);
   p.items = (long long)n_groups * P->n_kv_heads * p.tiles;
   p.steps = ((long long)P->max_pages * P->page_size + step - 1) / step * p.items;
   p.shares = p.steps < p.s.wgs ? (int)p.steps : p.s.wgs;
@@ -727,7 +775,7 @@ extern "C" a3_status a3_tree_attention(const a3_pages *P, const void *q, int n_g
     typedef decltype(elem) T;
     with_shape<T, d.value, q8.value>(plan.s, [&](auto form) {
       typedef decltype(form) F;
-      hipLaunchKernelGGL((tree_attention_kernel<F, T, d.value, q8.value>), dim3((unsigned)plan.shares), dim3(256), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((tree_attention_kernel<F, T, d.value, q8.value>), dim3((unsigned)plan.shares), dim3(64 * F::W), 0, (hipStream_t)stream, a);
       hipLaunchKernelGGL((tree_join_kernel<T, d.value, F::TC>), join, dim3(kJoinThreads), 0, (hipStream_t)stream, a);
     });
   });
