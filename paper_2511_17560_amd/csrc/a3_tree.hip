@@ -58,6 +58,15 @@ struct tree_form {
   static constexpr int TC = 16 * NB * WC;                      // columns of an item
   static constexpr int kStep = WS * SK;
   static constexpr bool kOnce = WC_ == 1;                      // a cache is read once: nontemporal
+  // Eight waves with bf16 rows: slabs through LDS, a ring of kStages steps.
+  static constexpr bool kLds = W_ == 8 && sizeof(T) == 2;
+  static constexpr int kHalf = SK * kRow, kScales = 2 * kHalf, kSlab = kScales + (Q8 ? 512 : 0);   // K, V, scales of both (256 bytes each)
+  static constexpr int kStage = WS * kSlab, kFit = 131072 / kStage, kStages = kFit > 4 ? 4 : kFit;
+  static constexpr int kLoads = kRow / 16 / WC, kPer = kLoads + (Q8 ? 1 : 0);  // direct-to-LDS loads of a wave and step
+  static constexpr int kBlocks = NB * D / 16;                  // accumulator blocks of a wave
+  static constexpr int kRoom = (kLds ? kStage : 0) / (W_ / 2) / 1024;          // of which the stage at hand has room for so many, of half the waves
+  static constexpr int kAtOnce = !kLds || kRoom >= kBlocks ? kBlocks : kRoom >= kBlocks / 2 ? kBlocks / 2 : kRoom >= kBlocks / 4 ? kBlocks / 4 : kBlocks / 8;
+  static constexpr int kLdsBytes = kLds ? kStages * kStage : WS > 1 ? W_ / 2 * kBlocks * 1024 : 16;
 };
 
 // Steps of a group's item, and items of its KV heads (0 steps: nothing of the group is written).
@@ -78,11 +87,11 @@ __device__ __forceinline__ group_work work_of(const tree_args &a, int start, int
 template <class F, typename T, int D, bool Q8>
 __global__ void __launch_bounds__(64 * F::W, F::W == 4 && !(sizeof(T) == 4 && D == 128 && F::NB == 2) ? 2 : 1)
 tree_attention_kernel(tree_args a) {
-  constexpr int SK = F::SK, NB = F::NB, WS = F::WS, WC = F::WC, W = F::W, kOS = D + 4;
+  constexpr int SK = F::SK, NB = F::NB, WS = F::WS, WC = F::WC, W = F::W;
+  extern __shared__ __align__(16) unsigned char lds[];
   __shared__ int scan[2][W], found[2], odd_waves[W];
-  __shared__ float2 ml[W][16];
-  __shared__ int sees[W][16];
-  __shared__ __align__(16) float os[W][16][kOS];
+  __shared__ float2 ml[NB][W][16];
+  __shared__ int sees[NB][W][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, lg = lane >> 4, G = a.p.Hq / a.p.Hkv, Hkv = a.p.Hkv, wc = wave % WC, wsl = wave / WC;
 
@@ -180,6 +189,7 @@ tree_attention_kernel(tree_args a) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pool) + x.block, 0, (int)head_bytes, 0x00020000);
   };
   auto load_k = [&](const where &x) {
+    if constexpr (F::kLds) return;
     const auto page = page_of(a.p.k_pool, x);
     const int at = x.at * F::kRow;
 #pragma unroll
@@ -194,6 +204,7 @@ tree_attention_kernel(tree_args a) {
     }
   };
   auto load_v = [&](const where &x) {
+    if constexpr (F::kLds) return;
     const auto page = page_of(a.p.v_pool, x);
     const int at = x.at * F::kRow;
 #pragma unroll
@@ -218,18 +229,63 @@ tree_attention_kernel(tree_args a) {
     }
   };
 
+  // Through LDS: the waves that share a slab bring equal parts of it, 1 KB a load, lane after lane 16 bytes.  16-byte piece c of slot s of K
+  // lies at place c ^ key(s) of its row, so that the 16 slots a quarter wave reads at one place lie in all 64 banks once.
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
+  constexpr int kPieces = F::kRow / 16, kRows = 1024 / F::kRow;         // pieces of a slot; slots of a load
+  auto key_of = [&](int s) { return ((s >> 3 & 3) << 2 | (s & 3)) >> (F::kRow == 256 ? 0 : F::kRow == 128 ? 1 : 2); };
+  uint32_t dma_off[F::kLds ? F::kLoads : 1];
+  if constexpr (F::kLds) {
+#pragma unroll
+    for (int t = 0; t < F::kLoads; ++t) {
+      const int q = wc * F::kLoads + t, half = 2 * kPieces / 4;              // loads of K, then of V: kRow / 32 each
+      const int s = (q % half) * kRows + lane / kPieces, c = lane % kPieces;
+      dma_off[t] = (uint32_t)(s * F::kRow + 16 * (q < half ? c ^ key_of(s) : c));
+    }
+  }
+  // Inline assembly on purpose: the compiler then neither treats these as LDS writes (it would wait for all of them before every LDS
+  // read) nor moves memory accesses across them; the waits for them are the explicit s_waitcnt below.
+  auto dma = [&](const where &x, uint32_t stage) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const uint64_t pk = (uint64_t)a.p.k_pool + x.block, pv = (uint64_t)a.p.v_pool + x.block;
+    const u32x4 rk = {(uint32_t)pk, (uint32_t)(pk >> 32) & 0xffffu, (uint32_t)head_bytes, 0x00020000u};
+    const u32x4 rv = {(uint32_t)pv, (uint32_t)(pv >> 32) & 0xffffu, (uint32_t)head_bytes, 0x00020000u};
+    constexpr int half = F::kRow / 32;
+    const uint32_t to = lds_base + stage * F::kStage + wsl * F::kSlab, at = (uint32_t)x.at * F::kRow;
+#pragma unroll
+    for (int t = 0; t < F::kLoads; ++t) {
+      const int q = wc * F::kLoads + t;
+      const u32x4 r = q < half ? rk : rv;
+      const uint32_t m0 = __builtin_amdgcn_readfirstlane(to + (q < half ? 0 : F::kHalf) + (q % half) * 1024);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(m0), "v"(dma_off[t]), "s"(r), "s"(at) : "memory");
+    }
+    if constexpr (Q8) {                                        // 64 scales, of which 32 are the slab's (behind the head's page: zeros)
+      const u32x4 r = wc & 1 ? rv : rk;
+      const uint32_t m0 = __builtin_amdgcn_readfirstlane(to + F::kScales + (wc & 1 ? 256 : 0)), sc = (uint32_t)(D << a.p.page_shift) + 4 * x.at;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(m0), "v"(4 * lane), "s"(r), "s"(sc) : "memory");
+    }
+  };
+
   // ---- the item's columns: their rows and the queries, operand of S^T ----------------------------------------------------
   constexpr int NQ = F::kF32 ? F::NK : D / 32;
   f32x4 qf[F::kF32 ? NB : 1][F::kF32 ? NQ : 1];
   bf16x8 qb[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kQParts][F::kF32 ? 1 : NQ];
-  int row[NB];                                                 // of the group
-  auto load_queries = [&](const place &p, int (&row)[NB]) {
+  struct columns { int row[NB]; uint32_t mask[NB][2]; };       // rows of the group, the first two words of their masks
+  columns col;
+  auto load_queries = [&](const place &p, columns &col) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // (columns past the last repeat it: nothing of them is stored)
       const int m = min(p.tile * F::TC + (wc * NB + nb) * 16 + l16, p.k.rows * G - 1);
-      row[nb] = m / G;
-      const T *q = (const T *)a.q + ((size_t)(p.k.first + row[nb]) * a.p.Hq + p.head * G + (m - row[nb] * G)) * D;
+      const int j = m / G;
+      col.row[nb] = j;
+      col.mask[nb][0] = col.mask[nb][1] = 0;
+      if (a.mask) {
+        const int *w = a.mask + (size_t)(p.k.first + j) * a.mask_words;
+        col.mask[nb][0] = (uint32_t)w[0];
+        if (a.mask_words > 1) col.mask[nb][1] = (uint32_t)w[1];
+      }
+      const T *q = (const T *)a.q + ((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (m - j * G)) * D;
       if constexpr (F::kF32) {
 #pragma unroll
         for (int i = 0; i < NQ; ++i) qf[nb][i] = *reinterpret_cast<const f32x4 *>(q + 16 * i + 4 * lg);
@@ -274,30 +330,50 @@ tree_attention_kernel(tree_args a) {
     odd = false;
   };
 
-  // Bits of the lane's slots (t0 .. t0 + NS - 1 of the tree; committed ones below 0) that row j sees.
-  auto seen_slots = [&](const place &p, int t0, int j) -> uint32_t {
+  // Bits of the lane's slots (t0 .. t0 + NS - 1 of the tree; committed ones below 0) that the row of block nb's column sees.
+  auto seen_slots = [&](const place &p, int t0, int nb) -> uint32_t {
     constexpr uint32_t kAll = (1u << F::NS) - 1;
     if (t0 + F::NS <= 0) return kAll;
     const int top = p.k.end - p.k.len - t0;                    // slots in front of the tree's end
     uint32_t bits;
     if (a.mask) {
       const int lo = max(t0, 0), word = lo >> 5;
-      const int *w = a.mask + (size_t)(p.k.first + j) * a.mask_words;
-      const uint64_t two = (word < a.mask_words ? (uint64_t)(uint32_t)w[word] : 0) | (word + 1 < a.mask_words ? (uint64_t)(uint32_t)w[word + 1] << 32 : 0);
-      bits = (uint32_t)(two >> (lo & 31));
+      uint32_t w0, w1;
+      if (a.mask_words <= 2) {
+        w0 = word == 0 ? col.mask[nb][0] : word == 1 ? col.mask[nb][1] : 0u;
+        w1 = word == 0 ? col.mask[nb][1] : 0u;
+      } else {
+        const int *w = a.mask + (size_t)(p.k.first + col.row[nb]) * a.mask_words;
+        w0 = word < a.mask_words ? (uint32_t)w[word] : 0u;
+        w1 = word + 1 < a.mask_words ? (uint32_t)w[word + 1] : 0u;
+      }
+      bits = (uint32_t)(((uint64_t)w1 << 32 | w0) >> (lo & 31));
       if (t0 < 0) bits = (bits << -t0) | ((1u << -t0) - 1);
     } else {
-      const int n = j + 1 - t0;
+      const int n = col.row[nb] + 1 - t0;
       bits = n >= F::NS ? kAll : n <= 0 ? 0u : (1u << n) - 1;
     }
     return bits & (top >= F::NS ? kAll : top <= 0 ? 0u : (1u << top) - 1);
   };
 
-  // One slab: `cur` is in the registers, `next` is asked for meanwhile.  MASKED: it reaches behind the committed slots, or does not exist.
-  // Loads come back in order: the next item's queries are asked for in front of its first K, so that a wait for that K is one for them.
-  auto work = [&](auto with_mask, const where &cur, const where &next, const place &p, const place *to) {
-    constexpr bool MASKED = decltype(with_mask)::value;
-    int row_next[NB];
+  // One slab, n slots of it, in the registers or in LDS; `next`, for the registers, is asked for meanwhile.
+  // Loads come back in order: the next item's queries (of `to`) are asked for in front of its first K, so that a wait for that K is one for them.
+  const int key = key_of(8 * (l16 >> 2) + (l16 & 3)), krow = (8 * (l16 >> 2) + (l16 & 3)) * F::kRow;
+  auto work = [&](int n, const where &next, uint32_t stage, const place &p, const place &to, bool another) {
+    const bool masked = n < SK || slot_of(p) + SK > p.k.len;   // (uniform) it reaches behind the committed slots, or does not exist
+    columns col_next;
+    const unsigned char *slab = lds + stage * F::kStage + wsl * F::kSlab;
+    auto k_at = [&](int b, int i) {
+      if constexpr (F::kLds) return *reinterpret_cast<const uint4 *>(slab + krow + (((4 * i + lg) ^ key) << 4) + 4 * b * F::kRow);
+      else return sk[b][i];
+    };
+    if constexpr (F::kLds && Q8) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        ks[b] = *reinterpret_cast<const f32x4 *>(slab + F::kScales + 32 * lg + 16 * b);
+        vs[b] = *reinterpret_cast<const f32x4 *>(slab + F::kScales + 256 + 32 * lg + 16 * b);
+      }
+    }
     f32x4 acc[NB][F::KB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -306,7 +382,7 @@ tree_attention_kernel(tree_args a) {
     if constexpr (F::kF32) {
 #pragma unroll
       for (int i = 0; i < F::NK; ++i) {
-        const f32x4 kf = __builtin_bit_cast(f32x4, sk[0][i]);
+        const f32x4 kf = __builtin_bit_cast(f32x4, k_at(0, i));
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -316,10 +392,11 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
       for (int i = 0; i < F::NK; ++i)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int b = 0; b < F::KB; ++b) {
+          const uint4 kk = k_at(b, i);
 #pragma unroll
-          for (int b = 0; b < F::KB; ++b) {
-            const uint32_t x[2] = {u ? sk[b][i].z : sk[b][i].x, u ? sk[b][i].w : sk[b][i].y};
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t x[2] = {u ? kk.z : kk.x, u ? kk.w : kk.y};
             const bf16x8 kf = codes8(x);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -327,6 +404,7 @@ tree_attention_kernel(tree_args a) {
               for (int k = 0; k < F::kQParts; ++k)
                 acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][k][2 * i + u], acc[nb][b], 0, 0, 0);
           }
+        }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -335,37 +413,48 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
       for (int i = 0; i < F::NK; ++i)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int b = 0; b < F::KB; ++b) {
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, k_at(b, i));
 #pragma unroll
-          for (int b = 0; b < F::KB; ++b)
-            acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, sk[b][i]), qb[nb][0][i], acc[nb][b], 0, 0, 0);
+          for (int nb = 0; nb < NB; ++nb) acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][0][i], acc[nb][b], 0, 0, 0);
+        }
     }
+    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
+    if (another) load_queries(to, col_next);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (MASKED) {
-      if (to) load_queries(*to, row_next);
-      __builtin_amdgcn_sched_barrier(0);
-    }
     load_k(next);
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
+    if constexpr (F::kLds) {
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i) {
+        typedef uint32_t words __attribute__((ext_vector_type(F::kVWords)));
+        const words y = *reinterpret_cast<const words *>(slab + F::kHalf + (F::NS * lg + i) * F::kRow + 4 * F::kVWords * l16);
+#pragma unroll
+        for (int u = 0; u < F::kVWords; ++u) sv[i][0][u] = y[u];
+      }
+    }
     uint32_t vis[NB];
     float top[NB];
     bool far = false;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      vis[nb] = ~0u;
-      if constexpr (MASKED) {
-        vis[nb] = cur.n <= 0 ? 0u : seen_slots(p, slot_of(p) + F::NS * lg - p.k.len, row[nb]);
+    for (int nb = 0; nb < NB; ++nb) vis[nb] = ~0u;
+    if (masked) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        vis[nb] = n <= 0 ? 0u : seen_slots(p, slot_of(p) + F::NS * lg - p.k.len, nb);
 #pragma unroll
         for (int i = 0; i < F::NS; ++i)
           if (!(vis[nb] >> i & 1)) acc[nb][i >> 2][i & 3] = -INFINITY;
-        if (vis[nb]) seen |= 1 << nb;
       }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if (vis[nb]) seen |= 1 << nb;
       top[nb] = acc[nb][0][0];
 #pragma unroll
       for (int i = 1; i < F::NS; ++i) top[nb] = fmaxf(top[nb], acc[nb][i >> 2][i & 3]);
       far |= fmaf(top[nb], a.scale, -m[nb]) > 8.f;
     }
-    if constexpr (!MASKED) seen = (1 << NB) - 1;
     if (__builtin_expect(__any(far), 0)) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -393,7 +482,7 @@ tree_attention_kernel(tree_args a) {
       }
       if constexpr (Q8) {
 #pragma unroll
-        for (int i = 0; i < F::NS; ++i) w[i] = !MASKED || vis[nb] >> i & 1 ? w[i] * vs[i >> 2][i & 3] : 0.f;
+        for (int i = 0; i < F::NS; ++i) w[i] = vis[nb] >> i & 1 ? w[i] * vs[i >> 2][i & 3] : 0.f;
       }
       if constexpr (F::kF32) {
 #pragma unroll
@@ -416,24 +505,39 @@ tree_attention_kernel(tree_args a) {
         }
       }
     }
-    if constexpr (MASKED && !Q8) {
+    if constexpr (!Q8) {
+      if (masked) {
+        uint32_t bad = 0;                                      // the top bit of a half (bf16) or of all: an exponent of ones
 #pragma unroll
-      for (int i = 0; i < F::NS; ++i) {
-        const bool none = F::NS * lg + i >= cur.n;             // behind the tree: anything
-        const bool drafted = slot_of(p) + F::NS * lg + i >= p.k.len;      // (every row sees the committed ones)
+        for (int i = 0; i < F::NS; ++i) {
+          const bool none = F::NS * lg + i >= n;               // behind the tree: anything
 #pragma unroll
-        for (int j = 0; j < F::NP; ++j)
+          for (int j = 0; j < F::NP; ++j)
 #pragma unroll
-          for (int u = 0; u < F::kVWords; ++u) {
-            uint32_t x = none ? 0u : sv[i][j][u];
-            if constexpr (sizeof(T) == 4) {
-              if (drafted && (x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
-            } else {
-              if (drafted && (x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
-              if (drafted && (x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+            for (int u = 0; u < F::kVWords; ++u) {
+              if (none) sv[i][j][u] = 0u;
+              bad |= sizeof(T) == 4 ? (sv[i][j][u] & 0x7f800000u) + 0x00800000u : (sv[i][j][u] & 0x7f807f80u) + 0x00800080u;
             }
-            sv[i][j][u] = x;
+        }
+        if (__builtin_expect(__any(bad & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)), 0)) {
+#pragma unroll
+          for (int i = 0; i < F::NS; ++i) {
+            if (slot_of(p) + F::NS * lg + i < p.k.len) continue;               // (every row sees the committed ones)
+#pragma unroll
+            for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+              for (int u = 0; u < F::kVWords; ++u) {
+                uint32_t x = sv[i][j][u];
+                if constexpr (sizeof(T) == 4) {
+                  if ((x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
+                } else {
+                  if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+                  if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+                }
+                sv[i][j][u] = x;
+              }
           }
+        }
       }
     }
     if constexpr (F::kF32) {
@@ -462,36 +566,40 @@ tree_attention_kernel(tree_args a) {
           for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[nb][k], o[nb][c], 0, 0, 0);
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
     load_v(next);
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (MASKED) {
-      if (to)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) row[nb] = row_next[nb];
-    }
+    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
+    if (another) col = col_next;
   };
 
-  // Rare: the values that are not finite, of the tree's slots that row j sees, into coordinates d .. d + 3 (of several pieces, each adds them all).
-  auto add_odd = [&](const place &p, int j, int d, f32x4 &sum) {
-    for (int slot = p.k.len; slot < p.k.end; ++slot) {
-      const int page = a.p.table[(size_t)p.k.req * a.p.max_pages + (slot >> a.p.page_shift)], t = slot - p.k.len;
-      if (page < 0 || page >= a.p.n_pages) continue;
-      if (a.mask ? !(a.mask[(size_t)(p.k.first + j) * a.mask_words + (t >> 5)] >> (t & 31) & 1) : t > j) continue;
-      const T *v = (const T *)(a.p.v_pool + ((size_t)page * Hkv + p.head) * head_bytes) + (size_t)(slot & ((1 << a.p.page_shift) - 1)) * D + d;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float x = (float)v[u];
-        if (!(fabsf(x) < INFINITY)) sum[u] += x;
+  // Rare: the values that are not finite, of the tree's slots that a column's row sees, decide its result there, whatever the sums are (of
+  // several pieces each gets them all).  A wave's columns once more, after they have been written.
+  auto write_odd = [&](const place &p, bool whole, int slot) {
+    for (int e = 0; e < NB * 16 * D / 64; ++e) {
+      const int in = (wc * NB + e / (D / 4)) * 16 + l16, at = p.tile * F::TC + in, d = e % (D / 4) * 4 + lg;
+      if (at >= p.k.rows * G) continue;
+      const int j = at / G;
+      float sum = 0.f;
+      for (int s = p.k.len; s < p.k.end; ++s) {
+        const int page = a.p.table[(size_t)p.k.req * a.p.max_pages + (s >> a.p.page_shift)], t = s - p.k.len;
+        if (page < 0 || page >= a.p.n_pages) continue;
+        if (a.mask ? !(a.mask[(size_t)(p.k.first + j) * a.mask_words + (t >> 5)] >> (t & 31) & 1) : t > j) continue;
+        const T *v = (const T *)(a.p.v_pool + ((size_t)page * Hkv + p.head) * head_bytes) + (size_t)(s & ((1 << a.p.page_shift) - 1)) * D;
+        const float x = (float)v[d];
+        if (!(fabsf(x) < INFINITY)) sum += x;
       }
+      if (fabsf(sum) < INFINITY) continue;
+      if (whole) ((T *)a.out)[((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D + d] = (T)sum;
+      else a.part_o[((size_t)slot * F::TC + in) * D + d] = sum;
     }
   };
 
   // ---- an item, or this workgroup's part of one, is done: join the waves that share columns ---------------------------------
-  auto finish = [&](const place &p, bool begins, bool ends) {
+  // Every wave brings its sums to the columns' common maximum; then half of the waves add those of the other half to their own, block by block as
+  // the registers hold them, until one wave of each has all.  (Slabs through LDS: in the stage that has just been used.)
+  auto finish = [&](const place &p, bool begins, bool ends, uint32_t stage) {
     const bool whole = begins && ends;
-    const int slot = 2 * w + (begins ? 1 : 0);
-    const int some_odd = __any(odd);
+    const int slot = 2 * w + (begins ? 1 : 0), some_odd = __any(odd);
     if (lane == 0) odd_waves[wave] = some_odd;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -500,112 +608,161 @@ tree_attention_kernel(tree_args a) {
       int any = seen >> nb & 1;
       any |= __shfl_xor(any, 16);
       any |= __shfl_xor(any, 32);
-      if (lg == 0) { ml[wave][l16] = make_float2(m[nb], l[nb]); sees[wave][l16] = any; }
-      A3_LDS_BARRIER();
-      float top = -INFINITY;
+      if (lg == 0) { ml[nb][wave][l16] = make_float2(m[nb], l[nb]); sees[nb][wave][l16] = any; }
+    }
+    A3_LDS_BARRIER();
+    float M[NB], L[NB];
+    int some[NB], odd_any = 0;
 #pragma unroll
-      for (int x = 0; x < WS; ++x) top = fmaxf(top, ml[x * WC + wc][l16].x);
-      const float f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - top);
+    for (int x = 0; x < W; ++x) odd_any |= odd_waves[x];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+    for (int nb = 0; nb < NB; ++nb) {
+      M[nb] = -INFINITY;
+      L[nb] = 0.f;
+      some[nb] = 0;
 #pragma unroll
-        for (int j = 0; j < F::NP; ++j)
+      for (int x = 0; x < WS; ++x) M[nb] = fmaxf(M[nb], ml[nb][x * WC + wc][l16].x);
 #pragma unroll
-          for (int c = 0; c < F::E; c += 4) {
-            const int b = j * F::E + c;
-            *reinterpret_cast<f32x4 *>(&os[wave][l16][16 * F::E * j + F::E * (4 * lg + r) + c]) =
-                f32x4{o[nb][b][r], o[nb][b + 1][r], o[nb][b + 2][r], o[nb][b + 3][r]} * f;
-          }
-      A3_LDS_BARRIER();
-      for (int e = tid; e < WC * 16 * (D / 4); e += 64 * W) {
-        const int col = e / (D / 4), d = 4 * (e % (D / 4)), cw = col >> 4, ci = col & 15;
-        const int in = (cw * NB + nb) * 16 + ci, at = p.tile * F::TC + in;   // its number in the item, and among the group's columns
+      for (int x = 0; x < WS; ++x) {
+        const float2 y = ml[nb][x * WC + wc][l16];
+        L[nb] += y.x == -INFINITY ? 0.f : y.y * __builtin_amdgcn_exp2f(y.x - M[nb]);
+        some[nb] |= sees[nb][x * WC + wc][l16];
+      }
+      const float f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - M[nb]);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
+    }
+    constexpr int kAtOnce = F::kAtOnce;
+    f32x4 *room = reinterpret_cast<f32x4 *>(lds + (F::kLds ? stage * F::kStage : 0));
+#pragma unroll
+    for (int half = WS / 2; half >= 1; half /= 2)
+#pragma unroll
+      for (int b0 = 0; b0 < F::kBlocks; b0 += kAtOnce) {
+        if (wsl >= half && wsl < 2 * half)
+#pragma unroll
+          for (int b = 0; b < kAtOnce; ++b) room[(((wsl - half) * WC + wc) * kAtOnce + b) * 64 + lane] = o[(b0 + b) / (D / 16)][(b0 + b) % (D / 16)];
+        A3_LDS_BARRIER();
+        if (wsl < half)
+#pragma unroll
+          for (int b = 0; b < kAtOnce; ++b) o[(b0 + b) / (D / 16)][(b0 + b) % (D / 16)] += room[((wsl * WC + wc) * kAtOnce + b) * 64 + lane];
+        A3_LDS_BARRIER();
+      }
+    if (wsl == 0) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int in = (wc * NB + nb) * 16 + l16, at = p.tile * F::TC + in;  // the column's number in the item, and among the group's
         if (at >= p.k.rows * G) continue;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float M = -INFINITY, L = 0.f;
-        int some = 0;
-#pragma unroll
-        for (int x = 0; x < WS; ++x) {
-          sum += *reinterpret_cast<const f32x4 *>(&os[x * WC + cw][ci][d]);
-          M = fmaxf(M, ml[x * WC + cw][ci].x);
-          some |= sees[x * WC + cw][ci];
-        }
-#pragma unroll
-        for (int x = 0; x < WS; ++x) {
-          const float2 y = ml[x * WC + cw][ci];
-          L += y.x == -INFINITY ? 0.f : y.y * __builtin_amdgcn_exp2f(y.x - M);
-        }
         const int j = at / G;
-        if constexpr (!Q8) {
-          int odd_any = 0;
+        T *out = (T *)a.out + ((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D;
+        float *part = a.part_o + ((size_t)slot * F::TC + in) * D;
 #pragma unroll
-          for (int x = 0; x < W; ++x) odd_any |= odd_waves[x];
-          if (__builtin_expect(odd_any, 0)) add_odd(p, j, d, sum);
-        }
-        if (whole) {
-          typedef T vec4 __attribute__((ext_vector_type(4)));
-          vec4 y;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) y[u] = (T)(some ? sum[u] / L : 0.f);
-          *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D + d) = y;
-        } else {
-          *reinterpret_cast<f32x4 *>(a.part_o + ((size_t)slot * F::TC + in) * D + d) = sum;
-          if (d == 0) a.part_ml[(size_t)slot * F::TC + in] = make_float2(M, some ? L : -1.f);
+          for (int c = 0; c < D / 16; c += 4) {
+            const int d = 16 * F::E * (c / F::E) + F::E * (4 * lg + r) + c % F::E;
+            f32x4 sum = {o[nb][c][r], o[nb][c + 1][r], o[nb][c + 2][r], o[nb][c + 3][r]};
+            if (whole) {
+              typedef T vec4 __attribute__((ext_vector_type(4)));
+              vec4 y;
+#pragma unroll
+              for (int u = 0; u < 4; ++u) y[u] = (T)(some[nb] ? sum[u] / L[nb] : 0.f);
+              *reinterpret_cast<vec4 *>(out + d) = y;
+            } else {
+              *reinterpret_cast<f32x4 *>(part + d) = sum;
+            }
+          }
+        if (!whole && lg == 0) a.part_ml[(size_t)slot * F::TC + in] = make_float2(M[nb], some[nb] ? L[nb] : -1.f);
+      }
+      if constexpr (!Q8) {
+        if (__builtin_expect(odd_any, 0)) {
+          __builtin_amdgcn_s_waitcnt(0);                       // behind the other lanes' stores to the same rows
+          write_odd(p, whole, slot);
         }
       }
-      A3_LDS_BARRIER();
     }
   };
 
   // ---- the run of steps: of every item first those whose slots are all committed ------------------------------------------
-  where cur = find(now);
-  load_queries(now, row);
-  __builtin_amdgcn_sched_barrier(0);
-  load_k(cur);
-  __builtin_amdgcn_sched_barrier(0);
-  load_v(cur);
-  __builtin_amdgcn_sched_barrier(0);
-  clear();
-  for (int left = n_steps; left > 0;) {                        // an item, or the part of it that is in this run
-    const bool begins = now.step == 0;
-    const int here = min(now.k.steps - now.step, left), begun = now.step;
-    const int plain = max(0, min(now.k.len / F::kStep, begun + here - 1) - begun);       // (the last one of the run's part is not among them)
-    int i = 0, page = page_at(now, slot_of(now) + F::kStep);
-    for (; i < plain && cur.n >= SK; ++i) {                    // (up to a page that does not exist)
-      const int slot = slot_of(now) + F::kStep, page2 = page_at(now, slot + F::kStep);     // a step ahead: a scalar load takes a while
-      const where next = on_page(now, slot, page);
-      work(std::false_type{}, cur, next, now, nullptr);
-      cur = next;
-      page = page2;
-      ++now.step;
-    }
-    for (; i < here; ++i) {
-      place p = now;
-      if (i + 1 < here) ++p.step;
-      else if (left > here) advance(p);
-      const where next = i + 1 < here || left > here ? find(p) : where{0, 0, 0};
-      work(std::true_type{}, cur, next, now, i + 1 == here && left > here ? &p : nullptr);
-      cur = next;
-      if (i + 1 < here) now = p;
-      else {
-        const bool ends = now.step == now.k.steps - 1;
-        finish(now, begins, ends);
-        if (begins && tid == 0) {
-          int pieces = 1;
-          if (!ends) {                                         // goes on in the workgroups behind: how many of them
-            // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
-            const int last = first + (n_steps - left) + now.k.steps - 1 - begun, fat = rest * (each + 1);
-            pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
-          }
-          if (a.by_item) a.cut[((size_t)now.g * Hkv + now.head) * a.tiles + now.tile] = make_int4(now.g, now.head, w, pieces);
-          else if (!ends) a.cut[w] = make_int4(now.g, now.head | now.tile << 16, w, pieces);
-        }
-        clear();
-        now = p;
+  // Everything that was asked for by now is there (the compiler's own waits would stand in the loops, and be for later loads too).
+  auto settle = [&]() {
+    if constexpr (F::kLds) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        asm volatile("" : "+v"(col.mask[nb][0]), "+v"(col.mask[nb][1]));
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) asm volatile("" : "+v"(qb[nb][0][i]));
       }
     }
-    left -= here;
+  };
+  constexpr int S = F::kLds ? F::kStages : 2;                  // through LDS: S - 1 steps ahead
+  place ahead = now;
+  int ahead_left = n_steps, ahead_page = page_at(ahead, slot_of(ahead)), queue[S];
+  auto look = [&]() {                                          // where the next slab lies (behind the run: the pool's start)
+    const where x = ahead_left > 0 ? on_page(ahead, slot_of(ahead), ahead_page) : where{0, 0, 0};
+    if (--ahead_left > 0) {
+      advance(ahead);
+      ahead_page = page_at(ahead, slot_of(ahead));             // used a step later: a scalar load takes a while
+    }
+    return x;
+  };
+  load_queries(now, col);
+  settle();
+  clear();
+  if constexpr (!F::kLds) {
+    const where x = look();
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(x);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(x);
+    __builtin_amdgcn_sched_barrier(0);
+    queue[0] = x.n;
   }
+  uint32_t stage = 0, to_stage = 0;
+  bool begins = now.step == 0;
+#pragma unroll 1
+  for (int t = F::kLds ? 1 - S : 0; t < n_steps; ++t) {
+    where next{0, 0, 0};
+    if constexpr (F::kLds) {
+      if (t >= 0) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::kPer * (S - 2)) : "memory");
+        A3_LDS_BARRIER();                                      // the step's slabs are there, and the stage before it is free
+      }
+      next = look();
+      dma(next, to_stage);
+      to_stage = to_stage + 1 == S ? 0 : to_stage + 1;
+#pragma unroll
+      for (int i = 0; i + 1 < S; ++i) queue[i] = queue[i + 1];
+      queue[S - 1] = next.n;
+      if (t < 0) continue;
+    } else {
+      next = look();
+    }
+    const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1, last = ends || !more;
+    place p = now;
+    if (!last) ++p.step;
+    else if (more) advance(p);
+    work(queue[0], next, stage, now, p, last && more);
+    if constexpr (!F::kLds) queue[0] = next.n;
+    if (last) {
+      finish(now, begins, ends, stage);
+      if (begins && tid == 0) {
+        int pieces = 1;
+        if (!ends) {                                           // goes on in the workgroups behind: how many of them
+          // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+          const int last = first + t + now.k.steps - 1 - now.step, fat = rest * (each + 1);
+          pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+        }
+        if (a.by_item) a.cut[((size_t)now.g * Hkv + now.head) * a.tiles + now.tile] = make_int4(now.g, now.head, w, pieces);
+        else if (!ends) a.cut[w] = make_int4(now.g, now.head | now.tile << 16, w, pieces);
+      }
+      begins = true;
+      clear();
+      settle();
+    }
+    now = p;
+    stage = stage + 1 == S ? 0 : stage + 1;
+  }
+  if constexpr (F::kLds) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the memory that the last loads go to is another workgroup's next)
 }
 
 // Joins the pieces of an item that is cut, kUnits columns' four coordinates a workgroup: of item blockIdx.x (by_item: few of them), or of
@@ -775,10 +932,19 @@ extern "C" a3_status a3_tree_attention(const a3_pages *P, const void *q, int n_g
     typedef decltype(elem) T;
     with_shape<T, d.value, q8.value>(plan.s, [&](auto form) {
       typedef decltype(form) F;
-      hipLaunchKernelGGL((tree_attention_kernel<F, T, d.value, q8.value>), dim3((unsigned)plan.shares), dim3(64 * F::W), 0, (hipStream_t)stream, a);
+      auto kern = tree_attention_kernel<F, T, d.value, q8.value>;
+      static a3_once_per_device lds_once;
+      if (F::kLdsBytes > 65536 && a3_once(lds_once, [&]() {
+            return hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, F::kLdsBytes);
+          }) != hipSuccess) {
+        s = a3_fail(A3_ERR_HIP, "a3_tree_attention: cannot raise the dynamic LDS limit");
+        return;
+      }
+      hipLaunchKernelGGL(kern, dim3((unsigned)plan.shares), dim3(64 * F::W), F::kLdsBytes, (hipStream_t)stream, a);
       hipLaunchKernelGGL((tree_join_kernel<T, d.value, F::TC>), join, dim3(kJoinThreads), 0, (hipStream_t)stream, a);
     });
   });
+  if (s != A3_OK) return s;
   A3_CHECK_LAUNCH("a3_tree_attention");
   return A3_OK;
 }
