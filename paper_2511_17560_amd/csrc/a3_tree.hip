@@ -10,38 +10,46 @@ struct tree_args {
   const int *start, *req, *len, *mask;
   int n_groups, n_rows, max_rows, mask_words;
   float scale;             // of the logits, in units of log 2
-  int shares, tiles, units;          // workgroups; most items of a (group, KV head); a workgroup of the join's columns' four coordinates
-  float *part_o;           // [2 * shares, columns, D] pieces: 2 w the one that began before run w, 2 w + 1 the one that goes on after it
+  int shares, tiles;       // workgroups; most items of a (group, KV head)
+  float *part_o;           // [2 * shares] pieces: 2 w the one that began before run w, 2 w + 1 the one that goes on after it; each the
+                           // accumulators of an item's columns as the waves hold them
   float2 *part_ml;         // [2 * shares, columns] (maximum, sum; sum < 0: nothing seen)
   int4 *cut;               // of run w: the item that goes on after it (group or -1, KV head and item of it, w, its pieces); with few items, of
   int by_item;             // each: the same, w the run that it begins in
 };
 
 // The rows of a group are packed with the query heads of a KV head: column m = row * G + head of it.  An item is 16 NB WC columns of one
-// (group, KV head): NB blocks of 16 a wave, WC waves beside each other; the other waves of the four take further slots.  A step of a workgroup
+// (group, KV head): NB blocks of 16 a wave, WC waves beside each other; the other waves take further slots.  A step of a workgroup
 // is WS SK slots, SK a wave: 32, or 16 with fp32 pages.  The steps of the call, groups first, then KV heads, then items, then slots, are cut
 // into as many runs, equal to one step, as there are workgroups, whatever the lengths are: every workgroup forms the running sum of the
 // groups' steps itself (they live on the device).  An item that ends up whole in one workgroup is finished there; of one that is cut, every
 // workgroup leaves a piece in ws and a second kernel joins them in the order of the slots.
 //
-// Matrix instructions, operands straight from memory to registers: S^T = K Q^T puts 16 columns beside the slots (rows), and O^T = V^T P^T
-// wants of a lane 8 consecutive slots of one coordinate.
+// Matrix instructions: S^T = K Q^T puts 16 columns beside the slots (rows), and O^T = V^T P^T wants of a lane 8 consecutive slots of one
+// coordinate.
 //   - which slot a row of S^T is, is free: row i of block b is slot 8 (i / 4) + 4 b + i % 4, so that the weights a lane (column l16, lane group
 //     lg) gets are those of slots 8 lg .. 8 lg + 7, the P^T operand as it stands
 //   - which coordinate a row of O^T is, is free too: row l16 of block c is coordinate E l16 + c, so that a lane loads E consecutive
 //     coordinates of its 8 slots and the V^T operands are a transposition inside the lane, formed once for all NB blocks of columns
 //   - the weights go in as a sum of two bf16 (three where rows are fp32), so that the only rounding of bf16 size is the output's; each
-//     part but the last is cut off below the weight, so that none is zero or negative and an infinite value stays one
+//     part but the last is cut off, not rounded, so that a remainder is never negative
 //   - codes of 8-bit pages are whole numbers that bf16 holds; the scales join the logits and the weights
-// The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float).
+// The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float), and to a whole
+// number: what moves sums, and weights that wait, is then a power of two.
 //
-// One slab of registers is enough to have the next one on its way: K of the next is asked for as soon as the products with this one's have
-// read it, V as soon as its operands are formed, so that each is under way for most of a step.  Nothing of that is conditional (a slab that
-// does not exist is read from the pool's start and counts nothing): a wait for V would otherwise have to be one for the next K too.
+// Up to 32 columns (and fp32 rows): K and V straight from memory to registers.  One slab of registers is enough to have the next one on its
+// way: K of the next is asked for as soon as the products with this one's have read it, V as soon as its operands are formed, so that each
+// is under way for most of a step.  Nothing of that is conditional (a slab that does not exist is read from the pool's start and counts
+// nothing): a wait for V would otherwise have to be one for the next K too.
+//
+// More columns: the 16 slots that a quarter wave reads of K lie in as many lines, which occupies the address units four times as long as
+// whole lines do, once for each of WC waves.  There K and V come through LDS, in whole lines, once for all of them, four steps deep, V two
+// steps behind K.  The work is staggered: while the weights of step i are formed on the vector unit, the matrix unit multiplies those of
+// step i - 1 with V and K of step i + 1 with Q, so that neither waits for the other.
 //
 // A lane's eight slots of a column are eight bits of the row's mask.  Only slabs that reach behind the committed slots look at it: a slot that
 // is not seen has weight 0.  0 times a value that is not finite would be NaN in the rows that do not see it, so there such values are taken out
-// of the product and, where there are any, added to the rows that see them when the item is put together (its result there is not finite
+// of the product, and where there are any the rows that see them get them when the item is put together (the result there is not finite
 // whatever the weights are).
 template <typename T, int D, bool Q8, int NB_, int WC_, int W_>
 struct tree_form {
@@ -58,15 +66,16 @@ struct tree_form {
   static constexpr int TC = 16 * NB * WC;                      // columns of an item
   static constexpr int kStep = WS * SK;
   static constexpr bool kOnce = WC_ == 1;                      // a cache is read once: nontemporal
-  // Eight waves with bf16 rows: slabs through LDS, a ring of kStages steps.
-  static constexpr bool kLds = W_ == 8 && sizeof(T) == 2;
-  static constexpr int kHalf = SK * kRow, kScales = 2 * kHalf, kSlab = kScales + (Q8 ? 512 : 0);   // K, V, scales of both (256 bytes each)
-  static constexpr int kStage = WS * kSlab, kFit = 131072 / kStage, kStages = kFit > 4 ? 4 : kFit;
-  static constexpr int kLoads = kRow / 16 / WC, kPer = kLoads + (Q8 ? 1 : 0);  // direct-to-LDS loads of a wave and step
   static constexpr int kBlocks = NB * D / 16;                  // accumulator blocks of a wave
-  static constexpr int kRoom = (kLds ? kStage : 0) / (W_ / 2) / 1024;          // of which the stage at hand has room for so many, of half the waves
-  static constexpr int kAtOnce = !kLds || kRoom >= kBlocks ? kBlocks : kRoom >= kBlocks / 2 ? kBlocks / 2 : kRoom >= kBlocks / 4 ? kBlocks / 4 : kBlocks / 8;
-  static constexpr int kLdsBytes = kLds ? kStages * kStage : WS > 1 ? W_ / 2 * kBlocks * 1024 : 16;
+  static constexpr bool kLds = sizeof(T) == 2 && WC_ > 1;      // through LDS: rings of K and V, four steps each, and of scales, eight steps
+  static constexpr int kHalf = SK * kRow, kKV = WS * kHalf, kScaleAt = 8 * kKV;
+  static constexpr int kLoads = kRow / 32 >= WC ? kRow / 32 / WC : 1;          // direct-to-LDS loads of a wave, of K and of V, a step
+  static constexpr int kPer = 2 * kLoads + (Q8 ? 1 : 0);
+  // blocks that half of the waves exchange at once, when waves are joined: in room of their own, or in two steps of the ring of V
+  static constexpr int kRoom = kKV / 1024 / (W_ / 4 > 0 ? W_ / 4 : 1);
+  static constexpr int kAtOnce = !kLds || kRoom >= kBlocks ? kBlocks : kRoom;
+  static constexpr int kLdsBytes = kLds ? kScaleAt + (Q8 ? 16 * WS * 256 : 0) : WS > 1 ? W_ / 2 * kBlocks * 1024 : 16;
+  static constexpr int kWaves = kLds ? 1 : kF32 && D == 128 && NB_ == 2 ? 1 : Q8 && sizeof(T) == 4 && D == 128 && NB_ == 2 ? 1 : 2;   // a SIMD
 };
 
 // Steps of a group's item, and items of its KV heads (0 steps: nothing of the group is written).
@@ -85,11 +94,11 @@ __device__ __forceinline__ group_work work_of(const tree_args &a, int start, int
 }
 
 template <class F, typename T, int D, bool Q8>
-__global__ void __launch_bounds__(64 * F::W, F::W == 4 && !(sizeof(T) == 4 && D == 128 && F::NB == 2) ? 2 : 1)
+__global__ void __launch_bounds__(64 * F::W, F::W == 4 ? F::kWaves : 1)
 tree_attention_kernel(tree_args a) {
   constexpr int SK = F::SK, NB = F::NB, WS = F::WS, WC = F::WC, W = F::W;
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ int scan[2][W], found[2], odd_waves[W];
+  __shared__ int scan[2][W], found[6], odd_waves[W];
   __shared__ float2 ml[NB][W][16];
   __shared__ int sees[NB][W][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -97,16 +106,20 @@ tree_attention_kernel(tree_args a) {
 
   // ---- this workgroup's run of steps -----------------------------------------------------------------------
   // Up to as many groups as threads: one thread a group.  More: the groups' sum first, then blocks of them up to the one the run begins in.
-  auto steps_of = [&](int g) {
-    if (g >= a.n_groups) return 0;
-    const group_work w = work_of<F::kStep, F::TC>(a, a.start[g], a.start[g + 1], a.req ? a.req[g] : g, a.len[g]);
+  struct bounds { int start, stop, req, len; };
+  auto bounds_of = [&](int g) {
+    return g < a.n_groups ? bounds{a.start[g], a.start[g + 1], a.req ? a.req[g] : g, a.len[g]} : bounds{0, 0, 0, 0};
+  };
+  auto steps_of = [&](const bounds &b) {
+    const group_work w = work_of<F::kStep, F::TC>(a, b.start, b.stop, b.req, b.len);
     return w.steps * w.tiles;
   };
-  int st = steps_of(tid), incl = a3_wave_prefix(st), sum = incl;
+  bounds mine = bounds_of(tid);
+  int st = steps_of(mine), incl = a3_wave_prefix(st), sum = incl;
   if (a.n_groups > 64 * W) {
-    int mine = st;
-    for (int g = tid + 64 * W; g < a.n_groups; g += 64 * W) mine += steps_of(g);
-    sum = a3_wave_prefix(mine);
+    int all = st;
+    for (int g = tid + 64 * W; g < a.n_groups; g += 64 * W) all += steps_of(bounds_of(g));
+    sum = a3_wave_prefix(all);
   }
   if (lane == 63) { scan[0][wave] = sum; scan[1][wave] = incl; }
   __syncthreads();
@@ -124,12 +137,20 @@ tree_attention_kernel(tree_args a) {
     int base = before;
     for (int i = 0; i < wave; ++i) base += scan[1][i];
     const int lo = (base + incl - st) * Hkv, hi = (base + incl) * Hkv;
-    if (first >= lo && first < hi) { found[0] = g0 + tid; found[1] = first - lo; }
+    if (first >= lo && first < hi) {
+      found[0] = g0 + tid;
+      found[1] = first - lo;
+      found[2] = mine.start;
+      found[3] = mine.stop;
+      found[4] = mine.req;
+      found[5] = mine.len;
+    }
 #pragma unroll
     for (int i = 0; i < W; ++i) before += scan[1][i];
     if (before * Hkv > first) break;
     g0 += 64 * W;
-    st = steps_of(g0 + tid);
+    mine = bounds_of(g0 + tid);
+    st = steps_of(mine);
     incl = a3_wave_prefix(st);
     __syncthreads();
     if (lane == 63) scan[1][wave] = incl;
@@ -139,13 +160,11 @@ tree_attention_kernel(tree_args a) {
 
   // ---- where the workgroup stands: a step of an item (all scalar) --------------------------------------------------
   struct place { int g, head, tile, step; group_work k; };
-  auto enter = [&](place &p) {
-    p.k = work_of<F::kStep, F::TC>(a, scalar_at(a.start, p.g), scalar_at(a.start, p.g + 1), a.req ? scalar_at(a.req, p.g) : p.g, scalar_at(a.len, p.g));
-  };
+  auto at_lds = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
   place now;
-  now.g = __builtin_amdgcn_readfirstlane(found[0]);
-  enter(now);
-  const int inside = __builtin_amdgcn_readfirstlane(found[1]);
+  now.g = at_lds(0);
+  now.k = work_of<F::kStep, F::TC>(a, at_lds(2), at_lds(3), at_lds(4), at_lds(5));
+  const int inside = at_lds(1);
   now.head = inside / (now.k.steps * now.k.tiles);
   now.tile = (inside - now.head * now.k.steps * now.k.tiles) / now.k.steps;
   now.step = inside % now.k.steps;
@@ -158,38 +177,63 @@ tree_attention_kernel(tree_args a) {
     p.head = 0;
     do {
       if (++p.g >= a.n_groups) return;                         // (only behind the last step of all)
-      enter(p);
+      p.k = work_of<F::kStep, F::TC>(a, scalar_at(a.start, p.g), scalar_at(a.start, p.g + 1), a.req ? scalar_at(a.req, p.g) : p.g,
+                                     scalar_at(a.len, p.g));
     } while (p.k.steps == 0);
   };
+  auto slot_of = [&](const place &p) { return p.step * F::kStep + SK * wsl; };      // a wave's first slot
 
-  // ---- one slab of one wave in registers ------------------------------------------------------------------
+  // ---- the slabs that are asked for, ahead of the work -------------------------------------------------------------
+  // Page numbers come 64 at a time into the lanes of a register (one at a time, each is a load that the next thing waits for).
+  struct where { size_t block; int at, n; };                   // n: its slots up to the tree's end (<= 0: none of them counts)
   const size_t head_bytes = page_head_bytes(Q8 ? A3_PAGES_Q8 : A3_PAGES_PLAIN, sizeof(T), 1 << a.p.page_shift, D);
-  // (buffer loads: the page in four scalars, a lane's place in one register)
+  constexpr int kNoPages = -(1 << 30);
+  // What was asked for by now is there.  (The compiler's own waits would stand where the values are used, in the loops, and be for all
+  // later loads too: it does not know of the direct-to-LDS ones.)
+  auto wait_loads = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                        // vmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+  };
+  place ahead = now;
+  int ahead_left = n_steps, pages = 0, pages_from = kNoPages;
+  auto look = [&]() {                                          // (behind the run: the pool's start)
+    where x{0, 0, 0};
+    if (ahead_left > 0) {
+      const int slot = slot_of(ahead), last = (ahead.k.end - 1) >> a.p.page_shift, no = min(slot >> a.p.page_shift, last);
+      if ((uint32_t)(no - pages_from) >= 64u) {
+        pages = a.p.table[(size_t)ahead.k.req * a.p.max_pages + min(no + lane, last)];
+        wait_loads();                                          // (here, not in every step)
+        pages_from = no;
+      }
+      const int page = __builtin_amdgcn_readlane(pages, no - pages_from);
+      if (slot < ahead.k.end && page >= 0 && page < a.p.n_pages) {
+        x.block = ((size_t)page * Hkv + ahead.head) * head_bytes;
+        x.at = slot & ((1 << a.p.page_shift) - 1);
+        x.n = ahead.k.end - slot;
+      }
+      if (--ahead_left > 0) {
+        const int g = ahead.g;
+        advance(ahead);
+        if (ahead.g != g) pages_from = kNoPages;
+      }
+    }
+    return x;
+  };
+
+  // ---- one slab of one wave in registers: buffer loads, the page in four scalars, a lane's place in one register ---------------------
   const uint32_t koff = (SK == 16 ? l16 : 8 * (l16 >> 2) + (l16 & 3)) * F::kRow + 16 * lg;
   const uint32_t voff = (uint32_t)(F::NS * lg * F::kRow + F::kVWords * 4 * l16);
-  auto slot_of = [&](const place &p) { return p.step * F::kStep + SK * wsl; };
   uint4 sk[F::KB][F::NK];
   uint32_t sv[F::NS][F::NP][F::kVWords];
   f32x4 ks[Q8 ? 2 : 1], vs[Q8 ? 2 : 1];
-  struct where { size_t block; int at, n; };                   // n: its slots up to the tree's end (<= 0: none of them counts)
-  auto page_at = [&](const place &p, int slot) {               // its number; behind the tree any
-    return scalar_at(a.p.table, (size_t)p.k.req * a.p.max_pages + (min(slot, p.k.end - 1) >> a.p.page_shift));
-  };
-  auto on_page = [&](const place &p, int slot, int page) {
-    const bool none = slot >= p.k.end || page < 0 || page >= a.p.n_pages;
-    where x;
-    x.block = none ? 0 : ((size_t)page * Hkv + p.head) * head_bytes;
-    x.at = none ? 0 : slot & ((1 << a.p.page_shift) - 1);
-    x.n = none ? 0 : p.k.end - slot;
-    return x;
-  };
-  auto find = [&](const place &p) { return on_page(p, slot_of(p), page_at(p, slot_of(p))); };
   constexpr int kAux = F::kOnce ? 2 : 0;                       // nontemporal
   auto page_of = [&](const char *pool, const where &x) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pool) + x.block, 0, (int)head_bytes, 0x00020000);
   };
   auto load_k = [&](const where &x) {
-    if constexpr (F::kLds) return;
     const auto page = page_of(a.p.k_pool, x);
     const int at = x.at * F::kRow;
 #pragma unroll
@@ -204,7 +248,6 @@ tree_attention_kernel(tree_args a) {
     }
   };
   auto load_v = [&](const where &x) {
-    if constexpr (F::kLds) return;
     const auto page = page_of(a.p.v_pool, x);
     const int at = x.at * F::kRow;
 #pragma unroll
@@ -229,41 +272,59 @@ tree_attention_kernel(tree_args a) {
     }
   };
 
-  // Through LDS: the waves that share a slab bring equal parts of it, 1 KB a load, lane after lane 16 bytes.  16-byte piece c of slot s of K
-  // lies at place c ^ key(s) of its row, so that the 16 slots a quarter wave reads at one place lie in all 64 banks once.
+  // ---- through LDS: the waves that share a slab bring equal parts of it, 1 KB a load, lane after lane 16 bytes ------------------------
+  // 16-byte piece c of slot s of K lies at place c ^ key(s) of its row, so that the 16 slots a quarter wave reads at one place lie in all 64
+  // banks once.  Step i of a run has place i % 4 of the rings of K and V, i % 8 of those of scales.
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
-  constexpr int kPieces = F::kRow / 16, kRows = 1024 / F::kRow;         // pieces of a slot; slots of a load
+  constexpr int kPieces = F::kRow / 16, kRows = 1024 / F::kRow, kHalfLoads = F::kRow / 32;     // pieces of a slot; slots of a load; loads of a slab
   auto key_of = [&](int s) { return ((s >> 3 & 3) << 2 | (s & 3)) >> (F::kRow == 256 ? 0 : F::kRow == 128 ? 1 : 2); };
-  uint32_t dma_off[F::kLds ? F::kLoads : 1];
+  const int my_slot = 8 * (l16 >> 2) + (l16 & 3), my_key = key_of(my_slot);    // a lane's row of S^T in block 0 (4 more in block 1)
+  uint32_t dma_k[F::kLds ? F::kLoads : 1], dma_v[F::kLds ? F::kLoads : 1];
   if constexpr (F::kLds) {
 #pragma unroll
     for (int t = 0; t < F::kLoads; ++t) {
-      const int q = wc * F::kLoads + t, half = 2 * kPieces / 4;              // loads of K, then of V: kRow / 32 each
-      const int s = (q % half) * kRows + lane / kPieces, c = lane % kPieces;
-      dma_off[t] = (uint32_t)(s * F::kRow + 16 * (q < half ? c ^ key_of(s) : c));
+      const int s = (wc * F::kLoads + t) % kHalfLoads * kRows + lane / kPieces, c = lane % kPieces;
+      dma_k[t] = (uint32_t)(s * F::kRow + 16 * (c ^ key_of(s)));
+      dma_v[t] = (uint32_t)(s * F::kRow + 16 * c);
     }
   }
   // Inline assembly on purpose: the compiler then neither treats these as LDS writes (it would wait for all of them before every LDS
   // read) nor moves memory accesses across them; the waits for them are the explicit s_waitcnt below.
-  auto dma = [&](const where &x, uint32_t stage) {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const uint64_t pk = (uint64_t)a.p.k_pool + x.block, pv = (uint64_t)a.p.v_pool + x.block;
-    const u32x4 rk = {(uint32_t)pk, (uint32_t)(pk >> 32) & 0xffffu, (uint32_t)head_bytes, 0x00020000u};
-    const u32x4 rv = {(uint32_t)pv, (uint32_t)(pv >> 32) & 0xffffu, (uint32_t)head_bytes, 0x00020000u};
-    constexpr int half = F::kRow / 32;
-    const uint32_t to = lds_base + stage * F::kStage + wsl * F::kSlab, at = (uint32_t)x.at * F::kRow;
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  auto page_at = [&](const char *pool, const where &x) {
+    const uint64_t p = (uint64_t)pool + x.block;
+    return u32x4{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, (uint32_t)head_bytes, 0x00020000u};
+  };
+  auto dma = [&](u32x4 page, uint32_t off, uint32_t at, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(page), "s"(at) : "memory");
+  };
+  where behind[2] = {{0, 0, 0}, {0, 0, 0}};                    // the two steps whose K is asked for and whose V is not
+  int queue[5] = {0, 0, 0, 0, 0};                              // slots that count, of the step at hand and of those whose K is asked for
+  auto ask = [&](int i) {                                      // K of step i, V of step i - 2 (a wave has as many loads in every step)
+    const where x = look();
+    const u32x4 pk = page_at(a.p.k_pool, x), pv = page_at(a.p.v_pool, behind[0]);
+    const uint32_t to = lds_base + wsl * F::kHalf;
 #pragma unroll
-    for (int t = 0; t < F::kLoads; ++t) {
-      const int q = wc * F::kLoads + t;
-      const u32x4 r = q < half ? rk : rv;
-      const uint32_t m0 = __builtin_amdgcn_readfirstlane(to + (q < half ? 0 : F::kHalf) + (q % half) * 1024);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(m0), "v"(dma_off[t]), "s"(r), "s"(at) : "memory");
-    }
+    for (int t = 0; t < F::kLoads; ++t)
+      dma(pk, dma_k[t], (uint32_t)x.at * F::kRow, to + (i & 3) * F::kKV + (wc * F::kLoads + t) % kHalfLoads * 1024);
+#pragma unroll
+    for (int t = 0; t < F::kLoads; ++t)
+      dma(pv, dma_v[t], (uint32_t)behind[0].at * F::kRow, to + (4 + ((i + 2) & 3)) * F::kKV + (wc * F::kLoads + t) % kHalfLoads * 1024);
     if constexpr (Q8) {                                        // 64 scales, of which 32 are the slab's (behind the head's page: zeros)
-      const u32x4 r = wc & 1 ? rv : rk;
-      const uint32_t m0 = __builtin_amdgcn_readfirstlane(to + F::kScales + (wc & 1 ? 256 : 0)), sc = (uint32_t)(D << a.p.page_shift) + 4 * x.at;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(m0), "v"(4 * lane), "s"(r), "s"(sc) : "memory");
+      const u32x4 page = wc & 1 ? page_at(a.p.v_pool, x) : pk;
+      const uint32_t sc = (uint32_t)(D << a.p.page_shift) + 4 * x.at, at = lds_base + F::kScaleAt + ((wc & 1) * 8 + (i & 7)) * WS * 256 + wsl * 256;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(at), "v"(4 * lane), "s"(page), "s"(sc) : "memory");
     }
+    behind[0] = behind[1];
+    behind[1] = x;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) queue[q] = queue[q + 1];
+    queue[4] = x.n;
+  };
+  // All loads of this wave but those of the last two steps are done; then those of all waves.
+  auto arrive = [&]() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::kPer) : "memory");
+    A3_LDS_BARRIER();
   };
 
   // ---- the item's columns: their rows and the queries, operand of S^T ----------------------------------------------------
@@ -312,7 +373,6 @@ tree_attention_kernel(tree_args a) {
       }
     }
   };
-
   // ---- running state of the item --------------------------------------------------------------------------
   f32x4 o[NB][D / 16];
   float m[NB], l[NB];
@@ -328,6 +388,70 @@ tree_attention_kernel(tree_args a) {
     }
     seen = 0;
     odd = false;
+  };
+
+  // ---- parts of a step ----------------------------------------------------------------------------------------------
+  typedef f32x4 logits[NB][F::KB];
+  struct weights {                                             // bf16 parts, or (fp32 pages) as they are
+    bf16x8 b[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kPParts];
+    float f[F::kF32 ? NB : 1][F::kF32 ? 4 : 1];
+  };
+  struct slab_info { int slot, n; bool masked; };              // masked: it reaches behind the committed slots, or does not exist
+  auto info_of = [&](const place &p, int n) {
+    const int slot = slot_of(p);
+    return slab_info{slot, n, n < SK || slot + SK > p.k.len};
+  };
+
+  // S^T of step i (its logits but for the scale)
+  auto multiply_k = [&](logits &acc, int i) {
+    const unsigned char *slab = lds + (i & 3) * F::kKV + wsl * F::kHalf + my_slot * F::kRow;
+    auto k_at = [&](int b, int x) {
+      if constexpr (F::kLds) return *reinterpret_cast<const uint4 *>(slab + (((4 * x + lg) ^ my_key) << 4) + 4 * b * F::kRow);
+      else return sk[b][x];
+    };
+    if constexpr (F::kLds && Q8) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        ks[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (i & 7) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int b = 0; b < F::KB; ++b) acc[nb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < F::NK; ++x)
+#pragma unroll
+      for (int b = 0; b < F::KB; ++b) {
+        const uint4 kk = k_at(b, x);
+        if constexpr (F::kF32) {
+          const f32x4 kf = __builtin_bit_cast(f32x4, kk);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) acc[nb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[nb][x][e], acc[nb][0], 0, 0, 0);
+        } else if constexpr (Q8) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t two[2] = {u ? kk.z : kk.x, u ? kk.w : kk.y};
+            const bf16x8 kf = codes8(two);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int k = 0; k < F::kQParts; ++k)
+                acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][k][2 * x + u], acc[nb][b], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), qb[nb][0][x], acc[nb][b], 0, 0, 0);
+        }
+      }
+    if constexpr (Q8) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[nb][b] *= ks[b];
+    }
   };
 
   // Bits of the lane's slots (t0 .. t0 + NS - 1 of the tree; committed ones below 0) that the row of block nb's column sees.
@@ -355,101 +479,23 @@ tree_attention_kernel(tree_args a) {
     }
     return bits & (top >= F::NS ? kAll : top <= 0 ? 0u : (1u << top) - 1);
   };
-
-  // One slab, n slots of it, in the registers or in LDS; `next`, for the registers, is asked for meanwhile.
-  // Loads come back in order: the next item's queries (of `to`) are asked for in front of its first K, so that a wait for that K is one for them.
-  const int key = key_of(8 * (l16 >> 2) + (l16 & 3)), krow = (8 * (l16 >> 2) + (l16 & 3)) * F::kRow;
-  auto work = [&](int n, const where &next, uint32_t stage, const place &p, const place &to, bool another) {
-    const bool masked = n < SK || slot_of(p) + SK > p.k.len;   // (uniform) it reaches behind the committed slots, or does not exist
-    columns col_next;
-    const unsigned char *slab = lds + stage * F::kStage + wsl * F::kSlab;
-    auto k_at = [&](int b, int i) {
-      if constexpr (F::kLds) return *reinterpret_cast<const uint4 *>(slab + krow + (((4 * i + lg) ^ key) << 4) + 4 * b * F::kRow);
-      else return sk[b][i];
-    };
-    if constexpr (F::kLds && Q8) {
+  uint32_t vis[NB];                                            // of the step at hand, where it is masked
+  auto hide = [&](logits &acc, const place &p, const slab_info &in) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        ks[b] = *reinterpret_cast<const f32x4 *>(slab + F::kScales + 32 * lg + 16 * b);
-        vs[b] = *reinterpret_cast<const f32x4 *>(slab + F::kScales + 256 + 32 * lg + 16 * b);
-      }
+    for (int nb = 0; nb < NB; ++nb) {
+      vis[nb] = in.n <= 0 ? 0u : seen_slots(p, in.slot + F::NS * lg - p.k.len, nb);
+      if (vis[nb]) seen |= 1 << nb;
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i)
+        if (!(vis[nb] >> i & 1)) acc[nb][i >> 2][i & 3] = -INFINITY;
     }
-    f32x4 acc[NB][F::KB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int b = 0; b < F::KB; ++b) acc[nb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (F::kF32) {
-#pragma unroll
-      for (int i = 0; i < F::NK; ++i) {
-        const f32x4 kf = __builtin_bit_cast(f32x4, k_at(0, i));
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) acc[nb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[nb][i][e], acc[nb][0], 0, 0, 0);
-      }
-    } else if constexpr (Q8) {
-#pragma unroll
-      for (int i = 0; i < F::NK; ++i)
-#pragma unroll
-        for (int b = 0; b < F::KB; ++b) {
-          const uint4 kk = k_at(b, i);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t x[2] = {u ? kk.z : kk.x, u ? kk.w : kk.y};
-            const bf16x8 kf = codes8(x);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-              for (int k = 0; k < F::kQParts; ++k)
-                acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][k][2 * i + u], acc[nb][b], 0, 0, 0);
-          }
-        }
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) acc[nb][b] *= ks[b];
-    } else {
-#pragma unroll
-      for (int i = 0; i < F::NK; ++i)
-#pragma unroll
-        for (int b = 0; b < F::KB; ++b) {
-          const bf16x8 kf = __builtin_bit_cast(bf16x8, k_at(b, i));
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[nb][0][i], acc[nb][b], 0, 0, 0);
-        }
-    }
-    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
-    if (another) load_queries(to, col_next);
-    __builtin_amdgcn_sched_barrier(0);
-    load_k(next);
-    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
-    if constexpr (F::kLds) {
-#pragma unroll
-      for (int i = 0; i < F::NS; ++i) {
-        typedef uint32_t words __attribute__((ext_vector_type(F::kVWords)));
-        const words y = *reinterpret_cast<const words *>(slab + F::kHalf + (F::NS * lg + i) * F::kRow + 4 * F::kVWords * l16);
-#pragma unroll
-        for (int u = 0; u < F::kVWords; ++u) sv[i][0][u] = y[u];
-      }
-    }
-    uint32_t vis[NB];
+  };
+  // The maximum moves where it has to; `pending`: weights that refer to the old one and are still to be multiplied.
+  auto move_maximum = [&](const logits &acc, weights *pending) {
     float top[NB];
     bool far = false;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) vis[nb] = ~0u;
-    if (masked) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        vis[nb] = n <= 0 ? 0u : seen_slots(p, slot_of(p) + F::NS * lg - p.k.len, nb);
-#pragma unroll
-        for (int i = 0; i < F::NS; ++i)
-          if (!(vis[nb] >> i & 1)) acc[nb][i >> 2][i & 3] = -INFINITY;
-      }
-    }
-#pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (vis[nb]) seen |= 1 << nb;
       top[nb] = acc[nb][0][0];
 #pragma unroll
       for (int i = 1; i < F::NS; ++i) top[nb] = fmaxf(top[nb], acc[nb][i >> 2][i & 3]);
@@ -458,19 +504,30 @@ tree_attention_kernel(tree_args a) {
     if (__builtin_expect(__any(far), 0)) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float t = top[nb] * a.scale;
+        float t = ceilf(top[nb] * a.scale);
         t = fmaxf(t, __shfl_xor(t, 16));
         t = fmaxf(t, __shfl_xor(t, 32));
-        const float up = fmaxf(m[nb], t), f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nb] - up);
+        const float up = fmaxf(m[nb], t), f = m[nb] == -INFINITY ? 0.f : ldexpf(1.f, (int)fmaxf(m[nb] - up, -1000.f));
         m[nb] = up;
         l[nb] *= f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
+        if constexpr (F::kLds) {
+          if (pending)
+#pragma unroll
+            for (int k = 0; k < F::kPParts; ++k)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) pending->b[nb][k][i] = a3_f2bf(a3_bf2f(pending->b[nb][k][i]) * f);
+        }
       }
     }
-    // weights: their parts (fp32 pages: themselves)
-    bf16x8 pf[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kPParts];
-    float pw[F::kF32 ? NB : 1][F::kF32 ? 4 : 1];
+  };
+  auto weigh = [&](const logits &acc, weights &p, int i, bool masked) {
+    if constexpr (F::kLds && Q8) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        vs[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (8 + (i & 7)) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
+    }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
@@ -480,66 +537,78 @@ tree_attention_kernel(tree_args a) {
         w[i] = __builtin_amdgcn_exp2f(fmaf(acc[nb][i >> 2][i & 3], a.scale, ref));
         l[nb] += w[i];
       }
-      if constexpr (Q8) {
+      if constexpr (Q8) {                                      // (behind the tree: any scale)
 #pragma unroll
-        for (int i = 0; i < F::NS; ++i) w[i] = vis[nb] >> i & 1 ? w[i] * vs[i >> 2][i & 3] : 0.f;
+        for (int i = 0; i < F::NS; ++i) w[i] = !masked || vis[nb] >> i & 1 ? w[i] * vs[i >> 2][i & 3] : 0.f;
       }
       if constexpr (F::kF32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pw[nb][i] = w[i];
+        for (int i = 0; i < 4; ++i) p.f[nb][i] = w[i];
       } else {
-        // (cut off, not rounded: a remainder is never negative; weights are finite or NaN, and a NaN here stays one without its lower half)
+        // (weights are finite or NaN, and a NaN here stays one without its lower half)
 #pragma unroll
-        for (int k = 0; k < F::kPParts; ++k) {
+        for (int k = 0; k + 1 < F::kPParts; ++k) {
           uint32_t x[4];
-          if (k == F::kPParts - 1) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pf[nb][k][i] = a3_f2bf(w[i]);
-            continue;
-          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(__float_as_uint(w[2 * i + 1]), __float_as_uint(w[2 * i]), 0x07060302u);
 #pragma unroll
           for (int i = 0; i < 8; ++i) w[i] -= __uint_as_float(__float_as_uint(w[i]) & 0xffff0000u);
-          pf[nb][k] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+          p.b[nb][k] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.b[nb][F::kPParts - 1][i] = a3_f2bf(w[i]);
       }
     }
+  };
+  // O^T += V^T P^T of step i
+  auto take_v = [&](int i) {
+    if constexpr (F::kLds) {
+      const unsigned char *slab = lds + (4 + (i & 3)) * F::kKV + wsl * F::kHalf + voff;
+#pragma unroll
+      for (int x = 0; x < F::NS; ++x) {
+        typedef uint32_t words __attribute__((ext_vector_type(F::kVWords)));
+        const words y = *reinterpret_cast<const words *>(slab + x * F::kRow);
+#pragma unroll
+        for (int u = 0; u < F::kVWords; ++u) sv[x][0][u] = y[u];
+      }
+    }
+  };
+  auto clean_v = [&](const slab_info &in, int len) {           // of a masked slab
     if constexpr (!Q8) {
-      if (masked) {
-        uint32_t bad = 0;                                      // the top bit of a half (bf16) or of all: an exponent of ones
+      uint32_t bad = 0;                                        // the top bit of a half (bf16) or of all: an exponent of ones
+#pragma unroll
+      for (int i = 0; i < F::NS; ++i) {
+        const bool none = F::NS * lg + i >= in.n;              // behind the tree: anything
+#pragma unroll
+        for (int j = 0; j < F::NP; ++j)
+#pragma unroll
+          for (int u = 0; u < F::kVWords; ++u) {
+            if (none) sv[i][j][u] = 0u;
+            bad |= sizeof(T) == 4 ? (sv[i][j][u] & 0x7f800000u) + 0x00800000u : (sv[i][j][u] & 0x7f807f80u) + 0x00800080u;
+          }
+      }
+      if (__builtin_expect(__any(bad & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)), 0)) {
 #pragma unroll
         for (int i = 0; i < F::NS; ++i) {
-          const bool none = F::NS * lg + i >= n;               // behind the tree: anything
+          if (in.slot + F::NS * lg + i < len) continue;        // (every row sees the committed ones)
 #pragma unroll
           for (int j = 0; j < F::NP; ++j)
 #pragma unroll
             for (int u = 0; u < F::kVWords; ++u) {
-              if (none) sv[i][j][u] = 0u;
-              bad |= sizeof(T) == 4 ? (sv[i][j][u] & 0x7f800000u) + 0x00800000u : (sv[i][j][u] & 0x7f807f80u) + 0x00800080u;
-            }
-        }
-        if (__builtin_expect(__any(bad & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)), 0)) {
-#pragma unroll
-          for (int i = 0; i < F::NS; ++i) {
-            if (slot_of(p) + F::NS * lg + i < p.k.len) continue;               // (every row sees the committed ones)
-#pragma unroll
-            for (int j = 0; j < F::NP; ++j)
-#pragma unroll
-              for (int u = 0; u < F::kVWords; ++u) {
-                uint32_t x = sv[i][j][u];
-                if constexpr (sizeof(T) == 4) {
-                  if ((x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
-                } else {
-                  if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
-                  if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
-                }
-                sv[i][j][u] = x;
+              uint32_t x = sv[i][j][u];
+              if constexpr (sizeof(T) == 4) {
+                if ((x & 0x7f800000u) == 0x7f800000u) { x = 0u; odd = true; }
+              } else {
+                if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+                if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
               }
-          }
+              sv[i][j][u] = x;
+            }
         }
       }
     }
+  };
+  auto multiply_v = [&](const weights &p) {
     if constexpr (F::kF32) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -547,7 +616,7 @@ tree_attention_kernel(tree_args a) {
         for (int c = 0; c < D / 16; ++c)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
-            o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, sv[i][c >> 2][c & 3]), pw[nb][i], o[nb][c], 0, 0, 0);
+            o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, sv[i][c >> 2][c & 3]), p.f[nb][i], o[nb][c], 0, 0, 0);
     } else {
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
@@ -563,20 +632,18 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
         for (int k = 0; k < F::kPParts; ++k)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[nb][k], o[nb][c], 0, 0, 0);
+          for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p.b[nb][k], o[nb][c], 0, 0, 0);
       }
     }
-    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
-    load_v(next);
-    if constexpr (!F::kLds) __builtin_amdgcn_sched_barrier(0);
-    if (another) col = col_next;
   };
 
   // Rare: the values that are not finite, of the tree's slots that a column's row sees, decide its result there, whatever the sums are (of
   // several pieces each gets them all).  A wave's columns once more, after they have been written.
+  auto piece_at = [&](int slot, int nb, int c) { return a.part_o + ((size_t)slot * F::TC * D + ((wc * NB + nb) * (D / 16) + c) * 256 + 4 * lane); };
   auto write_odd = [&](const place &p, bool whole, int slot) {
-    for (int e = 0; e < NB * 16 * D / 64; ++e) {
-      const int in = (wc * NB + e / (D / 4)) * 16 + l16, at = p.tile * F::TC + in, d = e % (D / 4) * 4 + lg;
+    for (int e = 0; e < F::kBlocks * 4; ++e) {
+      const int nb = e / (D / 4), c = e / 4 % (D / 16), r = e & 3, at = p.tile * F::TC + (wc * NB + nb) * 16 + l16;
+      const int d = 16 * F::E * (c / F::E) + F::E * (4 * lg + r) + c % F::E;
       if (at >= p.k.rows * G) continue;
       const int j = at / G;
       float sum = 0.f;
@@ -590,14 +657,14 @@ tree_attention_kernel(tree_args a) {
       }
       if (fabsf(sum) < INFINITY) continue;
       if (whole) ((T *)a.out)[((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D + d] = (T)sum;
-      else a.part_o[((size_t)slot * F::TC + in) * D + d] = sum;
+      else piece_at(slot, nb, c)[r] = sum;
     }
   };
 
   // ---- an item, or this workgroup's part of one, is done: join the waves that share columns ---------------------------------
   // Every wave brings its sums to the columns' common maximum; then half of the waves add those of the other half to their own, block by block as
-  // the registers hold them, until one wave of each has all.  (Slabs through LDS: in the stage that has just been used.)
-  auto finish = [&](const place &p, bool begins, bool ends, uint32_t stage) {
+  // the registers hold them, until one wave of each has all.  i: the step at hand (through LDS: V of it and of the one before is used up).
+  auto finish = [&](const place &p, bool begins, bool ends, int i) {
     const bool whole = begins && ends;
     const int slot = 2 * w + (begins ? 1 : 0), some_odd = __any(odd);
     if (lane == 0) odd_waves[wave] = some_odd;
@@ -632,149 +699,214 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
     }
-    constexpr int kAtOnce = F::kAtOnce;
-    f32x4 *room = reinterpret_cast<f32x4 *>(lds + (F::kLds ? stage * F::kStage : 0));
+    constexpr int kAtOnce = F::kAtOnce, kQuarter = W / 4;
+    auto room = [&](int q) {                                   // of the qth of the waves that hand over
+      if constexpr (F::kLds) return lds + (4 + ((i - (q < kQuarter ? 1 : 0)) & 3)) * F::kKV + q % kQuarter * kAtOnce * 1024 + 16 * lane;
+      else return lds + q * kAtOnce * 1024 + 16 * lane;
+    };
 #pragma unroll
     for (int half = WS / 2; half >= 1; half /= 2)
 #pragma unroll
       for (int b0 = 0; b0 < F::kBlocks; b0 += kAtOnce) {
-        if (wsl >= half && wsl < 2 * half)
+        if (wsl >= half && wsl < 2 * half) {
+          unsigned char *to = room((wsl - half) * WC + wc);
 #pragma unroll
-          for (int b = 0; b < kAtOnce; ++b) room[(((wsl - half) * WC + wc) * kAtOnce + b) * 64 + lane] = o[(b0 + b) / (D / 16)][(b0 + b) % (D / 16)];
+          for (int b = 0; b < kAtOnce; ++b) *reinterpret_cast<f32x4 *>(to + b * 1024) = o[(b0 + b) / (D / 16)][(b0 + b) % (D / 16)];
+        }
         A3_LDS_BARRIER();
-        if (wsl < half)
+        if (wsl < half) {
+          const unsigned char *from = room(wsl * WC + wc);
 #pragma unroll
-          for (int b = 0; b < kAtOnce; ++b) o[(b0 + b) / (D / 16)][(b0 + b) % (D / 16)] += room[((wsl * WC + wc) * kAtOnce + b) * 64 + lane];
-        A3_LDS_BARRIER();
+          for (int b = 0; b < kAtOnce; ++b) o[(b0 + b) / (D / 16)][(b0 + b) % (D / 16)] += *reinterpret_cast<const f32x4 *>(from + b * 1024);
+        }
+        if (half > 1 || b0 + kAtOnce < F::kBlocks) A3_LDS_BARRIER();
       }
+    if constexpr (F::kLds) wait_loads();                       // the next item's queries, before there are stores to be waited for too
     if (wsl == 0) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const int in = (wc * NB + nb) * 16 + l16, at = p.tile * F::TC + in;  // the column's number in the item, and among the group's
-        if (at >= p.k.rows * G) continue;
-        const int j = at / G;
-        T *out = (T *)a.out + ((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D;
-        float *part = a.part_o + ((size_t)slot * F::TC + in) * D;
+        if (!whole) {                                          // as the registers hold them: whole lines
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+          for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4 *>(piece_at(slot, nb, c)) = o[nb][c];
+          if (lg == 0) a.part_ml[(size_t)slot * F::TC + in] = make_float2(M[nb], some[nb] ? L[nb] : -1.f);
+        } else if (at < p.k.rows * G) {
+          const int j = at / G;
+          T *out = (T *)a.out + ((size_t)(p.k.first + j) * a.p.Hq + p.head * G + (at - j * G)) * D;
 #pragma unroll
-          for (int c = 0; c < D / 16; c += 4) {
-            const int d = 16 * F::E * (c / F::E) + F::E * (4 * lg + r) + c % F::E;
-            f32x4 sum = {o[nb][c][r], o[nb][c + 1][r], o[nb][c + 2][r], o[nb][c + 3][r]};
-            if (whole) {
-              typedef T vec4 __attribute__((ext_vector_type(4)));
-              vec4 y;
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-              for (int u = 0; u < 4; ++u) y[u] = (T)(some[nb] ? sum[u] / L[nb] : 0.f);
-              *reinterpret_cast<vec4 *>(out + d) = y;
-            } else {
-              *reinterpret_cast<f32x4 *>(part + d) = sum;
+            for (int c = 0; c < D / 16; c += F::E) {
+              typedef T vec __attribute__((ext_vector_type(F::E)));
+              vec y;
+#pragma unroll
+              for (int u = 0; u < F::E; ++u) y[u] = (T)(some[nb] ? o[nb][c + u][r] / L[nb] : 0.f);
+              *reinterpret_cast<vec *>(out + 16 * c + F::E * (4 * lg + r)) = y;
             }
-          }
-        if (!whole && lg == 0) a.part_ml[(size_t)slot * F::TC + in] = make_float2(M[nb], some[nb] ? L[nb] : -1.f);
+        }
       }
       if constexpr (!Q8) {
         if (__builtin_expect(odd_any, 0)) {
-          __builtin_amdgcn_s_waitcnt(0);                       // behind the other lanes' stores to the same rows
+          __builtin_amdgcn_s_waitcnt(0);
           write_odd(p, whole, slot);
         }
       }
     }
   };
+  // Which item goes on after this run, and in how many pieces.
+  auto note_cut = [&](const place &p, bool ends, int t) {
+    if (tid != 0) return;
+    int pieces = 1;
+    if (!ends) {                                               // goes on in the workgroups behind: how many of them
+      // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
+      const int last = first + t + p.k.steps - 1 - p.step, fat = rest * (each + 1);
+      pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
+    }
+    if (a.by_item) a.cut[((size_t)p.g * Hkv + p.head) * a.tiles + p.tile] = make_int4(p.g, p.head, w, pieces);
+    else if (!ends) a.cut[w] = make_int4(p.g, p.head | p.tile << 16, w, pieces);
+  };
 
-  // ---- the run of steps: of every item first those whose slots are all committed ------------------------------------------
-  // Everything that was asked for by now is there (the compiler's own waits would stand in the loops, and be for later loads too).
-  auto settle = [&]() {
-    if constexpr (F::kLds) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        asm volatile("" : "+v"(col.mask[nb][0]), "+v"(col.mask[nb][1]));
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) asm volatile("" : "+v"(qb[nb][0][i]));
-      }
-    }
-  };
-  constexpr int S = F::kLds ? F::kStages : 2;                  // through LDS: S - 1 steps ahead
-  place ahead = now;
-  int ahead_left = n_steps, ahead_page = page_at(ahead, slot_of(ahead)), queue[S];
-  auto look = [&]() {                                          // where the next slab lies (behind the run: the pool's start)
-    const where x = ahead_left > 0 ? on_page(ahead, slot_of(ahead), ahead_page) : where{0, 0, 0};
-    if (--ahead_left > 0) {
-      advance(ahead);
-      ahead_page = page_at(ahead, slot_of(ahead));             // used a step later: a scalar load takes a while
-    }
-    return x;
-  };
-  load_queries(now, col);
-  settle();
+  // ---- the run of steps ------------------------------------------------------------------------------------------------
+  bool begins = now.step == 0;
   clear();
   if constexpr (!F::kLds) {
-    const where x = look();
+    where next = look();
+    load_queries(now, col);
     __builtin_amdgcn_sched_barrier(0);
-    load_k(x);
+    load_k(next);
     __builtin_amdgcn_sched_barrier(0);
-    load_v(x);
+    load_v(next);
     __builtin_amdgcn_sched_barrier(0);
-    queue[0] = x.n;
-  }
-  uint32_t stage = 0, to_stage = 0;
-  bool begins = now.step == 0;
+    int n = next.n;
+    for (int t = 0; t < n_steps; ++t) {
+      next = look();
+      const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1, last = ends || !more;
+      place p = now;
+      if (!last) ++p.step;
+      else if (more) advance(p);
+      const slab_info in = info_of(now, n);
+      logits acc;
+      weights wt;
+      columns col_next;
+      multiply_k(acc, t);
+      __builtin_amdgcn_sched_barrier(0);
+      // (loads come back in order: the next item's queries in front of its first K, so that a wait for that K is one for them)
+      if (last && more) load_queries(p, col_next);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(next);
+      __builtin_amdgcn_sched_barrier(0);
+      if (in.masked) hide(acc, now, in);
+      else seen = (1 << NB) - 1;
+      move_maximum(acc, nullptr);
+      weigh(acc, wt, t, in.masked);
+      if (in.masked) clean_v(in, now.k.len);
+      multiply_v(wt);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(next);
+      __builtin_amdgcn_sched_barrier(0);
+      n = next.n;
+      if (last) {
+        finish(now, begins, ends, t);
+        if (begins) note_cut(now, ends, t);
+        begins = true;
+        clear();
+        if (more) col = col_next;
+      }
+      now = p;
+    }
+  } else {
 #pragma unroll 1
-  for (int t = F::kLds ? 1 - S : 0; t < n_steps; ++t) {
-    where next{0, 0, 0};
-    if constexpr (F::kLds) {
-      if (t >= 0) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::kPer * (S - 2)) : "memory");
-        A3_LDS_BARRIER();                                      // the step's slabs are there, and the stage before it is free
-      }
-      next = look();
-      dma(next, to_stage);
-      to_stage = to_stage + 1 == S ? 0 : to_stage + 1;
+    for (int i = 0; i < 4; ++i) ask(i);
+    load_queries(now, col);
+    wait_loads();
+    A3_LDS_BARRIER();
+    logits acc;
+    weights wt;                                                // of the step before, where it is `pending`: V is not yet multiplied with them
+    bool pending = false;
+    slab_info before{0, 0, false};
+    columns col_next = col;
+    multiply_k(acc, 0);
+    int t = 0;
+    slab_info in;
+    bool last;
+    auto next_step = [&]() {
+      // K of step t + 1 and V of step t - 1 are there; nobody reads K of step t and V of step t - 2 any more
+      arrive();
+      ask(t + 4);
+      in = info_of(now, queue[0]);
+      last = now.step == now.k.steps - 1 || t + 1 == n_steps;
+    };
+    next_step();
+    for (;;) {
+      while (pending && !in.masked && !before.masked && !last) {         // the common way: all of it at once
+        move_maximum(acc, &wt);
+        logits acc_next;
+        weights wt_next;
+        take_v(t - 1);
+        multiply_k(acc_next, t + 1);
+        weigh(acc, wt_next, t, false);
+        multiply_v(wt);
 #pragma unroll
-      for (int i = 0; i + 1 < S; ++i) queue[i] = queue[i + 1];
-      queue[S - 1] = next.n;
-      if (t < 0) continue;
-    } else {
-      next = look();
-    }
-    const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1, last = ends || !more;
-    place p = now;
-    if (!last) ++p.step;
-    else if (more) advance(p);
-    work(queue[0], next, stage, now, p, last && more);
-    if constexpr (!F::kLds) queue[0] = next.n;
-    if (last) {
-      finish(now, begins, ends, stage);
-      if (begins && tid == 0) {
-        int pieces = 1;
-        if (!ends) {                                           // goes on in the workgroups behind: how many of them
-          // (its last step is `last` of all: in a workgroup of the first `rest`, or behind them)
-          const int last = first + t + now.k.steps - 1 - now.step, fat = rest * (each + 1);
-          pieces += (last < fat ? last / (each + 1) : rest + (last - fat) / max(each, 1)) - w;
-        }
-        if (a.by_item) a.cut[((size_t)now.g * Hkv + now.head) * a.tiles + now.tile] = make_int4(now.g, now.head, w, pieces);
-        else if (!ends) a.cut[w] = make_int4(now.g, now.head | now.tile << 16, w, pieces);
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int b = 0; b < F::KB; ++b) acc[nb][b] = acc_next[nb][b];
+        wt = wt_next;
+        before = in;
+        ++now.step;
+        ++t;
+        next_step();
       }
-      begins = true;
-      clear();
-      settle();
+      if (pending) {
+        take_v(t - 1);
+        if (before.masked) clean_v(before, now.k.len);
+        multiply_v(wt);
+      }
+      if (in.masked) hide(acc, now, in);
+      else seen = (1 << NB) - 1;
+      move_maximum(acc, nullptr);
+      weigh(acc, wt, t, in.masked);
+      if (!last) {
+        multiply_k(acc, t + 1);
+        pending = true;
+        before = in;
+        ++now.step;
+      } else {
+        const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1;
+        place p = now;
+        if (more) advance(p);
+        arrive();                                              // V of this step
+        if (more) load_queries(p, col_next);
+        take_v(t);
+        if (in.masked) clean_v(in, now.k.len);
+        multiply_v(wt);
+        finish(now, begins, ends, t);
+        if (begins) note_cut(now, ends, t);
+        if (!more) break;
+        begins = true;
+        pending = false;
+        before.masked = false;
+        clear();
+        col = col_next;
+        multiply_k(acc, t + 1);
+        now = p;
+      }
+      ++t;
+      next_step();
     }
-    now = p;
-    stage = stage + 1 == S ? 0 : stage + 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the memory that the last loads go to is another workgroup's next)
   }
-  if constexpr (F::kLds) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the memory that the last loads go to is another workgroup's next)
 }
 
-// Joins the pieces of an item that is cut, kUnits columns' four coordinates a workgroup: of item blockIdx.x (by_item: few of them), or of
-// the one that goes on after workgroup blockIdx.x.  A thread sums its coordinates over every kth piece, the loads of eight pieces on their
-// way together; then the k partial sums are joined.
-constexpr int kJoinThreads = 256;
-template <typename T, int D, int TC>
-__global__ void __launch_bounds__(kJoinThreads)
+// Joins the pieces of an item that is cut: of item blockIdx.x (by_item: few of them), or of the one that goes on after workgroup blockIdx.x,
+// four accumulator blocks of 16 columns (blockIdx.y).  A wave sums every fourth piece, the loads of four pieces on their way together; then
+// the four partial sums are joined.
+template <class F, typename T, int D>
+__global__ void __launch_bounds__(256)
 tree_join_kernel(tree_args a) {
-  __shared__ f32x4 os[kJoinThreads];
-  __shared__ float2 mls[kJoinThreads];
-  const int tid = threadIdx.x, G = a.p.Hq / a.p.Hkv, groups = kJoinThreads / a.units;
+  constexpr int TC = F::TC, E = F::E;
+  __shared__ f32x4 os[4][4][64];
+  __shared__ float2 mls[4][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lg = lane >> 4, G = a.p.Hq / a.p.Hkv;
   int g, head, tile;
   if (a.by_item) {
     g = blockIdx.x / (a.p.Hkv * a.tiles);
@@ -790,55 +922,72 @@ tree_join_kernel(tree_args a) {
   const group_work k = work_of<1, TC>(a, a.start[g], a.start[g + 1], a.req ? a.req[g] : g, a.len[g]);
   if (k.steps == 0 || tile >= k.tiles) return;                 // (no such item: `cut` says nothing)
   const int4 c = a.cut[blockIdx.x];
-  const int w = c.z, n = c.w;
-  if (n < 2) return;
-  const int gr = tid / a.units, v = tid - gr * a.units, u = blockIdx.y * a.units + v, in = u / (D / 4), at = tile * TC + in;
-  const bool on = gr < groups && in < TC && at < k.rows * G;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const int w = c.z, n = c.w, cb = blockIdx.y / (D / 64), c0 = blockIdx.y % (D / 64) * 4, at = tile * TC + cb * 16 + l16;
+  if (n < 2 || tile * TC + cb * 16 >= k.rows * G) return;
+  f32x4 o[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = -1.f;                               // l < 0: nothing seen
-  auto take = [](f32x4 &o, float &m, float &l, const f32x4 &x, float2 ml, float top) {
+  auto take = [](f32x4 (&o)[4], float &l, const f32x4 (&x)[4], float2 ml, float top) {
     if (ml.y < 0.f) return;
     const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-    o += x * f;                                                // (a piece whose logits are all NaN has no maximum, and its NaN stays one times 0)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) o[b] += x[b] * f;              // (a piece whose logits are all NaN has no maximum, and its NaN stays one times 0)
     l = (l < 0.f ? 0.f : l) + ml.y * f;
   };
-  constexpr int K = 8;
-  if (on)
-    for (int i = gr; i < n; i += K * groups) {
-      f32x4 x[K];
-      float2 ml[K];
+  constexpr int K = 4;
+  for (int i = wave; i < n; i += 4 * K) {
+    f32x4 x[K][4];
+    float2 ml[K];
 #pragma unroll
-      for (int q = 0; q < K; ++q) {
-        const int p = min(i + q * groups, n - 1), slot = p == 0 ? 2 * w + 1 : 2 * (w + p);
-        x[q] = *reinterpret_cast<const f32x4 *>(a.part_o + (size_t)slot * TC * D + 4 * u);
-        ml[q] = a.part_ml[(size_t)slot * TC + in];
-      }
-      float top = m;
+    for (int q = 0; q < K; ++q) {
+      const int p = min(i + 4 * q, n - 1), slot = p == 0 ? 2 * w + 1 : 2 * (w + p);
+      const float *from = a.part_o + ((size_t)slot * TC * D + (cb * (D / 16) + c0) * 256 + 4 * lane);
 #pragma unroll
-      for (int q = 0; q < K; ++q) {
-        if (i + q * groups >= n) ml[q] = make_float2(-INFINITY, -1.f);
-        top = fmaxf(top, ml[q].x);
-      }
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-      if (!(l < 0.f)) { o *= f; l *= f; }
-      m = top;
-#pragma unroll
-      for (int q = 0; q < K; ++q) take(o, m, l, x[q], ml[q], top);
+      for (int b = 0; b < 4; ++b) x[q][b] = *reinterpret_cast<const f32x4 *>(from + 256 * b);
+      ml[q] = a.part_ml[(size_t)slot * TC + cb * 16 + l16];
     }
-  os[tid] = o;
-  mls[tid] = make_float2(m, l);
-  __syncthreads();
-  if (gr != 0 || !on) return;
-  for (int q = 1; q < groups; ++q) m = fmaxf(m, mls[q * a.units + v].x);
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-  l = -1.f;
-  for (int q = 0; q < groups; ++q) take(o, m, l, os[q * a.units + v], mls[q * a.units + v], m);
-  typedef T vec4 __attribute__((ext_vector_type(4)));
-  vec4 y;
+    float top = m;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = (T)(l < 0.f ? 0.f : o[e] / l);
+    for (int q = 0; q < K; ++q) {
+      if (i + 4 * q >= n) ml[q] = make_float2(-INFINITY, -1.f);
+      top = fmaxf(top, ml[q].x);
+    }
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    if (!(l < 0.f)) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) o[b] *= f;
+      l *= f;
+    }
+    m = top;
+#pragma unroll
+    for (int q = 0; q < K; ++q) take(o, l, x[q], ml[q], top);
+  }
+#pragma unroll
+  for (int b = 0; b < 4; ++b) os[wave][b][lane] = o[b];
+  if (lg == 0) mls[wave][l16] = make_float2(m, l);
+  __syncthreads();
+  if (wave != 0 || at >= k.rows * G) return;
+#pragma unroll
+  for (int q = 1; q < 4; ++q) m = fmaxf(m, mls[q][l16].x);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  l = -1.f;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const f32x4 x[4] = {os[q][0][lane], os[q][1][lane], os[q][2][lane], os[q][3][lane]};
+    take(o, l, x, mls[q][l16], m);
+  }
   const int j = at / G;
-  *reinterpret_cast<vec4 *>((T *)a.out + ((size_t)(k.first + j) * a.p.Hq + head * G + (at - j * G)) * D + 4 * (u % (D / 4))) = y;
+  T *out = (T *)a.out + ((size_t)(k.first + j) * a.p.Hq + head * G + (at - j * G)) * D + 16 * E * (c0 / E) + c0 % E;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    typedef T vec4 __attribute__((ext_vector_type(4)));
+    vec4 y;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) y[u] = (T)(l < 0.f ? 0.f : o[u][r] / l);
+    *reinterpret_cast<vec4 *>(out + E * (4 * lg + r)) = y;
+  }
 }
 
 constexpr int kMaxRows = 1024;
@@ -851,15 +1000,20 @@ tree_shape shape_of(const a3_pages *P, int max_rows) {
   if (cols <= 16) return {1, 1, 4, 512};
   if (cols <= 32) return {2, 1, 4, wide ? 256 : 512};
   if (wide) return {2, 4, 4, 256};
-  return {2, cols <= 64 ? 2 : 4, 8, 256};
+  if (P->dtype == A3_F32) return {2, cols <= 64 ? 2 : 4, 8, 256};
+  return {cols <= 64 ? 2 : 4, 2, 4, 256};
 }
 template <typename T, int D, bool Q8, class F>
 void with_shape(tree_shape s, F f) {
   if (s.nb == 1) f(tree_form<T, D, Q8, 1, 1, 4>{});
   else if (s.wc == 1) f(tree_form<T, D, Q8, 2, 1, 4>{});
   else if constexpr (sizeof(T) == 4 && D == 128) f(tree_form<T, D, Q8, 2, 4, 4>{});
-  else if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 8>{});
-  else f(tree_form<T, D, Q8, 2, 4, 8>{});
+  else if constexpr (sizeof(T) == 4) {
+    if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 8>{});
+    else f(tree_form<T, D, Q8, 2, 4, 8>{});
+  }
+  else if (s.nb == 2) f(tree_form<T, D, Q8, 2, 2, 4>{});
+  else f(tree_form<T, D, Q8, 4, 2, 4>{});
 }
 struct tree_plan { tree_shape s; int tc, tiles, shares; long long items, steps; };
 tree_plan plan_of(const a3_pages *P, int n_groups, int max_rows) {
@@ -926,8 +1080,7 @@ extern "C" a3_status a3_tree_attention(const a3_pages *P, const void *q, int n_g
   a.tiles = plan.tiles;
   a.by_item = plan.items <= plan.shares;
   tree_ws(P, plan, ws, &a);
-  a.units = 64;
-  const dim3 join((unsigned)(a.by_item ? plan.items : plan.shares), (unsigned)(plan.tc * (P->head_dim / 4) / a.units));
+  const dim3 join((unsigned)(a.by_item ? plan.items : plan.shares), (unsigned)(plan.tc / 16 * (P->head_dim / 64)));
   with_format(P, [&](auto elem, auto d, auto q8) {
     typedef decltype(elem) T;
     with_shape<T, d.value, q8.value>(plan.s, [&](auto form) {
@@ -941,7 +1094,7 @@ extern "C" a3_status a3_tree_attention(const a3_pages *P, const void *q, int n_g
         return;
       }
       hipLaunchKernelGGL(kern, dim3((unsigned)plan.shares), dim3(64 * F::W), F::kLdsBytes, (hipStream_t)stream, a);
-      hipLaunchKernelGGL((tree_join_kernel<T, d.value, F::TC>), join, dim3(kJoinThreads), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((tree_join_kernel<F, T, d.value>), join, dim3(256), 0, (hipStream_t)stream, a);
     });
   });
   if (s != A3_OK) return s;
