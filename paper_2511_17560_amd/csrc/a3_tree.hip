@@ -67,7 +67,7 @@ struct tree_form {
   static constexpr int kStep = WS * SK;
   static constexpr bool kOnce = WC_ == 1;                      // a cache is read once: nontemporal
   static constexpr int kBlocks = NB * D / 16;                  // accumulator blocks of a wave
-  static constexpr bool kLds = sizeof(T) == 2 && WC_ > 1;      // through LDS: rings of K and V, four steps each, and of scales, eight steps
+  static constexpr bool kLds = sizeof(T) == 2 && WC_ > 1 && NB_ > 2;      // through LDS: rings of K and V, four steps each, and of scales, eight steps
   static constexpr int kHalf = SK * kRow, kKV = WS * kHalf, kScaleAt = 8 * kKV;
   static constexpr int kLoads = kRow / 32 >= WC ? kRow / 32 / WC : 1;          // direct-to-LDS loads of a wave, of K and of V, a step
   static constexpr int kPer = 2 * kLoads + (Q8 ? 1 : 0);
@@ -1001,7 +1001,7 @@ tree_shape shape_of(const a3_pages *P, int max_rows) {
   if (cols <= 32) return {2, 1, 4, wide ? 256 : 512};
   if (wide) return {2, 4, 4, 256};
   if (P->dtype == A3_F32) return {2, cols <= 64 ? 2 : 4, 8, 256};
-  return {cols <= 64 ? 2 : 4, 2, 4, 256};
+  return {cols <= 64 ? 2 : 4, 2, 4, cols <= 64 ? 512 : 256};
 }
 template <typename T, int D, bool Q8, class F>
 void with_shape(tree_shape s, F f) {
