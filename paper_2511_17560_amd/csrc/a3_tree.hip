@@ -93,6 +93,14 @@ __device__ __forceinline__ group_work work_of(const tree_args &a, int start, int
   return w;
 }
 
+template <int N, class Fn>
+__device__ __forceinline__ void each_of(Fn f) {               // f(0) .. f(N - 1), the numbers as constants
+  if constexpr (N > 0) {
+    each_of<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
 template <class F, typename T, int D, bool Q8>
 __global__ void __launch_bounds__(64 * F::W, F::W == 4 ? F::kWaves : 1)
 tree_attention_kernel(tree_args a) {
@@ -223,6 +231,24 @@ tree_attention_kernel(tree_args a) {
     return x;
   };
 
+  // How many of the next ones need no more than a look at the lane that has their page's number.
+  auto count_simple = [&]() {
+    const int slot = slot_of(ahead), from = pages_from << a.p.page_shift, room = from + (64 << a.p.page_shift) - slot;
+    if (pages_from == kNoPages || slot < from || room <= 0) return 0;
+    return min(min(ahead.k.steps - 1 - ahead.step, ahead_left - 1), (room - 1) / F::kStep + 1);
+  };
+  auto look_simply = [&]() {
+    where x{0, 0, 0};
+    const int slot = slot_of(ahead), page = __builtin_amdgcn_readlane(pages, (slot >> a.p.page_shift) - pages_from);
+    const bool there = (uint32_t)page < (uint32_t)a.p.n_pages;
+    x.block = there ? ((size_t)(uint32_t)page * (uint32_t)Hkv + ahead.head) * head_bytes : 0;
+    x.at = there ? slot & ((1 << a.p.page_shift) - 1) : 0;
+    x.n = there ? ahead.k.end - slot : 0;
+    ++ahead.step;
+    --ahead_left;
+    return x;
+  };
+
   // ---- one slab of one wave in registers: buffer loads, the page in four scalars, a lane's place in one register ---------------------
   const uint32_t koff = (SK == 16 ? l16 : 8 * (l16 >> 2) + (l16 & 3)) * F::kRow + 16 * lg;
   const uint32_t voff = (uint32_t)(F::NS * lg * F::kRow + F::kVWords * 4 * l16);
@@ -291,39 +317,51 @@ tree_attention_kernel(tree_args a) {
   // Inline assembly on purpose: the compiler then neither treats these as LDS writes (it would wait for all of them before every LDS
   // read) nor moves memory accesses across them; the waits for them are the explicit s_waitcnt below.
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  auto page_at = [&](const char *pool, const where &x) {
-    const uint64_t p = (uint64_t)pool + x.block;
+  auto page_at = [&](const char *pool, size_t block) {
+    const uint64_t p = (uint64_t)pool + block;
     return u32x4{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, (uint32_t)head_bytes, 0x00020000u};
   };
   auto dma = [&](u32x4 page, uint32_t off, uint32_t at, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(page), "s"(at) : "memory");
   };
-  where behind[2] = {{0, 0, 0}, {0, 0, 0}};                    // the two steps whose K is asked for and whose V is not
-  int queue[5] = {0, 0, 0, 0, 0};                              // slots that count, of the step at hand and of those whose K is asked for
-  auto ask = [&](int i) {                                      // K of step i, V of step i - 2 (a wave has as many loads in every step)
-    const where x = look();
-    const u32x4 pk = page_at(a.p.k_pool, x), pv = page_at(a.p.v_pool, behind[0]);
-    const uint32_t to = lds_base + wsl * F::kHalf;
-#pragma unroll
-    for (int t = 0; t < F::kLoads; ++t)
-      dma(pk, dma_k[t], (uint32_t)x.at * F::kRow, to + (i & 3) * F::kKV + (wc * F::kLoads + t) % kHalfLoads * 1024);
-#pragma unroll
-    for (int t = 0; t < F::kLoads; ++t)
-      dma(pv, dma_v[t], (uint32_t)behind[0].at * F::kRow, to + (4 + ((i + 2) & 3)) * F::kKV + (wc * F::kLoads + t) % kHalfLoads * 1024);
+  struct { size_t block; int at; } behind[2] = {{0, 0}, {0, 0}};       // the two steps whose K is asked for and whose V is not
+  uint32_t missing = 0;                                        // bit q: step t + q does not count (no page, behind the tree's end)
+  struct request { u32x4 k, v, scales; uint32_t k_at, v_at, scale_at, to_k, to_v, to_scales; };
+  auto request_of = [&](int i, const where &x) {               // K of step i, V of step i - 2 (a wave has as many loads in every step)
+    request r;
+    r.k = page_at(a.p.k_pool, x.block);
+    r.v = page_at(a.p.v_pool, behind[0].block);
+    r.k_at = (uint32_t)x.at * F::kRow;
+    r.v_at = (uint32_t)behind[0].at * F::kRow;
+    r.to_k = lds_base + wsl * F::kHalf + (i & 3) * F::kKV;
+    r.to_v = lds_base + wsl * F::kHalf + (4 + ((i + 2) & 3)) * F::kKV;
     if constexpr (Q8) {                                        // 64 scales, of which 32 are the slab's (behind the head's page: zeros)
-      const u32x4 page = wc & 1 ? page_at(a.p.v_pool, x) : pk;
-      const uint32_t sc = (uint32_t)(D << a.p.page_shift) + 4 * x.at, at = lds_base + F::kScaleAt + ((wc & 1) * 8 + (i & 7)) * WS * 256 + wsl * 256;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(at), "v"(4 * lane), "s"(page), "s"(sc) : "memory");
+      r.scales = wc & 1 ? page_at(a.p.v_pool, x.block) : r.k;
+      r.scale_at = (uint32_t)(D << a.p.page_shift) + 4 * x.at;
+      r.to_scales = lds_base + F::kScaleAt + ((wc & 1) * 8 + (i & 7)) * WS * 256 + wsl * 256;
     }
     behind[0] = behind[1];
-    behind[1] = x;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) queue[q] = queue[q + 1];
-    queue[4] = x.n;
+    behind[1] = {x.block, x.at};
+    missing = missing >> 1 | (x.n <= 0 ? 16u : 0u);
+    return r;
   };
-  // All loads of this wave but those of the last two steps are done; then those of all waves.
+  auto ask_part = [&](const request &r, int t) {               // load t of kPer
+    if (t < F::kLoads) {
+      dma(r.k, dma_k[t], r.k_at, r.to_k + (wc * F::kLoads + t) % kHalfLoads * 1024);
+    } else if (t < 2 * F::kLoads) {
+      dma(r.v, dma_v[t - F::kLoads], r.v_at, r.to_v + (wc * F::kLoads + t - F::kLoads) % kHalfLoads * 1024);
+    } else {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(r.to_scales), "v"(4 * lane), "s"(r.scales),
+                   "s"(r.scale_at) : "memory");
+    }
+  };
+  auto ask = [&](const request &r) {
+#pragma unroll
+    for (int t = 0; t < F::kPer; ++t) ask_part(r, t);
+  };
+  // All loads of this wave but those of the last step are done; then those of all waves.
   auto arrive = [&]() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::kPer) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::kPer) : "memory");
     A3_LDS_BARRIER();
   };
 
@@ -390,10 +428,16 @@ tree_attention_kernel(tree_args a) {
     odd = false;
   };
 
+  auto two_bf16 = [](float x, float y) {
+    typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{a3_f2bf(x), a3_f2bf(y)});
+  };
+
   // ---- parts of a step ----------------------------------------------------------------------------------------------
   typedef f32x4 logits[NB][F::KB];
-  struct weights {                                             // bf16 parts, or (fp32 pages) as they are
-    bf16x8 b[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kPParts];
+  typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+  struct weights {                                             // two bf16 of a part in a word, or (fp32 pages) as they are
+    words4 b[F::kF32 ? 1 : NB][F::kF32 ? 1 : F::kPParts];
     float f[F::kF32 ? NB : 1][F::kF32 ? 4 : 1];
   };
   struct slab_info { int slot, n; bool masked; };              // masked: it reaches behind the committed slots, or does not exist
@@ -403,26 +447,29 @@ tree_attention_kernel(tree_args a) {
   };
 
   // S^T of step i (its logits but for the scale)
-  auto multiply_k = [&](logits &acc, int i) {
-    const unsigned char *slab = lds + (i & 3) * F::kKV + wsl * F::kHalf + my_slot * F::kRow;
-    auto k_at = [&](int b, int x) {
-      if constexpr (F::kLds) return *reinterpret_cast<const uint4 *>(slab + (((4 * x + lg) ^ my_key) << 4) + 4 * b * F::kRow);
-      else return sk[b][x];
-    };
+  auto take_k = [&](int i) {
+    if constexpr (F::kLds) {
+      const unsigned char *slab = lds + (i & 3) * F::kKV + wsl * F::kHalf + my_slot * F::kRow;
+#pragma unroll
+      for (int x = 0; x < F::NK; ++x)
+#pragma unroll
+        for (int b = 0; b < F::KB; ++b) sk[b][x] = *reinterpret_cast<const uint4 *>(slab + (((4 * x + lg) ^ my_key) << 4) + 4 * b * F::kRow);
+    }
     if constexpr (F::kLds && Q8) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
         ks[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (i & 7) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
     }
+  };
+  auto multiply_k_part = [&](logits &acc, int x) {             // with bytes 64 x .. of the slots
+    if (x == 0)
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int b = 0; b < F::KB; ++b) acc[nb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < F::NK; ++x)
+        for (int b = 0; b < F::KB; ++b) acc[nb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int b = 0; b < F::KB; ++b) {
-        const uint4 kk = k_at(b, x);
+        const uint4 kk = sk[b][x];
         if constexpr (F::kF32) {
           const f32x4 kf = __builtin_bit_cast(f32x4, kk);
 #pragma unroll
@@ -446,12 +493,20 @@ tree_attention_kernel(tree_args a) {
             acc[nb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), qb[nb][0][x], acc[nb][b], 0, 0, 0);
         }
       }
+  };
+  auto scale_k = [&](logits &acc) {
     if constexpr (Q8) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int b = 0; b < 2; ++b) acc[nb][b] *= ks[b];
     }
+  };
+  auto multiply_k = [&](logits &acc, int i) {
+    take_k(i);
+#pragma unroll
+    for (int x = 0; x < F::NK; ++x) multiply_k_part(acc, x);
+    scale_k(acc);
   };
 
   // Bits of the lane's slots (t0 .. t0 + NS - 1 of the tree; committed ones below 0) that the row of block nb's column sees.
@@ -490,8 +545,8 @@ tree_attention_kernel(tree_args a) {
         if (!(vis[nb] >> i & 1)) acc[nb][i >> 2][i & 3] = -INFINITY;
     }
   };
-  // The maximum moves where it has to; `pending`: weights that refer to the old one and are still to be multiplied.
-  auto move_maximum = [&](const logits &acc, weights *pending) {
+  // The maximum moves where it has to; `pending` (if some are): weights that refer to the old one and are still to be multiplied.
+  auto move_maximum = [&](const logits &acc, weights &pending, auto some_pending) {
     float top[NB];
     bool far = false;
 #pragma unroll
@@ -512,53 +567,57 @@ tree_attention_kernel(tree_args a) {
         l[nb] *= f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
-        if constexpr (F::kLds) {
-          if (pending)
+        if constexpr (decltype(some_pending)::value) {
 #pragma unroll
             for (int k = 0; k < F::kPParts; ++k)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) pending->b[nb][k][i] = a3_f2bf(a3_bf2f(pending->b[nb][k][i]) * f);
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t x = pending.b[nb][k][i];
+                pending.b[nb][k][i] = two_bf16(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+              }
         }
       }
     }
   };
-  auto weigh = [&](const logits &acc, weights &p, int i, bool masked) {
+  auto take_scales = [&](int i) {
     if constexpr (F::kLds && Q8) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
         vs[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (8 + (i & 7)) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
     }
+  };
+  auto weigh_two = [&](const logits &acc, weights &p, int nb, int q, bool masked) {    // the weights of block nb's slots 2 q and 2 q + 1
+    const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
+    float w[2];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const float ref = m[nb] == -INFINITY ? 0.f : -m[nb];
-      float w[F::NS];
-#pragma unroll
-      for (int i = 0; i < F::NS; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(fmaf(acc[nb][i >> 2][i & 3], a.scale, ref));
-        l[nb] += w[i];
-      }
-      if constexpr (Q8) {                                      // (behind the tree: any scale)
-#pragma unroll
-        for (int i = 0; i < F::NS; ++i) w[i] = !masked || vis[nb] >> i & 1 ? w[i] * vs[i >> 2][i & 3] : 0.f;
-      }
-      if constexpr (F::kF32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p.f[nb][i] = w[i];
-      } else {
-        // (weights are finite or NaN, and a NaN here stays one without its lower half)
-#pragma unroll
-        for (int k = 0; k + 1 < F::kPParts; ++k) {
-          uint32_t x[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(__float_as_uint(w[2 * i + 1]), __float_as_uint(w[2 * i]), 0x07060302u);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] -= __uint_as_float(__float_as_uint(w[i]) & 0xffff0000u);
-          p.b[nb][k] = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p.b[nb][F::kPParts - 1][i] = a3_f2bf(w[i]);
-      }
+    for (int e = 0; e < 2; ++e) {
+      const int i = 2 * q + e;
+      w[e] = __builtin_amdgcn_exp2f(fmaf(acc[nb][i >> 2][i & 3], a.scale, ref));
+      l[nb] += w[e];
+      if constexpr (Q8) w[e] = !masked || vis[nb] >> i & 1 ? w[e] * vs[i >> 2][i & 3] : 0.f;       // (behind the tree: any scale)
+      if constexpr (F::kF32) p.f[nb][i] = w[e];
     }
+    if constexpr (!F::kF32) {
+      // (weights are finite or NaN, and a NaN here stays one without its lower half)
+#pragma unroll
+      for (int k = 0; k + 1 < F::kPParts; ++k) {
+        uint32_t x = __builtin_amdgcn_perm(__float_as_uint(w[1]), __float_as_uint(w[0]), 0x07060302u);
+        if constexpr (F::kLds) asm volatile("" : "+v"(x));     // (here, not where it is used)
+        p.b[nb][k][q] = x;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) w[e] -= __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
+      }
+      uint32_t x = two_bf16(w[0], w[1]);
+      if constexpr (F::kLds) asm volatile("" : "+v"(x));
+      p.b[nb][F::kPParts - 1][q] = x;
+    }
+  };
+  auto weigh = [&](const logits &acc, weights &p, int i, bool masked) {
+    take_scales(i);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int q = 0; q < F::NS / 2; ++q) weigh_two(acc, p, nb, q, masked);
   };
   // O^T += V^T P^T of step i
   auto take_v = [&](int i) {
@@ -608,6 +667,24 @@ tree_attention_kernel(tree_args a) {
       }
     }
   };
+  auto multiply_v_part = [&](const weights &p, int c) {        // coordinates of block c (bf16)
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (Q8)
+        x[i] = pack_codes((float)(signed char)(sv[2 * i][0][c >> 2] >> 8 * (c & 3)), (float)(signed char)(sv[2 * i + 1][0][c >> 2] >> 8 * (c & 3)));
+      else
+        x[i] = __builtin_amdgcn_perm(sv[2 * i + 1][0][c >> 1], sv[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+    }
+    const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+    for (int k = 0; k < F::kPParts; ++k)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, p.b[nb][k]);
+        o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[nb][c], 0, 0, 0);
+      }
+  };
   auto multiply_v = [&](const weights &p) {
     if constexpr (F::kF32) {
 #pragma unroll
@@ -619,21 +696,7 @@ tree_attention_kernel(tree_args a) {
             o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, sv[i][c >> 2][c & 3]), p.f[nb][i], o[nb][c], 0, 0, 0);
     } else {
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (Q8)
-            x[i] = pack_codes((float)(signed char)(sv[2 * i][0][c >> 2] >> 8 * (c & 3)), (float)(signed char)(sv[2 * i + 1][0][c >> 2] >> 8 * (c & 3)));
-          else
-            x[i] = __builtin_amdgcn_perm(sv[2 * i + 1][0][c >> 1], sv[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
-        }
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
-#pragma unroll
-        for (int k = 0; k < F::kPParts; ++k)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p.b[nb][k], o[nb][c], 0, 0, 0);
-      }
+      for (int c = 0; c < D / 16; ++c) multiply_v_part(p, c);
     }
   };
 
@@ -797,7 +860,7 @@ tree_attention_kernel(tree_args a) {
       __builtin_amdgcn_sched_barrier(0);
       if (in.masked) hide(acc, now, in);
       else seen = (1 << NB) - 1;
-      move_maximum(acc, nullptr);
+      move_maximum(acc, wt, std::false_type{});
       weigh(acc, wt, t, in.masked);
       if (in.masked) clean_v(in, now.k.len);
       multiply_v(wt);
@@ -816,7 +879,7 @@ tree_attention_kernel(tree_args a) {
     }
   } else {
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) ask(i);
+    for (int i = 0; i < 4; ++i) ask(request_of(i, look()));
     load_queries(now, col);
     wait_loads();
     A3_LDS_BARRIER();
@@ -827,35 +890,76 @@ tree_attention_kernel(tree_args a) {
     columns col_next = col;
     multiply_k(acc, 0);
     int t = 0;
-    slab_info in;
-    bool last;
+    request r;
     auto next_step = [&]() {
-      // K of step t + 1 and V of step t - 1 are there; nobody reads K of step t and V of step t - 2 any more
+      // K of step t + 2 and V of step t are there; nobody reads K of step t and V of step t - 2 any more
       arrive();
-      ask(t + 4);
-      in = info_of(now, queue[0]);
-      last = now.step == now.k.steps - 1 || t + 1 == n_steps;
+      r = request_of(t + 4, look());
     };
     next_step();
     for (;;) {
-      while (pending && !in.masked && !before.masked && !last) {         // the common way: all of it at once
-        move_maximum(acc, &wt);
+      // The common way: V's products of the step before, K's of the next one and this one's weights, which need nothing of one another.  A wave
+      // issues in order, so they stand in turn, an equal part of the weights and of the loads behind every NB x 2 products.
+      const int first_slot = slot_of(place{0, 0, 0, 0, {}}), full = now.k.len - first_slot >= SK ? (now.k.len - first_slot - SK) / F::kStep + 1 : 0;
+      int plain = !pending || before.masked ? 0 : min(min(full, now.k.steps - 1) - now.step, n_steps - 1 - t);
+      plain = min(plain, count_simple());
+      if (plain > 0 && !(missing & 1)) {
+       take_k(t + 1);
+       do {
+        constexpr int kWide = Q8 ? 2 : 1, kParts = F::NK * kWide + D / 16, kWeigh = NB * F::NS / 2;
+        move_maximum(acc, wt, std::true_type{});
         logits acc_next;
         weights wt_next;
+        take_scales(t);
         take_v(t - 1);
-        multiply_k(acc_next, t + 1);
-        weigh(acc, wt_next, t, false);
-        multiply_v(wt);
+        __builtin_amdgcn_sched_barrier(0);
+        each_of<kParts>([&](auto part) {
+          constexpr int p = part, pv = p - (kParts - D / 16);
+          if constexpr (pv >= 0) multiply_v_part(wt, pv);
+          else if constexpr (p % kWide == 0) multiply_k_part(acc_next, p / kWide);
+          if constexpr (pv == 0) {
+            scale_k(acc_next);
+            take_k(t + 2);
+          }
+          each_of<kWeigh * (p + 1) / kParts - kWeigh * p / kParts>([&](auto i) {
+            constexpr int q = kWeigh * p / kParts + i, nb = q / (F::NS / 2), e = q % (F::NS / 2);
+            weigh_two(acc, wt_next, nb, e, false);
+          });
+          each_of<F::kPer * (p + 1) / kParts - F::kPer * p / kParts>([&](auto i) { ask_part(r, F::kPer * p / kParts + i); });
+          if constexpr (pv >= 0 || p % kWide == kWide - 1) {
+            // (products too would else move behind the barrier)
+            if constexpr (pv >= 0) {
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+a"(o[nb][pv]));
+            } else {
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int b = 0; b < F::KB; ++b) asm volatile("" : "+a"(acc_next[nb][b]));
+            }
+#pragma unroll
+            for (int q = 0; q < 2 * NB * (pv >= 0 ? 1 : kWide); ++q) {
+              __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+              __builtin_amdgcn_sched_group_barrier(0x402, 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        });
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int b = 0; b < F::KB; ++b) acc[nb][b] = acc_next[nb][b];
         wt = wt_next;
-        before = in;
         ++now.step;
         ++t;
-        next_step();
+        arrive();
+        r = request_of(t + 4, look_simply());
+       } while (--plain > 0 && !(missing & 1));
+       before.masked = false;
       }
+      ask(r);
+      const slab_info in = info_of(now, missing & 1 ? 0 : now.k.end - slot_of(now));
+      const bool last = now.step == now.k.steps - 1 || t + 1 == n_steps;
       if (pending) {
         take_v(t - 1);
         if (before.masked) clean_v(before, now.k.len);
@@ -863,7 +967,7 @@ tree_attention_kernel(tree_args a) {
       }
       if (in.masked) hide(acc, now, in);
       else seen = (1 << NB) - 1;
-      move_maximum(acc, nullptr);
+      move_maximum(acc, wt, std::false_type{});
       weigh(acc, wt, t, in.masked);
       if (!last) {
         multiply_k(acc, t + 1);
@@ -874,7 +978,6 @@ tree_attention_kernel(tree_args a) {
         const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1;
         place p = now;
         if (more) advance(p);
-        arrive();                                              // V of this step
         if (more) load_queries(p, col_next);
         take_v(t);
         if (in.masked) clean_v(in, now.k.len);
