@@ -29,55 +29,68 @@ __device__ __forceinline__ unsigned long long max_of_lanes(unsigned long long k,
 }
 
 // The largest logit of a slice of a row.  A thread keeps the maximum of its values and the chunk of 32 that it came from: one instruction a
-// value, so that reading is all that counts.  Its key is found in that chunk afterwards.  (A maximum of -inf says nothing: all may be NaN.)
+// value, so that reading is all that counts.  The key of the largest is found in that chunk afterwards, by the threads that have it alone.  (A
+// maximum of -inf says nothing: all may be NaN.)
 template <typename T>
 __global__ void __launch_bounds__(kLpThreads)
 pick_kernel(accept_args a) {
-  typedef lp_row<T> R;
+  typedef lp_row<T, true> R;
   constexpr int V = R::V, U = R::U, kChunk = R::kChunk;
-  __shared__ unsigned long long best[4];
+  __shared__ unsigned long long best;
+  __shared__ float tops[4];
   const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x;
   R r;
   r.x = (const T *)a.x + (size_t)row * a.ld;
   r.vocab = a.vocab;
-  r.skew = (int)(((uintptr_t)r.x & 15) / sizeof(T));
-  const int n_vec = (int)(((long long)a.vocab + r.skew + V - 1) / V), per = n_vec / a.slices, rest = n_vec - per * a.slices;
+  r.skew = 0;
+  const int n_vec = (a.vocab + V - 1) / V, per = n_vec / a.slices, rest = n_vec - per * a.slices;
   r.v0 = slice * per + min(slice, rest);
   r.v1 = r.v0 + per + (slice < rest ? 1 : 0);
+  // Where the slice or the row ends some of it is read again: the maximum minds no value twice, and the loads need no branches.
+  typename R::vec_t raw[U];
+  auto element = [&](int c, int u) {
+    const int e = min(c + u * kLpThreads + tid, r.v1 - 1) * V;
+    return r.vocab >= V ? min(e, r.vocab - V) : e;
+  };
+  auto load = [&](int c) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      raw[u] = r.vocab >= V ? *reinterpret_cast<const typename R::vec_any *>(r.x + element(c, u)) : r.vec(0);
+  };
   float m = -INFINITY;
-  int from = -1;
-  for (int c = r.v0; c < r.v1; c += kChunk) {
-    typename R::vec_t raw[U];
-    if (c * V >= r.skew && c + kChunk <= r.v1 && (long long)(c + kChunk) * V - r.skew <= r.vocab) {
-      const T *x = r.x + ((long long)c * V - r.skew);
-#pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const typename R::vec_t *>(x + (u * kLpThreads + tid) * V);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = r.vec(c + u * kLpThreads + tid);
-    }
+  int from = r.v0, c = r.v0;
+  for (;; c += kChunk) {
+    load(c);
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kLpValues; ++i) top = fmaxf(top, (float)raw[i / V][i % V]);
     if (top > m) { m = top; from = c; }
+    if (c + kChunk >= r.v1) break;
   }
-  unsigned long long k = 0;
-  const bool all = __syncthreads_and(m == -INFINITY);          // nothing but -inf and NaN: every value is looked at
-  for (int c = all ? r.v0 : from; c >= 0 && c < r.v1; c = all ? c + kChunk : -1)
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = c + u * kLpThreads + tid;
-      const typename R::vec_t raw = r.vec(v);
-#pragma unroll
-      for (int i = 0; i < V; ++i) { const unsigned long long x = r.key(v, i, (float)raw[i]); k = x > k ? x : k; }
-    }
-  k = max_of_lanes(k, 64);
-  if ((tid & 63) == 0) best[tid >> 6] = k;
+  const float mw = wave_max(m);
+  if ((tid & 63) == 0) tops[tid >> 6] = mw;
+  if (tid == 0) best = 0;
   __syncthreads();
-  if (tid != 0) return;
+  const float M = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  const bool all = M == -INFINITY;                             // nothing but -inf and NaN: every value is looked at
+  if (all || m == M) {
+    unsigned long long k = 0;
+    for (int at = all ? r.v0 : from; at < r.v1; at = all ? at + kChunk : r.v1) {
+      if (at != c) load(at);
+      c = at;
 #pragma unroll
-  for (int w = 1; w < 4; ++w) k = best[w] > k ? best[w] : k;
-  a.part[blockIdx.x] = k;
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int e = element(at, u) + i;
+          const unsigned long long x = e < r.vocab ? top_key((float)raw[u][i], e) : 0ull;
+          k = x > k ? x : k;
+        }
+    }
+    atomicMax(&best, k);                                       // (the order does not matter)
+  }
+  __syncthreads();
+  if (tid == 0) a.part[blockIdx.x] = best;
 }
 
 // Workgroup g < n_groups follows the tree of group g; the others write the picks of 64 rows each (rows may be in no group).
@@ -145,81 +158,86 @@ follow_kernel(accept_args a) {
   }
 }
 
-// Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of no less than a vector a thread.
+// Slices of a row: few rows are cut so that some thousand workgroups share the reading, into pieces of a chunk at least.
 constexpr int kPickPieces = 2048;
-int pick_slices(int n_rows, int vocab, int elem) {
+int pick_slices(int n_rows, int vocab) {
   const int by_rows = n_rows >= kPickPieces ? 1 : (kPickPieces + n_rows - 1) / n_rows;
-  const long long by_size = (long long)vocab * elem / (16 * kLpThreads);
-  return by_size < 1 ? 1 : by_size < by_rows ? (int)by_size : by_rows < 128 ? by_rows : 128;
+  const int by_size = (int)(((long long)vocab + kLpValues * kLpThreads - 1) / (kLpValues * kLpThreads));
+  return by_size < by_rows ? by_size : by_rows < 128 ? by_rows : 128;
 }
 
 // ---------------------------------------------------------------------------------------
 // cache rows moved
 // ---------------------------------------------------------------------------------------
-constexpr int kLayersAtOnce = 64;
+constexpr int kLayersAtOnce = 64, kMoveGroups = 8192, kMoveSlots = 256;      // (slots of all moves of a set that a workgroup has at once)
 struct move_args {
   pages_args p;                        // (pools: of the layers below)
   char *pools[2 * kLayersAtOnce];      // K and V of every layer
   const int *src_req, *src_slot, *dst_req, *dst_slot, *n_slots;
   int max_slots, set_size, row_bytes, q8;
-  int row_shift, slot_shift, groups;   // a workgroup: 2^row_shift vectors of a row, 2^slot_shift slots, 256 >> both KV heads; groups of those
+  // a workgroup: 2^row_shift vectors of a row, 2^slot_shift slots, `heads` KV heads (256 >> both shifts); groups of those, units: of all pools
+  int row_shift, slot_shift, heads, groups, units;
   size_t head_bytes;
 };
 
-// The physical slot of a request's, -1 where there is none.  (Everything is looked up, whether it is needed or not: the moves of a set are
-// on their way together.)
+// The physical slot of a request's, -1 where there is none.
 __device__ __forceinline__ long long place_of(const pages_args &p, int req, int first, int o) {
   const long long slot = (long long)first + o;
-  const bool in = req >= 0 && req < p.n_req && first >= 0 && slot < p.slots;
-  const int page = p.table[in ? (size_t)req * p.max_pages + (size_t)(slot >> p.page_shift) : 0];
-  return in && page >= 0 && page < p.n_pages ? ((long long)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1)) : -1;
+  if (req < 0 || req >= p.n_req || first < 0 || slot >= p.slots) return -1;
+  const int page = p.table[(size_t)req * p.max_pages + (size_t)(slot >> p.page_shift)];
+  return page >= 0 && page < p.n_pages ? ((long long)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1)) : -1;
 }
 
 // A thread has 16 bytes of one KV head at one slot o of the runs, of all N moves of its set: it reads them all, then writes them all, and no
 // other thread touches what it does, so that a set needs neither a barrier nor a copy in between.  8-bit pages: then the scales, four bytes
-// a slot.  Bound by memory (reading and writing the rows that change their place).
+// a slot.  Where the slots are is the same in every pool and head: looked up once, for every gridDim.z-th of them.  Bound by memory (reading and
+// writing the rows that change their place).
 template <int N>
 __global__ void __launch_bounds__(256)
 move_kernel(move_args a) {
-  const int set = blockIdx.y, tid = threadIdx.x, pool_no = blockIdx.z / a.groups, group = blockIdx.z - pool_no * a.groups;
-  char *pool = a.pools[pool_no];
-  struct one { int from, to, n, sr, dr; };
-  __shared__ one list[N];
-  if (tid < N) {
-    const size_t i = (size_t)set * a.set_size + min(tid, a.set_size - 1);
-    list[tid] = {a.src_slot[i], a.dst_slot[i], tid < a.set_size ? min(a.n_slots ? a.n_slots[i] : 1, a.max_slots) : 0, a.src_req ? a.src_req[i] : set,
-                 a.dst_req ? a.dst_req[i] : set};
-  }
+  const int set = blockIdx.y, tid = threadIdx.x, slots = 1 << a.slot_shift, slot_mask = (1 << a.p.page_shift) - 1;
+  struct place { long long from, to; int from_slot, to_slot; };        // of a page in the pool (to < 0: nothing to move); a slot of it
+  __shared__ place places[N * (kMoveSlots / N)];
+  __shared__ int last[N];
+  const size_t first = (size_t)set * a.set_size;
+  const int m_of = tid & (N - 1), m_at = min(m_of, a.set_size - 1);
+  const int from = a.src_slot[first + m_at], to = a.dst_slot[first + m_at], n = m_of < a.set_size ? min(a.n_slots ? a.n_slots[first + m_at] : 1, a.max_slots) : 0,
+            from_req = a.src_req ? a.src_req[first + m_at] : set, to_req = a.dst_req ? a.dst_req[first + m_at] : set;
+  if (tid < N) last[tid] = n;
   __syncthreads();
   int most = 0;
 #pragma unroll 8
-  for (int m = 0; m < N; ++m) most = max(most, list[m].n);
-  // Moves words W of KV head h at slot o: the lane's `at` bytes into the slot's `width` bytes, `begin` bytes into the head's page.
-  auto move = [&](auto word, int o, int h, size_t begin, int width, int at) {
+  for (int m = 0; m < N; ++m) most = max(most, last[m]);
+  // Moves words W of slot `so` of these, of KV heads h, h + heads a pool, ..: the lane's `at` bytes into the slot's `width` bytes.
+  auto move = [&](auto word, int so, int h, size_t at, int width) {
     typedef decltype(word) W;
-    W x[N];
-    long long dst[N];
+    const place *p = places + so * N;
+    for (int unit = blockIdx.z; unit < a.units; unit += gridDim.z) {
+      const int pool_no = unit / a.groups, head = (unit - pool_no * a.groups) * a.heads + h;
+      char *pool = a.pools[pool_no] + (size_t)head * a.head_bytes + at;
+      if (head >= a.p.Hkv) continue;
+      W x[N];
 #pragma unroll
-    for (int m = 0; m < N; ++m) {
-      const one l = list[m];
-      const long long from = place_of(a.p, l.sr, l.from, o), to = place_of(a.p, l.dr, l.to, o);
-      const bool on = o < l.n && from >= 0 && to >= 0 && from != to && h < a.p.Hkv;
-      auto where = [&](long long place) {
-        return (long long)(((size_t)(place >> a.p.page_shift) * a.p.Hkv + h) * a.head_bytes + begin +
-                           (size_t)(place & ((1 << a.p.page_shift) - 1)) * width + at);
-      };
-      x[m] = *reinterpret_cast<const W *>(pool + (on ? where(from) : 0));
-      dst[m] = on ? where(to) : -1;
+      for (int m = 0; m < N; ++m)
+        if (p[m].to >= 0) x[m] = *reinterpret_cast<const W *>(pool + p[m].from + (uint32_t)(p[m].from_slot * width));
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+        if (p[m].to >= 0) *reinterpret_cast<W *>(pool + p[m].to + (uint32_t)(p[m].to_slot * width)) = x[m];
     }
-#pragma unroll
-    for (int m = 0; m < N; ++m)
-      if (dst[m] >= 0) *reinterpret_cast<W *>(pool + dst[m]) = x[m];
   };
-  const int heads = 256 >> (a.row_shift + a.slot_shift), slots = 1 << a.slot_shift;
-  const int c = tid & ((1 << a.row_shift) - 1), so = (tid >> a.row_shift) & (slots - 1), h = group * heads + (tid >> (a.row_shift + a.slot_shift));
   for (int o0 = blockIdx.x * slots; o0 < most; o0 += gridDim.x * slots) {
-    move(a3_u32x4{}, o0 + so, h, 0, a.row_bytes, 16 * c);
-    if (a.q8 && tid < slots * heads) move(uint32_t{}, o0 + (tid & (slots - 1)), group * heads + (tid >> a.slot_shift), (size_t)a.row_bytes << a.p.page_shift, 4, 0);
+    for (int i = tid; i < N * slots; i += 256) {               // (256 is a multiple of N: a thread has one move of the set)
+      const int o = o0 + i / N;
+      const long long x = o < n ? place_of(a.p, from_req, from, o) : -1, y = o < n ? place_of(a.p, to_req, to, o) : -1;
+      const size_t page_bytes = a.p.Hkv * a.head_bytes;
+      places[i] = x >= 0 && y >= 0 && x != y ? place{(long long)((x >> a.p.page_shift) * page_bytes), (long long)((y >> a.p.page_shift) * page_bytes),
+                                                     (int)(x & slot_mask), (int)(y & slot_mask)}
+                                             : place{0, -1, 0, 0};
+    }
+    __syncthreads();
+    move(a3_u32x4{}, (tid >> a.row_shift) & (slots - 1), tid >> (a.row_shift + a.slot_shift), 16 * (tid & ((1 << a.row_shift) - 1)), a.row_bytes);
+    if (a.q8 && tid < slots * a.heads) move(uint32_t{}, tid & (slots - 1), tid >> a.slot_shift, (size_t)a.row_bytes << a.p.page_shift, 4);
+    __syncthreads();
   }
 }
 
@@ -231,7 +249,8 @@ move_kernel(move_args a) {
 // that starts, so that beams that are the same have the same sums.  A chunk's 32 exponentials are summed in float, chunks in double.
 // A second kernel, one workgroup a group, makes worths of its lists (one of every slice of every beam, best first) in double and puts
 // them together: the n_best-th of the lists' heads (or of their first few, where there are fewer lists) bounds what can be among the best,
-// what reaches it is gathered, at most n_best values of n_best lists, and ranked by counting.
+// what reaches it is gathered, n_best^2 values at most, and ranked by counting.  It is a chain of latencies: three trips to
+// memory, and nothing that goes through all lists one by one.
 struct beam_args {
   const void *x;
   long long ld;
@@ -325,59 +344,105 @@ beam_row_kernel(beam_args a) {
 struct candidate { double worth; unsigned long long id; };
 __device__ __forceinline__ bool before(const candidate &a, const candidate &b) { return a.worth > b.worth || (a.worth == b.worth && a.id < b.id); }
 
-constexpr int kBeamLists = 512, kBeamHeads = kBeamLists + kMaxBest;
+constexpr int kBeamLists = 512, kBeamHeads = kBeamLists + kMaxBest, kHeadsAThread = (kBeamHeads + 255) / 256;
 __global__ void __launch_bounds__(256)
 beam_join_kernel(beam_args a) {
   extern __shared__ candidate gathered[];                      // [n_best * n_best]
   __shared__ candidate head[kBeamHeads], bound;
   __shared__ double base[kMaxBeams];
   __shared__ unsigned char kind[kMaxBeams];                    // 0: no candidates, 1: logits, 2: has ended
-  __shared__ int count;
+  __shared__ unsigned short place[kBeamHeads], chosen[kMaxBest];       // of the heads kept; lists that may have more of the best
+  __shared__ uint32_t bounds[4];
+  __shared__ int count, kept, n_lists;
   const int g = blockIdx.x, tid = threadIdx.x, lists = a.n_beams * a.slices, first = g * a.n_beams;
-  // worth of a logit: base + x
-  for (int b = tid; b < a.n_beams; b += 256) {
-    const float s = a.score[first + b];
-    const bool ended = a.done && a.done[first + b];
+  // the lists' first `deep`: n_best of them at least, more where there are threads for them
+  const int deep = min(a.n_best, max((a.n_best + lists - 1) / lists, 256 / lists)), heads = lists * deep;
+  const unsigned long long *tops = a.part_top + (size_t)first * a.slices * a.n_best;
+  unsigned long long keys[kHeadsAThread];                      // (on their way while the beams' sums are joined)
+#pragma unroll
+  for (int q = 0; q < kHeadsAThread; ++q) {
+    const int i = min(tid + 256 * q, heads - 1);
+    keys[q] = tops[(size_t)(i / deep) * a.n_best + i % deep];
+  }
+  if (tid == 0) { bound = candidate{-INFINITY, 0}; count = kept = n_lists = 0; }
+  // worth of a logit: base + x; as many lanes a beam as it has slices
+  int lanes = 1;
+  while (lanes < 64 && lanes < a.slices) lanes <<= 1;
+  for (int b0 = 0; b0 < a.n_beams; b0 += 256 / lanes) {
+    const int b = b0 + tid / lanes, bb = min(b, a.n_beams - 1);
+    const float s = a.score[first + bb];
+    const bool ended = a.done && a.done[first + bb];
     int k = !(fabsf(s) < INFINITY) ? 0 : ended ? 2 : 1;
     double M = -INFINITY, Z = 0.0;
-    if (k == 1) {
-      const double2 *p = a.part + (size_t)(first + b) * a.slices;
-      for (int i = 0; i < a.slices; ++i) M = fmax(M, p[i].x);
-      for (int i = 0; i < a.slices; ++i) Z += p[i].x == -INFINITY && p[i].y == 0.0 ? 0.0 : p[i].y * exp(p[i].x - M);
+    if (k == 1) {                                              // (the same in all lanes of a beam)
+      const double2 *p = a.part + (size_t)(first + bb) * a.slices;
+      for (int i = tid % lanes; i < a.slices; i += lanes) {
+        const double2 x = p[i];
+        if (x.x == -INFINITY && x.y == 0.0) continue;
+        const double up = fmax(M, x.x);
+        Z = (M == up ? Z : Z * exp(M - up)) + (x.x == up ? x.y : x.y * exp(x.x - up));
+        M = up;
+      }
+      double up = M;
+      for (int o = lanes >> 1; o; o >>= 1) up = fmax(up, __shfl_xor(up, o));
+      Z = M == up || Z == 0.0 ? Z : Z * exp(M - up);
+      for (int o = lanes >> 1; o; o >>= 1) Z += __shfl_xor(Z, o);
+      M = up;
       if (!(Z > 0.0 && Z < INFINITY && fabs(M) < INFINITY)) k = 0;
     }
-    kind[b] = (unsigned char)k;
-    base[b] = k == 2 ? (double)s : (double)s - M - log(Z);
+    if (b < a.n_beams && tid % lanes == 0) {
+      kind[b] = (unsigned char)k;
+      base[b] = k == 2 ? (double)s : (double)s - M - log(Z);
+    }
   }
-  if (tid == 0) count = 0;
   __syncthreads();
-  auto at = [&](int list, int j) {                             // the jth of a list
+  auto made = [&](int list, int j, unsigned long long key) {   // the jth of a list
     const int b = list / a.slices;
     const unsigned long long id = (unsigned long long)b << 32;
     if (kind[b] == 0) return candidate{-INFINITY, 0};
     if (kind[b] == 2) return list == b * a.slices && j == 0 ? candidate{base[b], id | (uint32_t)a.end} : candidate{-INFINITY, 0};
-    const unsigned long long k = a.part_top[((size_t)first * a.slices + list) * a.n_best + j];
-    return k ? candidate{base[b] + (double)top_value(k), id | (uint32_t)~(uint32_t)k} : candidate{-INFINITY, 0};
+    return key ? candidate{base[b] + (double)top_value(key), id | (uint32_t)~(uint32_t)key} : candidate{-INFINITY, 0};
   };
-  const int deep = (a.n_best + lists - 1) / lists, heads = lists * deep;      // at least n_best of them
-  for (int i = tid; i < heads; i += 256) head[i] = at(i / deep, i % deep);
-  if (tid == 0) bound = candidate{-INFINITY, 0};
+  // A first bound: the largest of the waves' n_best-th heads, in float; the heads that reach it are ranked.
+  candidate mine[kHeadsAThread];
+  uint32_t order[kHeadsAThread];
+#pragma unroll
+  for (int q = 0; q < kHeadsAThread; ++q) {
+    const int i = tid + 256 * q;
+    mine[q] = i < heads ? made(i / deep, i % deep, keys[q]) : candidate{-INFINITY, 0};
+    order[q] = mine[q].worth > -INFINITY ? max(top_order((float)mine[q].worth), 1u) : 0u;
+  }
+  const uint32_t nth = wave_nth<32, kHeadsAThread>(order, a.n_best);
+  if ((tid & 63) == 0) bounds[tid >> 6] = nth;
   __syncthreads();
-  for (int i = tid; i < heads; i += 256) {
+  const uint32_t reach = max(max(bounds[0], bounds[1]), max(max(bounds[2], bounds[3]), 1u));
+#pragma unroll
+  for (int q = 0; q < kHeadsAThread; ++q)
+    if (order[q] >= reach) {
+      const int to = atomicAdd(&kept, 1);
+      head[to] = mine[q];
+      place[to] = (unsigned short)(tid + 256 * q);
+    }
+  __syncthreads();
+  const int n_heads = kept;
+  for (int i = tid; i < n_heads; i += 256) {
     const candidate c = head[i];
     int rank = 0;
 #pragma unroll 4
-    for (int o = 0; o < heads; ++o) rank += before(head[o], c);
-    if (rank == a.n_best - 1 && c.worth > -INFINITY) bound = c;
+    for (int o = 0; o < n_heads; ++o) rank += before(head[o], c);
+    if (rank >= a.n_best) continue;
+    if (rank == a.n_best - 1) bound = c;
+    gathered[atomicAdd(&count, 1)] = c;
+    if (deep < a.n_best && place[i] % deep == deep - 1) chosen[atomicAdd(&n_lists, 1)] = (unsigned short)(place[i] / deep);
   }
   __syncthreads();
   const candidate last = bound;                                // (none: all there are)
-  for (int i = tid; i < lists; i += 256)
-    for (int j = 0; j < a.n_best; ++j) {
-      const candidate c = at(i, j);
-      if (!(c.worth > -INFINITY) || (last.worth > -INFINITY && before(last, c))) break;
-      gathered[atomicAdd(&count, 1)] = c;
-    }
+  const int more = a.n_best - deep;
+  for (int i = tid; i < n_lists * more; i += 256) {
+    const int list = chosen[i / more], j = deep + i % more;
+    const candidate c = made(list, j, tops[(size_t)list * a.n_best + j]);
+    if (c.worth > -INFINITY && !(last.worth > -INFINITY && before(last, c))) gathered[atomicAdd(&count, 1)] = c;
+  }
   __syncthreads();
   const int n = count;
   for (int i = tid; i < n; i += 256) {
@@ -452,7 +517,7 @@ extern "C" a3_status a3_tree_accept(int dtype, const void *logits, int vocab, lo
   A3_REQUIRE(logits == nullptr || (ws && a3_aligned16(ws) && ws_bytes >= need), A3_ERR_WORKSPACE,
              "a3_tree_accept: workspace %zu bytes (16-byte aligned), need %zu", ws ? ws_bytes : 0, need);
   accept_args a{logits, ld, vocab, picked, tokens, parent, group_start, group_len, n_groups, n_rows, max_rows, max_path,
-                count, path, next_token, src_slot, dst_slot, n_rows ? pick_slices(n_rows, vocab, dtype == A3_BF16 ? 2 : 4) : 1,
+                count, path, next_token, src_slot, dst_slot, n_rows ? pick_slices(n_rows, vocab) : 1,
                 (unsigned long long *)ws};
   const int more = logits ? (int)(((long long)n_rows + 63) / 64) : 0;
   A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31) && (long long)n_groups + more < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_tree_accept: too many rows");
@@ -497,27 +562,28 @@ extern "C" a3_status a3_paged_move(const a3_pages *layers, int n_layers, const i
   a.head_bytes = page_head_bytes(layers->format, elem_bytes(layers), layers->page_size, layers->head_dim);
   a.row_shift = __builtin_ctz((unsigned)(a.row_bytes / 16));
   a.slot_shift = 0;
-  while (a.slot_shift < 8 - a.row_shift && (1 << a.slot_shift) < a.max_slots) ++a.slot_shift;
-  const int heads = 256 >> (a.row_shift + a.slot_shift);
-  a.groups = (layers->n_kv_heads + heads - 1) / heads;
-  const int at_once = 65535 / (2 * a.groups) < kLayersAtOnce ? 65535 / (2 * a.groups) : kLayersAtOnce;
-  A3_REQUIRE(at_once >= 1, A3_ERR_UNSUPPORTED, "a3_paged_move: %d KV heads", layers->n_kv_heads);
+  int size = 2;
+  while (size < set_size) size *= 2;
+  while (a.slot_shift < 8 - a.row_shift && (1 << a.slot_shift) < a.max_slots && (size << a.slot_shift) < kMoveSlots) ++a.slot_shift;
+  a.heads = 256 >> (a.row_shift + a.slot_shift);
+  a.groups = (layers->n_kv_heads + a.heads - 1) / a.heads;
   // (the runs may be shorter than max_slots says: some workgroups that go on along them, not one for each piece that there might be)
   const long long tiles = ((long long)a.max_slots + (1 << a.slot_shift) - 1) >> a.slot_shift;
-  for (int l0 = 0; l0 < n_layers; l0 += at_once) {
-    const int n = n_layers - l0 < at_once ? n_layers - l0 : at_once;
+  for (int l0 = 0; l0 < n_layers; l0 += kLayersAtOnce) {
+    const int n = n_layers - l0 < kLayersAtOnce ? n_layers - l0 : kLayersAtOnce;
     for (int l = 0; l < n; ++l) {
       a.pools[2 * l] = (char *)layers[l0 + l].k_pool;
       a.pools[2 * l + 1] = (char *)layers[l0 + l].v_pool;
     }
-    const long long others = (long long)n_sets * 2 * n * a.groups, want = (8192 + others - 1) / others;
-    const dim3 grid((unsigned)(tiles < want ? tiles : want), (unsigned)n_sets, (unsigned)(2 * n * a.groups));
+    a.units = 2 * n * a.groups;
+    const long long gx = tiles < kMoveGroups ? tiles : kMoveGroups, others = gx * n_sets, want = (kMoveGroups + others - 1) / others;
+    const dim3 grid((unsigned)gx, (unsigned)n_sets, (unsigned)(a.units < want ? a.units : want));
     auto launch = [&](auto size) { hipLaunchKernelGGL(move_kernel<size.value>, grid, dim3(256), 0, (hipStream_t)stream, a); };
-    if (set_size <= 2) launch(std::integral_constant<int, 2>{});
-    else if (set_size <= 4) launch(std::integral_constant<int, 4>{});
-    else if (set_size <= 8) launch(std::integral_constant<int, 8>{});
-    else if (set_size <= 16) launch(std::integral_constant<int, 16>{});
-    else if (set_size <= 32) launch(std::integral_constant<int, 32>{});
+    if (size == 2) launch(std::integral_constant<int, 2>{});
+    else if (size == 4) launch(std::integral_constant<int, 4>{});
+    else if (size == 8) launch(std::integral_constant<int, 8>{});
+    else if (size == 16) launch(std::integral_constant<int, 16>{});
+    else if (size == 32) launch(std::integral_constant<int, 32>{});
     else launch(std::integral_constant<int, 64>{});
     A3_CHECK_LAUNCH("a3_paged_move");
   }
