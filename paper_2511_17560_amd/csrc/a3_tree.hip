@@ -67,15 +67,14 @@ struct tree_form {
   static constexpr int kStep = WS * SK;
   static constexpr bool kOnce = WC_ == 1;                      // a cache is read once: nontemporal
   static constexpr int kBlocks = NB * D / 16;                  // accumulator blocks of a wave
-  static constexpr bool kLds = sizeof(T) == 2 && WC_ > 1 && NB_ > 2;      // through LDS: rings of K and V, four steps each, and of scales, eight steps
+  static constexpr bool kLds = sizeof(T) == 2 && WC_ > 2;      // through LDS: rings of K and V, and of scales, four steps each
   static constexpr int kHalf = SK * kRow, kKV = WS * kHalf, kScaleAt = 8 * kKV;
   static constexpr int kLoads = kRow / 32 >= WC ? kRow / 32 / WC : 1;          // direct-to-LDS loads of a wave, of K and of V, a step
   static constexpr int kPer = 2 * kLoads + (Q8 ? 1 : 0);
-  // blocks that half of the waves exchange at once, when waves are joined: in room of their own, or in two steps of the ring of V
-  static constexpr int kRoom = kKV / 1024 / (W_ / 4 > 0 ? W_ / 4 : 1);
-  static constexpr int kAtOnce = !kLds || kRoom >= kBlocks ? kBlocks : kRoom;
-  static constexpr int kLdsBytes = kLds ? kScaleAt + (Q8 ? 16 * WS * 256 : 0) : WS > 1 ? W_ / 2 * kBlocks * 1024 : 16;
-  static constexpr int kWaves = kLds ? 1 : kF32 && D == 128 && NB_ == 2 ? 1 : Q8 && sizeof(T) == 4 && D == 128 && NB_ == 2 ? 1 : 2;   // a SIMD
+  static constexpr int kAtOnce = kLds ? 4 : kBlocks;           // blocks that half of the waves exchange at once, when waves are joined
+  static constexpr int kRoomAt = kLds ? kScaleAt + (Q8 ? 8 * WS * 256 : 0) : 0;
+  static constexpr int kLdsBytes = kRoomAt + (WS > 1 ? W_ / 2 * kAtOnce * 1024 : 16);
+  static constexpr int kWaves = kF32 && D == 128 && NB_ == 2 ? 1 : Q8 && sizeof(T) == 4 && D == 128 && NB_ == 2 ? 1 : 2;   // a SIMD
 };
 
 // Steps of a group's item, and items of its KV heads (0 steps: nothing of the group is written).
@@ -300,7 +299,7 @@ tree_attention_kernel(tree_args a) {
 
   // ---- through LDS: the waves that share a slab bring equal parts of it, 1 KB a load, lane after lane 16 bytes ------------------------
   // 16-byte piece c of slot s of K lies at place c ^ key(s) of its row, so that the 16 slots a quarter wave reads at one place lie in all 64
-  // banks once.  Step i of a run has place i % 4 of the rings of K and V, i % 8 of those of scales.
+  // banks once.  Step i of a run has place i % 4 of the rings.
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
   constexpr int kPieces = F::kRow / 16, kRows = 1024 / F::kRow, kHalfLoads = F::kRow / 32;     // pieces of a slot; slots of a load; loads of a slab
   auto key_of = [&](int s) { return ((s >> 3 & 3) << 2 | (s & 3)) >> (F::kRow == 256 ? 0 : F::kRow == 128 ? 1 : 2); };
@@ -324,32 +323,27 @@ tree_attention_kernel(tree_args a) {
   auto dma = [&](u32x4 page, uint32_t off, uint32_t at, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(page), "s"(at) : "memory");
   };
-  struct { size_t block; int at; } behind[2] = {{0, 0}, {0, 0}};       // the two steps whose K is asked for and whose V is not
   uint32_t missing = 0;                                        // bit q: step t + q does not count (no page, behind the tree's end)
-  struct request { u32x4 k, v, scales; uint32_t k_at, v_at, scale_at, to_k, to_v, to_scales; };
-  auto request_of = [&](int i, const where &x) {               // K of step i, V of step i - 2 (a wave has as many loads in every step)
+  struct request { u32x4 k, v, scales; uint32_t at, scale_at, to, to_scales; };
+  auto request_of = [&](int i, const where &x) {               // step i (a wave has as many loads in every step)
     request r;
     r.k = page_at(a.p.k_pool, x.block);
-    r.v = page_at(a.p.v_pool, behind[0].block);
-    r.k_at = (uint32_t)x.at * F::kRow;
-    r.v_at = (uint32_t)behind[0].at * F::kRow;
-    r.to_k = lds_base + wsl * F::kHalf + (i & 3) * F::kKV;
-    r.to_v = lds_base + wsl * F::kHalf + (4 + ((i + 2) & 3)) * F::kKV;
+    r.v = page_at(a.p.v_pool, x.block);
+    r.at = (uint32_t)x.at * F::kRow;
+    r.to = lds_base + wsl * F::kHalf + (i & 3) * F::kKV;
     if constexpr (Q8) {                                        // 64 scales, of which 32 are the slab's (behind the head's page: zeros)
-      r.scales = wc & 1 ? page_at(a.p.v_pool, x.block) : r.k;
+      r.scales = page_at(wc & 1 ? a.p.v_pool : a.p.k_pool, x.block);
       r.scale_at = (uint32_t)(D << a.p.page_shift) + 4 * x.at;
-      r.to_scales = lds_base + F::kScaleAt + ((wc & 1) * 8 + (i & 7)) * WS * 256 + wsl * 256;
+      r.to_scales = lds_base + F::kScaleAt + ((wc & 1) * 4 + (i & 3)) * WS * 256 + wsl * 256;
     }
-    behind[0] = behind[1];
-    behind[1] = {x.block, x.at};
-    missing = missing >> 1 | (x.n <= 0 ? 16u : 0u);
+    missing = missing >> 1 | (x.n <= 0 ? 8u : 0u);
     return r;
   };
   auto ask_part = [&](const request &r, int t) {               // load t of kPer
     if (t < F::kLoads) {
-      dma(r.k, dma_k[t], r.k_at, r.to_k + (wc * F::kLoads + t) % kHalfLoads * 1024);
+      dma(r.k, dma_k[t], r.at, r.to + (wc * F::kLoads + t) % kHalfLoads * 1024);
     } else if (t < 2 * F::kLoads) {
-      dma(r.v, dma_v[t - F::kLoads], r.v_at, r.to_v + (wc * F::kLoads + t - F::kLoads) % kHalfLoads * 1024);
+      dma(r.v, dma_v[t - F::kLoads], r.at, r.to + 4 * F::kKV + (wc * F::kLoads + t - F::kLoads) % kHalfLoads * 1024);
     } else {
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(r.to_scales), "v"(4 * lane), "s"(r.scales),
                    "s"(r.scale_at) : "memory");
@@ -358,11 +352,6 @@ tree_attention_kernel(tree_args a) {
   auto ask = [&](const request &r) {
 #pragma unroll
     for (int t = 0; t < F::kPer; ++t) ask_part(r, t);
-  };
-  // All loads of this wave but those of the last step are done; then those of all waves.
-  auto arrive = [&]() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::kPer) : "memory");
-    A3_LDS_BARRIER();
   };
 
   // ---- the item's columns: their rows and the queries, operand of S^T ----------------------------------------------------
@@ -458,7 +447,7 @@ tree_attention_kernel(tree_args a) {
     if constexpr (F::kLds && Q8) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
-        ks[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (i & 7) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
+        ks[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (i & 3) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
     }
   };
   auto multiply_k_part = [&](logits &acc, int x) {             // with bytes 64 x .. of the slots
@@ -545,8 +534,8 @@ tree_attention_kernel(tree_args a) {
         if (!(vis[nb] >> i & 1)) acc[nb][i >> 2][i & 3] = -INFINITY;
     }
   };
-  // The maximum moves where it has to; `pending` (if some are): weights that refer to the old one and are still to be multiplied.
-  auto move_maximum = [&](const logits &acc, weights &pending, auto some_pending) {
+  // The maximum moves where it has to.
+  auto move_maximum = [&](const logits &acc) {
     float top[NB];
     bool far = false;
 #pragma unroll
@@ -567,15 +556,6 @@ tree_attention_kernel(tree_args a) {
         l[nb] *= f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
-        if constexpr (decltype(some_pending)::value) {
-#pragma unroll
-            for (int k = 0; k < F::kPParts; ++k)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t x = pending.b[nb][k][i];
-                pending.b[nb][k][i] = two_bf16(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
-              }
-        }
       }
     }
   };
@@ -583,7 +563,7 @@ tree_attention_kernel(tree_args a) {
     if constexpr (F::kLds && Q8) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
-        vs[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (8 + (i & 7)) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
+        vs[b] = *reinterpret_cast<const f32x4 *>(lds + F::kScaleAt + (4 + (i & 3)) * WS * 256 + wsl * 256 + 32 * lg + 16 * b);
     }
   };
   auto weigh_two = [&](const logits &acc, weights &p, int nb, int q, bool masked) {    // the weights of block nb's slots 2 q and 2 q + 1
@@ -667,7 +647,7 @@ tree_attention_kernel(tree_args a) {
       }
     }
   };
-  auto multiply_v_part = [&](const weights &p, int c) {        // coordinates of block c (bf16)
+  auto v_operand = [&](int c) {                                // coordinates of block c (bf16)
     uint32_t x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -676,14 +656,14 @@ tree_attention_kernel(tree_args a) {
       else
         x[i] = __builtin_amdgcn_perm(sv[2 * i + 1][0][c >> 1], sv[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
     }
-    const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+    return words4{x[0], x[1], x[2], x[3]};
+  };
+  auto multiply_v_part = [&](const weights &p, const words4 &v, int c) {
 #pragma unroll
     for (int k = 0; k < F::kPParts; ++k)
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, p.b[nb][k]);
-        o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[nb][c], 0, 0, 0);
-      }
+      for (int nb = 0; nb < NB; ++nb)
+        o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p.b[nb][k]), o[nb][c], 0, 0, 0);
   };
   auto multiply_v = [&](const weights &p) {
     if constexpr (F::kF32) {
@@ -696,7 +676,7 @@ tree_attention_kernel(tree_args a) {
             o[nb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, sv[i][c >> 2][c & 3]), p.f[nb][i], o[nb][c], 0, 0, 0);
     } else {
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) multiply_v_part(p, c);
+      for (int c = 0; c < D / 16; ++c) multiply_v_part(p, v_operand(c), c);
     }
   };
 
@@ -726,8 +706,8 @@ tree_attention_kernel(tree_args a) {
 
   // ---- an item, or this workgroup's part of one, is done: join the waves that share columns ---------------------------------
   // Every wave brings its sums to the columns' common maximum; then half of the waves add those of the other half to their own, block by block as
-  // the registers hold them, until one wave of each has all.  i: the step at hand (through LDS: V of it and of the one before is used up).
-  auto finish = [&](const place &p, bool begins, bool ends, int i) {
+  // the registers hold them, until one wave of each has all.
+  auto finish = [&](const place &p, bool begins, bool ends) {
     const bool whole = begins && ends;
     const int slot = 2 * w + (begins ? 1 : 0), some_odd = __any(odd);
     if (lane == 0) odd_waves[wave] = some_odd;
@@ -762,11 +742,8 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[nb][c] *= f;
     }
-    constexpr int kAtOnce = F::kAtOnce, kQuarter = W / 4;
-    auto room = [&](int q) {                                   // of the qth of the waves that hand over
-      if constexpr (F::kLds) return lds + (4 + ((i - (q < kQuarter ? 1 : 0)) & 3)) * F::kKV + q % kQuarter * kAtOnce * 1024 + 16 * lane;
-      else return lds + q * kAtOnce * 1024 + 16 * lane;
-    };
+    constexpr int kAtOnce = F::kAtOnce;
+    auto room = [&](int q) { return lds + F::kRoomAt + q * kAtOnce * 1024 + 16 * lane; };      // of the qth of the waves that hand over
 #pragma unroll
     for (int half = WS / 2; half >= 1; half /= 2)
 #pragma unroll
@@ -860,7 +837,7 @@ tree_attention_kernel(tree_args a) {
       __builtin_amdgcn_sched_barrier(0);
       if (in.masked) hide(acc, now, in);
       else seen = (1 << NB) - 1;
-      move_maximum(acc, wt, std::false_type{});
+      move_maximum(acc);
       weigh(acc, wt, t, in.masked);
       if (in.masked) clean_v(in, now.k.len);
       multiply_v(wt);
@@ -869,7 +846,7 @@ tree_attention_kernel(tree_args a) {
       __builtin_amdgcn_sched_barrier(0);
       n = next.n;
       if (last) {
-        finish(now, begins, ends, t);
+        finish(now, begins, ends);
         if (begins) note_cut(now, ends, t);
         begins = true;
         clear();
@@ -878,123 +855,97 @@ tree_attention_kernel(tree_args a) {
       now = p;
     }
   } else {
+    // Two phases a step, a barrier behind each: products on the matrix unit (V of the step before, K of this one), then weights on the vector unit.
+    // The two waves of a SIMD are a phase apart.
+    const bool late = wsl == 1;
+    int t = 0;
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) ask(request_of(i, look()));
+    for (int i = 0; i < 3; ++i) ask(request_of(i, look()));
     load_queries(now, col);
     wait_loads();
+    request r = request_of(3, look());
+    int simple = count_simple();
     A3_LDS_BARRIER();
+    if (late) A3_LDS_BARRIER();
     logits acc;
-    weights wt;                                                // of the step before, where it is `pending`: V is not yet multiplied with them
-    bool pending = false;
-    slab_info before{0, 0, false};
+    weights wt;
+    words4 vt[D / 16];
     columns col_next = col;
-    multiply_k(acc, 0);
-    int t = 0;
-    request r;
-    auto next_step = [&]() {
-      // K of step t + 2 and V of step t are there; nobody reads K of step t and V of step t - 2 any more
-      arrive();
-      r = request_of(t + 4, look());
+    bool pending = false;
+    auto end_phase = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
+      A3_LDS_BARRIER();
+      __builtin_amdgcn_sched_barrier(0);
     };
-    next_step();
-    for (;;) {
-      // The common way: V's products of the step before, K's of the next one and this one's weights, which need nothing of one another.  A wave
-      // issues in order, so they stand in turn, an equal part of the weights and of the loads behind every NB x 2 products.
-      const int first_slot = slot_of(place{0, 0, 0, 0, {}}), full = now.k.len - first_slot >= SK ? (now.k.len - first_slot - SK) / F::kStep + 1 : 0;
-      int plain = !pending || before.masked ? 0 : min(min(full, now.k.steps - 1) - now.step, n_steps - 1 - t);
-      plain = min(plain, count_simple());
-      if (plain > 0 && !(missing & 1)) {
-       take_k(t + 1);
-       do {
-        constexpr int kWide = Q8 ? 2 : 1, kParts = F::NK * kWide + D / 16, kWeigh = NB * F::NS / 2;
-        move_maximum(acc, wt, std::true_type{});
-        logits acc_next;
-        weights wt_next;
-        take_scales(t);
-        take_v(t - 1);
-        __builtin_amdgcn_sched_barrier(0);
-        each_of<kParts>([&](auto part) {
-          constexpr int p = part, pv = p - (kParts - D / 16);
-          if constexpr (pv >= 0) multiply_v_part(wt, pv);
-          else if constexpr (p % kWide == 0) multiply_k_part(acc_next, p / kWide);
-          if constexpr (pv == 0) {
-            scale_k(acc_next);
-            take_k(t + 2);
-          }
-          each_of<kWeigh * (p + 1) / kParts - kWeigh * p / kParts>([&](auto i) {
-            constexpr int q = kWeigh * p / kParts + i, nb = q / (F::NS / 2), e = q % (F::NS / 2);
-            weigh_two(acc, wt_next, nb, e, false);
-          });
-          each_of<F::kPer * (p + 1) / kParts - F::kPer * p / kParts>([&](auto i) { ask_part(r, F::kPer * p / kParts + i); });
-          if constexpr (pv >= 0 || p % kWide == kWide - 1) {
-            // (products too would else move behind the barrier)
-            if constexpr (pv >= 0) {
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+a"(o[nb][pv]));
-            } else {
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int b = 0; b < F::KB; ++b) asm volatile("" : "+a"(acc_next[nb][b]));
-            }
-#pragma unroll
-            for (int q = 0; q < 2 * NB * (pv >= 0 ? 1 : kWide); ++q) {
-              __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-              __builtin_amdgcn_sched_group_barrier(0x402, 2, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
+    for (;; ++t) {
+      take_k(t);
+      if (pending) {
+        each_of<D / 16>([&](auto c) {
+          multiply_v_part(wt, vt[c], c);
+          each_of<F::kPer * (c + 1) / (D / 16) - F::kPer * c / (D / 16)>([&](auto i) { ask_part(r, F::kPer * c / (D / 16) + i); });
         });
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int b = 0; b < F::KB; ++b) acc[nb][b] = acc_next[nb][b];
-        wt = wt_next;
-        ++now.step;
-        ++t;
-        arrive();
-        r = request_of(t + 4, look_simply());
-       } while (--plain > 0 && !(missing & 1));
-       before.masked = false;
+      } else {
+        ask(r);
       }
-      ask(r);
+#pragma unroll
+      for (int x = 0; x < F::NK; ++x) multiply_k_part(acc, x);
+      // (the compiler would else move products behind the barrier)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int b = 0; b < F::KB; ++b) asm volatile("" : "+v"(acc[nb][b]));
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) asm volatile("" : "+v"(o[nb][c]));
+      }
+      end_phase();
+      take_v(t);
+      take_scales(t);
+      scale_k(acc);
       const slab_info in = info_of(now, missing & 1 ? 0 : now.k.end - slot_of(now));
       const bool last = now.step == now.k.steps - 1 || t + 1 == n_steps;
-      if (pending) {
-        take_v(t - 1);
-        if (before.masked) clean_v(before, now.k.len);
-        multiply_v(wt);
-      }
       if (in.masked) hide(acc, now, in);
       else seen = (1 << NB) - 1;
-      move_maximum(acc, wt, std::false_type{});
+      move_maximum(acc);
       weigh(acc, wt, t, in.masked);
-      if (!last) {
-        multiply_k(acc, t + 1);
-        pending = true;
-        before = in;
-        ++now.step;
-      } else {
-        const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1;
-        place p = now;
-        if (more) advance(p);
-        if (more) load_queries(p, col_next);
-        take_v(t);
-        if (in.masked) clean_v(in, now.k.len);
-        multiply_v(wt);
-        finish(now, begins, ends, t);
-        if (begins) note_cut(now, ends, t);
-        if (!more) break;
-        begins = true;
-        pending = false;
-        before.masked = false;
-        clear();
-        col = col_next;
-        multiply_k(acc, t + 1);
-        now = p;
+      if (in.masked) clean_v(in, now.k.len);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        vt[c] = v_operand(c);
+        asm volatile("" : "+v"(vt[c]));
       }
-      ++t;
-      next_step();
+      // K and V of step t + 1 are there (of this wave's loads; behind the barrier, of all)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::kPer) : "memory");
+      if (simple > 0) {
+        r = request_of(t + 4, look_simply());
+        --simple;
+      } else {
+        r = request_of(t + 4, look());
+        simple = count_simple();
+      }
+      if (!last) {
+        pending = true;
+        ++now.step;
+        end_phase();
+        continue;
+      }
+      const bool more = t + 1 < n_steps, ends = now.step == now.k.steps - 1;
+      place p = now;
+      if (more) {
+        advance(p);
+        load_queries(p, col_next);
+      }
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) multiply_v_part(wt, vt[c], c);
+      if (!late) A3_LDS_BARRIER();                             // (the late waves' products)
+      finish(now, begins, ends);
+      if (begins) note_cut(now, ends, t);
+      if (!more) break;
+      if (late) A3_LDS_BARRIER();
+      begins = true;
+      pending = false;
+      clear();
+      col = col_next;
+      now = p;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (the memory that the last loads go to is another workgroup's next)
   }
@@ -1104,7 +1055,7 @@ tree_shape shape_of(const a3_pages *P, int max_rows) {
   if (cols <= 32) return {2, 1, 4, wide ? 256 : 512};
   if (wide) return {2, 4, 4, 256};
   if (P->dtype == A3_F32) return {2, cols <= 64 ? 2 : 4, 8, 256};
-  return {cols <= 64 ? 2 : 4, 2, 4, cols <= 64 ? 512 : 256};
+  return cols <= 64 ? tree_shape{2, 2, 4, 512} : tree_shape{2, 4, 8, 256};
 }
 template <typename T, int D, bool Q8, class F>
 void with_shape(tree_shape s, F f) {
@@ -1115,8 +1066,8 @@ void with_shape(tree_shape s, F f) {
     if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 8>{});
     else f(tree_form<T, D, Q8, 2, 4, 8>{});
   }
-  else if (s.nb == 2) f(tree_form<T, D, Q8, 2, 2, 4>{});
-  else f(tree_form<T, D, Q8, 4, 2, 4>{});
+  else if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 4>{});
+  else f(tree_form<T, D, Q8, 2, 4, 8>{});
 }
 struct tree_plan { tree_shape s; int tc, tiles, shares; long long items, steps; };
 tree_plan plan_of(const a3_pages *P, int n_groups, int max_rows) {
