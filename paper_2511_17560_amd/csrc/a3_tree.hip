@@ -878,6 +878,7 @@ tree_attention_kernel(tree_args a) {
       __builtin_amdgcn_sched_barrier(0);
     };
     for (;; ++t) {
+      __builtin_amdgcn_s_setprio(1);
       take_k(t);
       if (pending) {
         each_of<D / 16>([&](auto c) {
@@ -887,6 +888,9 @@ tree_attention_kernel(tree_args a) {
       } else {
         ask(r);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      take_v(t);
+      take_scales(t);
 #pragma unroll
       for (int x = 0; x < F::NK; ++x) multiply_k_part(acc, x);
       // (the compiler would else move products behind the barrier)
@@ -897,9 +901,8 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) asm volatile("" : "+v"(o[nb][c]));
       }
+      __builtin_amdgcn_s_setprio(0);
       end_phase();
-      take_v(t);
-      take_scales(t);
       scale_k(acc);
       const slab_info in = info_of(now, missing & 1 ? 0 : now.k.end - slot_of(now));
       const bool last = now.step == now.k.steps - 1 || t + 1 == n_steps;
