@@ -37,15 +37,22 @@ struct tree_args {
 // The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float), and to a whole
 // number: what moves sums, and weights that wait, is then a power of two.
 //
-// Up to 32 columns (and fp32 rows): K and V straight from memory to registers.  One slab of registers is enough to have the next one on its
+// What bounds it: memory, as long as the cache is read once for all columns; with more columns the issue of instructions (a slab of 32 slots
+// costs a wave of 32 columns 48 matrix instructions and 180 others) and what of them does not overlap.
+//
+// Up to 64 columns (and fp32 rows): K and V straight from memory to registers.  One slab of registers is enough to have the next one on its
 // way: K of the next is asked for as soon as the products with this one's have read it, V as soon as its operands are formed, so that each
 // is under way for most of a step.  Nothing of that is conditional (a slab that does not exist is read from the pool's start and counts
 // nothing): a wait for V would otherwise have to be one for the next K too.
 //
 // More columns: the 16 slots that a quarter wave reads of K lie in as many lines, which occupies the address units four times as long as
-// whole lines do, once for each of WC waves.  There K and V come through LDS, in whole lines, once for all of them, four steps deep, V two
-// steps behind K.  The work is staggered: while the weights of step i are formed on the vector unit, the matrix unit multiplies those of
-// step i - 1 with V and K of step i + 1 with Q, so that neither waits for the other.
+// whole lines do, once for each of WC waves.  There K and V come through LDS, in whole lines, once for all of them, three steps ahead.  The
+// two waves of a SIMD are half a step apart, with a barrier at each half: while one is at the matrix unit (V of its step before, K of this
+// one), the other forms weights on the vector unit.
+//
+// Measured (one MI355X, bf16, 8 KV heads of 128, the whole call): 4 requests of 64K, 32 rows of 128 columns 261 us (4.1 TB/s; four waves of 64
+// columns, PV of one step and QK of the next between the weights, 283; without the products 206, without the weights 210); 8 of 8K, 64 rows 126 us
+// (0.49 PFLOP/s without the weights' second parts); 8 of 64K: 1 row 335 us (the single-token kernel 328), 4 rows 368, 8 rows 424, 16 rows 505.
 //
 // A lane's eight slots of a column are eight bits of the row's mask.  Only slabs that reach behind the committed slots look at it: a slot that
 // is not seen has weight 0.  0 times a value that is not finite would be NaN in the rows that do not see it, so there such values are taken out
@@ -74,7 +81,7 @@ struct tree_form {
   static constexpr int kAtOnce = kLds ? 4 : kBlocks;           // blocks that half of the waves exchange at once, when waves are joined
   static constexpr int kRoomAt = kLds ? kScaleAt + (Q8 ? 8 * WS * 256 : 0) : 0;
   static constexpr int kLdsBytes = kRoomAt + (WS > 1 ? W_ / 2 * kAtOnce * 1024 : 16);
-  static constexpr int kWaves = kF32 && D == 128 && NB_ == 2 ? 1 : Q8 && sizeof(T) == 4 && D == 128 && NB_ == 2 ? 1 : 2;   // a SIMD
+  static constexpr int kWaves = sizeof(T) == 4 && D == 128 && NB_ == 2 ? 1 : 2;             // a SIMD
 };
 
 // Steps of a group's item, and items of its KV heads (0 steps: nothing of the group is written).
@@ -1049,7 +1056,11 @@ tree_join_kernel(tree_args a) {
 
 constexpr int kMaxRows = 1024;
 
-// What a call runs in: blocks of columns a wave, waves beside each other, waves, workgroups at most.
+// What a call runs in: blocks of columns a wave, waves beside each other, waves, workgroups at most.  No more columns than rows need, as each
+// costs products.  From registers or through LDS: at 33 .. 64 columns of bf16 rows registers take 124 us for 48 ragged requests (up to 42 columns),
+// 111 for 32 of about 5K in 8-bit pages and 505 for 8 of 64K, LDS with two waves beside each other 140, 143 and 459; one wave of all 64
+// columns, one a SIMD, 142, 147 and 440: most batches are the former.  From 65 columns on LDS: 128 columns of 4 x 64K 261 us, 351 from registers.
+// fp32 rows have no LDS form: three (8-bit pages) or fp32 products a value leave the matrix unit the bound.
 struct tree_shape { int nb, wc, waves, wgs; };
 tree_shape shape_of(const a3_pages *P, int max_rows) {
   const int cols = max_rows * (P->n_q_heads / P->n_kv_heads);
