@@ -428,8 +428,8 @@ a3_status a3_pages_prepare(const a3_pages *pages, void *stream);
  * stand at their positions already (a prompt's fused cache: row_req = layout->tok_req, row_slot = layout->tok_pos), q must be
  * NULL.  k, v: [n_rows, n_kv_heads, head_dim]; q, q_out: [n_rows, n_q_heads, head_dim]; index arrays: device int32 [n_rows].
  * A row whose request, slot, page or position does not exist is skipped: nothing of it is written, q_out included (a padded
- * batch marks its rows with request or slot -1).  No two rows may name the same slot of the same request, no page may belong
- * to two requests.  Turned in float and rounded once; A3_PAGES_Q8: turned in double, so that the codes are those of the exact
+ * batch marks its rows with request or slot -1).  No two rows may name the same slot of the same request, no page that a
+ * row goes to may belong to two requests.  Turned in float and rounded once; A3_PAGES_Q8: turned in double, so that the codes are those of the exact
  * values (finite values: as with a3_quantize_q8, a NaN element does not stay one in 8 bits). */
 a3_status a3_paged_append(const a3_pages *pages, const void *k, const void *v, const int *row_req, const int *row_slot,
                           const int *row_pos, int n_rows, const void *q, void *q_out, void *stream);
@@ -532,7 +532,7 @@ a3_status a3_paged_move(const a3_pages *layers, int n_layers, const int *src_req
  *   best_score[g, j] (float), best_row[g, j] (its row of logits), best_token[g, j]
  * A token with a logit of -inf is none; a beam whose score is not finite, or whose row of logits has no distribution (NaN, +inf, nothing but
  * -inf) and that is not done, has none; where a group has fewer than n_best, the rest is -inf, -1, -1.
- * Z is summed and worths are compared beyond float's precision (double where terms meet).
+ * Z is summed in double (32 exponentials at a time in float), worths are compared in double.
  * logits: `dtype` (an a3_dtype), ld >= vocab, any start; score: float [n_groups * n_beams]; done: int32.  1 <= n_beams, n_best <= 64.
  * ws: a3_beam_select_ws_bytes() bytes (which serve fewer groups too), 16-byte aligned, contents of no concern. */
 size_t a3_beam_select_ws_bytes(int n_groups, int n_beams, int vocab, int n_best);

@@ -885,7 +885,6 @@ tree_attention_kernel(tree_args a) {
       __builtin_amdgcn_sched_barrier(0);
     };
     for (;; ++t) {
-      __builtin_amdgcn_s_setprio(1);
       take_k(t);
       if (pending) {
         each_of<D / 16>([&](auto c) {
@@ -908,7 +907,6 @@ tree_attention_kernel(tree_args a) {
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) asm volatile("" : "+v"(o[nb][c]));
       }
-      __builtin_amdgcn_s_setprio(0);
       end_phase();
       scale_k(acc);
       const slab_info in = info_of(now, missing & 1 ? 0 : now.k.end - slot_of(now));
