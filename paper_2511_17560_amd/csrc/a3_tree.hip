@@ -40,7 +40,7 @@ struct tree_args {
 // What bounds it: memory, as long as the cache is read once for all columns; with more columns the issue of instructions (a slab of 32 slots
 // costs a wave of 32 columns 48 matrix instructions and 180 others) and what of them does not overlap.
 //
-// Up to 64 columns (and fp32 rows): K and V straight from memory to registers.  One slab of registers is enough to have the next one on its
+// Up to 32 columns, up to 64 over 8-bit pages, and fp32 rows: K and V straight from memory to registers.  One slab of registers is enough to have the next one on its
 // way: K of the next is asked for as soon as the products with this one's have read it, V as soon as its operands are formed, so that each
 // is under way for most of a step.  Nothing of that is conditional (a slab that does not exist is read from the pool's start and counts
 // nothing): a wait for V would otherwise have to be one for the next K too.
@@ -52,7 +52,7 @@ struct tree_args {
 //
 // Measured (one MI355X, bf16, 8 KV heads of 128, the whole call): 4 requests of 64K, 32 rows of 128 columns 261 us (4.1 TB/s; four waves of 64
 // columns, PV of one step and QK of the next between the weights, 283; without the products 206, without the weights 210); 8 of 8K, 64 rows 126 us
-// (0.49 PFLOP/s without the weights' second parts); 8 of 64K: 1 row 335 us (the single-token kernel 328), 4 rows 368, 8 rows 424, 16 rows 505.
+// (0.49 PFLOP/s without the weights' second parts); 8 of 64K: 1 row 335 us (the single-token kernel 328), 4 rows 368, 8 rows 424, 16 rows 456.
 //
 // A lane's eight slots of a column are eight bits of the row's mask.  Only slabs that reach behind the committed slots look at it: a slot that
 // is not seen has weight 0.  0 times a value that is not finite would be NaN in the rows that do not see it, so there such values are taken out
@@ -1055,9 +1055,9 @@ tree_join_kernel(tree_args a) {
 constexpr int kMaxRows = 1024;
 
 // What a call runs in: blocks of columns a wave, waves beside each other, waves, workgroups at most.  No more columns than rows need, as each
-// costs products.  From registers or through LDS: at 33 .. 64 columns of bf16 rows registers take 124 us for 48 ragged requests (up to 42 columns),
-// 111 for 32 of about 5K in 8-bit pages and 505 for 8 of 64K, LDS with two waves beside each other 140, 143 and 459; one wave of all 64
-// columns, one a SIMD, 142, 147 and 440: most batches are the former.  From 65 columns on LDS: 128 columns of 4 x 64K 261 us, 351 from registers.
+// costs products.  33 .. 64 columns of bf16 rows, through LDS with a block a wave, or from registers with two and two waves beside each other: a
+// tree of 16 over 16K 32 and 34 us, 48 ragged chains (up to 42 columns) 125 and 124, 8 requests of 64K 456 and 505; with 8-bit pages, whose codes
+// every wave makes bf16 of, 32 requests of about 5K 157 and 111, of 8K 272 and 207.  From 65 columns on: 128 columns of 4 x 64K 260 and 351 us.
 // fp32 rows have no LDS form: three (8-bit pages) or fp32 products a value leave the matrix unit the bound.
 struct tree_shape { int nb, wc, waves, wgs; };
 tree_shape shape_of(const a3_pages *P, int max_rows) {
@@ -1067,19 +1067,21 @@ tree_shape shape_of(const a3_pages *P, int max_rows) {
   if (cols <= 32) return {2, 1, 4, wide ? 256 : 512};
   if (wide) return {2, 4, 4, 256};
   if (P->dtype == A3_F32) return {2, cols <= 64 ? 2 : 4, 8, 256};
-  return cols <= 64 ? tree_shape{2, 2, 4, 512} : tree_shape{2, 4, 8, 256};
+  if (cols <= 64 && P->format == A3_PAGES_Q8) return {2, 2, 4, 512};
+  return {cols <= 64 ? 1 : 2, 4, 8, 256};
 }
 template <typename T, int D, bool Q8, class F>
 void with_shape(tree_shape s, F f) {
-  if (s.nb == 1) f(tree_form<T, D, Q8, 1, 1, 4>{});
+  if (s.nb == 1 && s.wc == 1) f(tree_form<T, D, Q8, 1, 1, 4>{});
   else if (s.wc == 1) f(tree_form<T, D, Q8, 2, 1, 4>{});
   else if constexpr (sizeof(T) == 4 && D == 128) f(tree_form<T, D, Q8, 2, 4, 4>{});
   else if constexpr (sizeof(T) == 4) {
     if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 8>{});
     else f(tree_form<T, D, Q8, 2, 4, 8>{});
   }
-  else if (s.wc == 2) f(tree_form<T, D, Q8, 2, 2, 4>{});
-  else f(tree_form<T, D, Q8, 2, 4, 8>{});
+  else if (s.nb == 2 && s.wc == 4) f(tree_form<T, D, Q8, 2, 4, 8>{});
+  else if constexpr (Q8) f(tree_form<T, D, Q8, 2, 2, 4>{});
+  else f(tree_form<T, D, Q8, 1, 4, 8>{});
 }
 struct tree_plan { tree_shape s; int tc, tiles, shares; long long items, steps; };
 tree_plan plan_of(const a3_pages *P, int n_groups, int max_rows) {
