@@ -245,6 +245,8 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
         raise ValueError(f"buffers of {b.logits.shape[1]} logits for a vocabulary of {w_vocab.shape[0]}")
     if tree is not None and b.ws_tree is None:
         raise ValueError("buffers without room for trees for a step over trees")
+    if tree is not None and tree.n_rows != n:
+        raise ValueError(f"trees of {tree.n_rows} rows for a step of {n}")
     _fit(pages, len(layers), n if row_req is None else 0, 0, layout, prompt=False)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
@@ -321,11 +323,13 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     """One step of beam search: a token of every beam through every block, the best continuations of every group of ``out.n_beams`` rows
     (row = beam = request of the pages), and the caches of the beams that go on in place of the others: beam j of a group takes over
     slots ``first_slot`` .. + ``n_slots`` (at most ``max_slots``) of row ``out.row[g, j]``; in front of them the beams of a group have the same
-    tokens, in pages of their own or shared.  ``first_slot``, ``n_slots``: device int32 [rows], the latter counting the new token.
+    tokens, in pages of their own or shared.  ``first_slot`` (equal within a group), ``n_slots``: device int32 [rows], the latter counting the new token.
     ``score`` of every row, ``done`` and ``end_token`` as for a3_beam_select; ``out`` has as many best ones as beams.  Returns decode_stack's
     dict."""
     if out.n_best != out.n_beams:
         raise ValueError(f"beam_stack: {out.n_best} continuations for {out.n_beams} beams")
+    if layout.n_req % out.n_beams:
+        raise ValueError(f"beam_stack: {layout.n_req} rows are no groups of {out.n_beams} beams")
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, row_slot, row_pos, row_len, bufs, w_vocab=w_vocab, stream=stream)
     api.a3_beam_select(r["logits"], score, done, end_token, out, stream=stream)
     api.a3_paged_move(pages, out.row, first_slot, bufs.rows, first_slot, n_slots, max_slots, layout.n_req // out.n_beams, out.n_beams, stream=stream)
