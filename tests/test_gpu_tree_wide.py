@@ -7,7 +7,8 @@ import pytest
 import torch
 
 from oracle import candidates_oracle as cand
-from test_gpu_tree_attention import _values, attend, close, filled
+from test_gpu_tree_attention import _values, attend, check, close, filled, test_large_logits_and_a_scale_of_ones_own as large_logits
+from test_gpu_tree_attention import test_values_that_are_not_finite as values_that_are_not_finite
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,25 @@ def test_the_same_bits_whatever_else_is_in_the_batch_of_one_item_a_workgroup():
         to = (at - 30) % sum(rows)
         close(turned[to:to + rows[r]], want, np.abs(v).max(), "bf16")
         at += rows[r]
+
+
+@pytest.mark.parametrize("rows", [(9, 16), (17, 20)])
+@pytest.mark.parametrize("q8", [False, True])
+def test_many_groups_of_many_columns(q8, rows):
+    """More groups than a workgroup has threads, 36 to 80 columns each, of a few requests."""
+    p, held, rng = filled([200, 75, 64], [24, 24, 24], q8=q8, seed=rows[0])
+    n_groups = 600
+    req = rng.integers(0, 3, n_groups).tolist()
+    lens = [int(rng.integers(0, [200, 75, 64][r] + 1)) for r in req]
+    size = rng.integers(rows[0], rows[1] + 1, n_groups)
+    size[rng.integers(0, n_groups, 40)] = 0
+    size = size.tolist()
+    q = _values(rng, "bf16", sum(size), 8, 128)
+    got = attend(p, q, size, lens, None, req=req, max_rows=rows[1])
+    check(p, held, q, got, size, lens, [np.tri(n, dtype=bool) for n in size], req=req)
+
+
+def test_a_block_of_columns_a_wave():
+    values_that_are_not_finite("bf16", 12)
+    large_logits("bf16", False, 12)
+    large_logits("bf16", True, 12)
