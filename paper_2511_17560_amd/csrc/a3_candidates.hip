@@ -182,7 +182,7 @@ struct move_args {
 };
 
 // The physical slot of a request's, -1 where there is none.
-__device__ __forceinline__ long long place_of(const pages_args &p, int req, int first, int o) {
+__device__ __forceinline__ long long place_of(const pages_args &p, int req, int first, uint32_t o) {
   const long long slot = (long long)first + o;
   if (req < 0 || req >= p.n_req || first < 0 || slot >= p.slots) return -1;
   const int page = p.table[(size_t)req * p.max_pages + (size_t)(slot >> p.page_shift)];
@@ -209,7 +209,7 @@ move_kernel(move_args a) {
   __syncthreads();
   int most = 0;
 #pragma unroll 8
-  for (int m = 0; m < N; ++m) most = max(most, last[m]);
+  for (int m = 0; m < N; ++m) most = max(most, last[m]);       // (up to 2^31 - 1: what comes behind it is counted unsigned)
   // Moves words W of slot `so` of these, of KV heads h, h + heads a pool, ..: the lane's `at` bytes into the slot's `width` bytes.
   auto move = [&](auto word, int so, int h, size_t at, int width) {
     typedef decltype(word) W;
@@ -227,10 +227,11 @@ move_kernel(move_args a) {
         if (p[m].to >= 0) *reinterpret_cast<W *>(pool + p[m].to + (uint32_t)(p[m].to_slot * width)) = x[m];
     }
   };
-  for (int o0 = blockIdx.x * slots; o0 < most; o0 += gridDim.x * slots) {
+  for (uint32_t o0 = blockIdx.x * slots; o0 < (uint32_t)most; o0 += gridDim.x * slots) {
     for (int i = tid; i < N * slots; i += 256) {               // (256 is a multiple of N: a thread has one move of the set)
-      const int o = o0 + i / N;
-      const long long x = o < n ? place_of(a.p, from_req, from, o) : -1, y = o < n ? place_of(a.p, to_req, to, o) : -1;
+      const uint32_t o = o0 + i / N;
+      const bool on = (long long)o < n;
+      const long long x = on ? place_of(a.p, from_req, from, o) : -1, y = on ? place_of(a.p, to_req, to, o) : -1;
       const size_t page_bytes = a.p.Hkv * a.head_bytes;
       places[i] = x >= 0 && y >= 0 && x != y ? place{(long long)((x >> a.p.page_shift) * page_bytes), (long long)((y >> a.p.page_shift) * page_bytes),
                                                      (int)(x & slot_mask), (int)(y & slot_mask)}
@@ -558,7 +559,7 @@ extern "C" a3_status a3_paged_move(const a3_pages *layers, int n_layers, const i
   move_args a{};
   a.p = args_of(layers);
   a.src_req = src_req; a.src_slot = src_slot; a.dst_req = dst_req; a.dst_slot = dst_slot; a.n_slots = n_slots;
-  a.max_slots = n_slots ? max_slots : 1;
+  a.max_slots = !n_slots ? 1 : max_slots < a.p.slots ? max_slots : a.p.slots;      // (none behind the table's end)
   a.set_size = set_size;
   a.row_bytes = layers->head_dim * (q8 ? 1 : elem_bytes(layers));
   a.q8 = q8;

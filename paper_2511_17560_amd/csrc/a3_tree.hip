@@ -239,7 +239,7 @@ tree_attention_kernel(tree_args a) {
 
   // How many of the next ones need no more than a look at the lane that has their page's number.
   auto count_simple = [&]() {
-    const int slot = slot_of(ahead), from = pages_from << a.p.page_shift, room = from + (64 << a.p.page_shift) - slot;
+    const int slot = slot_of(ahead), from = (int)((uint32_t)pages_from << a.p.page_shift), room = (int)((uint32_t)from + (64u << a.p.page_shift) - (uint32_t)slot);
     if (pages_from == kNoPages || slot < from || room <= 0) return 0;
     return min(min(ahead.k.steps - 1 - ahead.step, ahead_left - 1), (room - 1) / F::kStep + 1);
   };

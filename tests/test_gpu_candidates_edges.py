@@ -75,3 +75,13 @@ def test_fewer_workgroups_than_pools_and_heads(q8):
             sets.append([(s * size + int(rng.integers(0, size)), at, s * size + b, at, int(rng.integers(0, 44))) for b in range(size)])
         move(pages, sets)
         check_moves(pages, before, sets)
+
+
+def test_runs_as_long_as_a_number_goes():
+    """Runs of 2^31 - 1 slots, cut where the pages' table ends; the rest of the tables' slots are moved."""
+    pages = _layers([128] * 3, 2, Hq=4, Hkv=2, page=64, slack=0)
+    before = _snapshot(pages)
+    most = 2 ** 31 - 1
+    sets = [[(0, 5, 1, 5, most), (1, 5, 0, 5, most)], [(2, 100, 2, 100, most), (2, most, 2, 0, most)]]
+    move(pages, sets, most=most)
+    check_moves(pages, before, [[(0, 5, 1, 5, 123), (1, 5, 0, 5, 123)]])
