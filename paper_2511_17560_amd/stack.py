@@ -223,6 +223,7 @@ class DecodeBuffers:
         self.ws_attn = pages[0].workspace(n)
         self.ws_tree = pages[0].tree_workspace(*tree) if tree else None
         self.rows = torch.arange(n, dtype=torch.int32, device=dev)
+        self.source, self.runs = torch.empty_like(self.rows), torch.empty_like(self.rows)    # of steps of beams
         # (few rows can need more than many: their reductions are split, and the partial results want room)
         self.ws_tail = torch.empty(max([256] + [api.a3_block_tail_ws_bytes(layout, ffn, m) for m in range(1, n + 1)]), dtype=torch.uint8, device=dev)
         self.logits = torch.empty((n, vocab), dtype=torch.float32, device=dev) if vocab else None
@@ -322,8 +323,9 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
                out: api.BeamChoice, done=None, end_token: int = 0, stream=None) -> dict:
     """One step of beam search: a token of every beam through every block, the best continuations of every group of ``out.n_beams`` rows
     (row = beam = request of the pages), and the caches of the beams that go on in place of the others: beam j of a group takes over
-    slots ``first_slot`` .. + ``n_slots`` (at most ``max_slots``) of row ``out.row[g, j]``; in front of them the beams of a group have the same
-    tokens, in pages of their own or shared.  ``first_slot`` (equal within a group), ``n_slots``: device int32 [rows], the latter counting the new token.
+    slots ``first_slot`` .. + ``n_slots`` (at most ``max_slots``) of row ``out.row[g, j]``, as many as that row has; in front of them the beams of
+    a group have the same tokens, in pages of their own or shared.  ``first_slot`` (equal within a group), ``n_slots`` (of every row its own: beams
+    that have ended may hold fewer): device int32 [rows], the latter counting the new token.
     ``score`` of every row, ``done`` and ``end_token`` as for a3_beam_select; ``out`` has as many best ones as beams.  Returns decode_stack's
     dict."""
     if out.n_best != out.n_beams:
@@ -332,7 +334,12 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
         raise ValueError(f"beam_stack: {layout.n_req} rows are no groups of {out.n_beams} beams")
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, row_slot, row_pos, row_len, bufs, w_vocab=w_vocab, stream=stream)
     api.a3_beam_select(r["logits"], score, done, end_token, out, stream=stream)
-    api.a3_paged_move(pages, out.row, first_slot, bufs.rows, first_slot, n_slots, max_slots, layout.n_req // out.n_beams, out.n_beams, stream=stream)
+    # a move is as long as its source's run (where there is no source, -1, nothing moves, whatever the length)
+    n = layout.n_req
+    with torch.cuda.stream(api.torch_stream(stream)):
+        torch.clamp(out.row.view(-1)[:n], min=0, out=bufs.source[:n])
+        torch.index_select(n_slots.view(-1), 0, bufs.source[:n], out=bufs.runs[:n])
+    api.a3_paged_move(pages, out.row, first_slot, bufs.rows, first_slot, bufs.runs, max_slots, n // out.n_beams, out.n_beams, stream=stream)
     return r
 
 
