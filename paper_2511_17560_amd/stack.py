@@ -308,6 +308,8 @@ def verify_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
     ``out`` receives the picked tokens (largest logits), the accepted paths and the tokens behind them; the accepted rows of every
     layer's cache move to the slots behind the committed ones, so that a request has ``group_len + count`` of them afterwards (what
     lies behind is free).  ``layout`` has a row for each drafted token.  Returns decode_stack's dict."""
+    if w_vocab is None:
+        raise ValueError("verify_stack: the picks are of the step's logits: w_vocab is needed")
     if out.max_path != tree.path_req.shape[1]:
         raise ValueError(f"verify_stack: paths of {out.max_path} for trees of paths of {tree.path_req.shape[1]}")
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, tree.row_slot, tree.row_pos, None, bufs, row_req=tree.row_req,
@@ -332,6 +334,8 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
         raise ValueError(f"beam_stack: {out.n_best} continuations for {out.n_beams} beams")
     if layout.n_req % out.n_beams:
         raise ValueError(f"beam_stack: {layout.n_req} rows are no groups of {out.n_beams} beams")
+    if w_vocab is None:
+        raise ValueError("beam_stack: the choice is of the step's logits: w_vocab is needed")
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, row_slot, row_pos, row_len, bufs, w_vocab=w_vocab, stream=stream)
     api.a3_beam_select(r["logits"], score, done, end_token, out, stream=stream)
     # a move is as long as its source's run (where there is no source, -1, nothing moves, whatever the length)
