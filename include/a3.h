@@ -500,7 +500,7 @@ a3_status a3_tree_attention(const a3_pages *pages, const void *q, int n_groups, 
 /* From the logits of drafted rows to the accepted path of every tree.  picked[i] = the largest logit's index of row i (equal ones: the
  * lowest; -0 equals 0; NaN below everything); logits NULL: picked is given (a sampler's choice).  The path begins at row 0 and goes
  * on, as long as there is one, to the first row c behind the last one, parent[c] = the last one (numbers inside the group), with
- * tokens[c] = its picked token; a path of max_path rows ends.  For group g, with L = group_len[g]:
+ * tokens[c] = its picked token; a path of max_path rows ends.  For group g, with L = max(group_len[g], 0):
  *   count[g]        rows of the path (0: the group is empty, everything else of it -1)
  *   path[g, m]      their numbers inside the group; -1 behind the last
  *   next_token[g]   what was picked behind the last one

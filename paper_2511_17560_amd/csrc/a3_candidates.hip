@@ -121,7 +121,7 @@ follow_kernel(accept_args a) {
     join(first, min(64, a.n_rows - first), a.picked + first);
     return;
   }
-  const int first = a.start[g], end = a.start[g + 1], L = a.len ? a.len[g] : 0;
+  const int first = a.start[g], end = a.start[g + 1], L = a.len ? max(a.len[g], 0) : 0;
   const int n = first < 0 || end > a.n_rows || end < first ? 0 : min(end - first, a.max_rows);
   for (int i = tid; i < n; i += 256) {
     parent[i] = a.parent[first + i];

@@ -289,14 +289,15 @@ class TreeRows:
                     seen[row], depth[row] = seen[start[g] + p], depth[start[g] + p] + 1
                 seen[row, j] = 1
         reqs = np.arange(len(rows)) if reqs is None else np.asarray(reqs)
-        first = np.asarray(lens if positions is None else positions, dtype=np.int64)
+        lens = np.maximum(np.asarray(lens, dtype=np.int64), 0)       # (below 0: none, as a3_tree_attention takes it)
+        first = lens if positions is None else np.asarray(positions, dtype=np.int64)
         inside = np.arange(n) - np.repeat(start[:-1], rows)
         self.n_rows, self.tokens = n, i32(np.zeros(n) if tokens is None else tokens)
         self.group_start, self.group_req, self.group_len = i32(start), i32(reqs), i32(lens)
         self.parent = i32(np.concatenate([np.asarray(p, dtype=np.int32) for p in parents] + [np.zeros(0, dtype=np.int32)]))
         self.mask = i32(np.packbits(seen, axis=1, bitorder="little").view(np.int32)) if n else i32(np.zeros((0, words)))
         self.path_req = i32(np.repeat(reqs[:, None], max_path, 1))
-        self.row_req, self.row_slot = i32(np.repeat(reqs, rows)), i32(np.repeat(np.asarray(lens), rows) + inside)
+        self.row_req, self.row_slot = i32(np.repeat(reqs, rows)), i32(np.repeat(lens, rows) + inside)
         self.row_pos = i32(np.repeat(first, rows) + depth)
 
 
