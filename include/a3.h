@@ -528,7 +528,8 @@ a3_status a3_paged_move(const a3_pages *layers, int n_layers, const int *src_req
 
 /* The n_best best continuations of every group of n_beams beams.  Rows g * n_beams + b of logits belong to group g; the continuation of
  * beam b with token v is worth score[row] + x_v - m - log Z (the row's log probability as in a3_token_logprobs), one of a beam with done[row]
- * != 0 exists once, with end_token, and is worth score[row] (done NULL: none).  Best first; equal ones by the lower beam, then the lower token.
+ * != 0 exists once, with end_token, and is worth score[row] (done NULL: none).  Best first; equal ones by the lower beam, then the lower token.  (Of one beam the
+ * larger logit goes first also where a large score leaves no difference between worths in double.)
  *   best_score[g, j] (float), best_row[g, j] (its row of logits), best_token[g, j]
  * A token with a logit of -inf is none; a beam whose score is not finite, or whose row of logits has no distribution (NaN, +inf, nothing but
  * -inf) and that is not done, has none; where a group has fewer than n_best, the rest is -inf, -1, -1.

@@ -66,20 +66,21 @@ def move(cache, moves):
 
 
 def beams(x, score, done, end, n_best):
-    """x [beams, vocab] of one group.  (score, beam, token) lists of n_best, -inf, -1, -1 where there is none."""
+    """x [beams, vocab] of one group.  (score, beam, token) lists of n_best, -inf, -1, -1 where there is none.  Tokens of one beam whose worths
+    a double holds as equal go by their logits."""
     got = []
     for b, row in enumerate(np.asarray(x, dtype=np.float64)):
         if not np.isfinite(score[b]):
             continue
         if done is not None and done[b]:
-            got.append((-float(score[b]), b, end))
+            got.append((-float(score[b]), b, 0.0, end))
             continue
         lp = gen.log_probs(row[None])[0]
         if np.isnan(lp).any():
             continue
         total = float(score[b]) + lp
-        best = np.lexsort((np.arange(len(row)), -total))[:n_best]
-        got += [(-total[t], b, int(t)) for t in best if total[t] > -np.inf]
+        best = np.lexsort((np.arange(len(row)), -row))[:n_best]
+        got += [(-total[t], b, -row[t], int(t)) for t in best if total[t] > -np.inf]
     got = sorted(got)[:n_best]
-    got += [(np.inf, -1, -1)] * (n_best - len(got))
-    return np.array([-g[0] for g in got]), np.array([g[1] for g in got]), np.array([g[2] for g in got])
+    got += [(np.inf, -1, 0.0, -1)] * (n_best - len(got))
+    return np.array([-g[0] for g in got]), np.array([g[1] for g in got]), np.array([g[3] for g in got])

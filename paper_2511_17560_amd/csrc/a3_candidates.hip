@@ -344,9 +344,24 @@ beam_row_kernel(beam_args a) {
   for (int j = tid; j < a.n_best; j += kLpThreads) a.part_top[(size_t)blockIdx.x * a.n_best + j] = s.list[j];
 }
 
-// Larger worth, then lower beam, then lower token; worth -inf: no candidate.
-struct candidate { double worth; unsigned long long id; };
-__device__ __forceinline__ bool before(const candidate &a, const candidate &b) { return a.worth > b.worth || (a.worth == b.worth && a.id < b.id); }
+// Larger worth, then lower beam, then larger logit, then lower token; worth -inf: no candidate.  Worths of one beam differ as its logits do: where
+// a large score leaves a double no room for the difference, the logits decide, which the lists are ordered by.
+struct candidate { double worth; int beam; unsigned long long key; };       // key: the logit's, as in the lists
+__device__ __forceinline__ bool before(const candidate &a, const candidate &b) {
+  return a.worth > b.worth || (a.worth == b.worth && (a.beam < b.beam || (a.beam == b.beam && a.key > b.key)));
+}
+// How many of n candidates are before one of them: worths first, the rest only where some are equal.
+__device__ __forceinline__ int rank_of(const candidate &c, const candidate *of, int n) {
+  int rank = 0, equal = 0;
+#pragma unroll 4
+  for (int o = 0; o < n; ++o) {
+    rank += of[o].worth > c.worth;
+    equal += of[o].worth == c.worth;
+  }
+  if (equal > 1)
+    for (int o = 0; o < n; ++o) rank += of[o].worth == c.worth && before(of[o], c);
+  return rank;
+}
 
 constexpr int kBeamLists = 512, kBeamHeads = kBeamLists + kMaxBest, kHeadsAThread = (kBeamHeads + 255) / 256;
 __global__ void __launch_bounds__(256)
@@ -368,7 +383,7 @@ beam_join_kernel(beam_args a) {
     const int i = min(tid + 256 * q, heads - 1);
     keys[q] = tops[(size_t)(i / deep) * a.n_best + i % deep];
   }
-  if (tid == 0) { bound = candidate{-INFINITY, 0}; count = kept = n_lists = 0; }
+  if (tid == 0) { bound = candidate{-INFINITY, 0, 0}; count = kept = n_lists = 0; }
   // worth of a logit: base + x; as many lanes a beam as it has slices
   int lanes = 1;
   while (lanes < 64 && lanes < a.slices) lanes <<= 1;
@@ -402,10 +417,10 @@ beam_join_kernel(beam_args a) {
   __syncthreads();
   auto made = [&](int list, int j, unsigned long long key) {   // the jth of a list
     const int b = list / a.slices;
-    const unsigned long long id = (unsigned long long)b << 32;
-    if (kind[b] == 0) return candidate{-INFINITY, 0};
-    if (kind[b] == 2) return list == b * a.slices && j == 0 ? candidate{base[b], id | (uint32_t)a.end} : candidate{-INFINITY, 0};
-    return key ? candidate{base[b] + (double)top_value(key), id | (uint32_t)~(uint32_t)key} : candidate{-INFINITY, 0};
+    const candidate none{-INFINITY, 0, 0};
+    if (kind[b] == 0) return none;
+    if (kind[b] == 2) return list == b * a.slices && j == 0 ? candidate{base[b], b, top_key(0.f, a.end)} : none;
+    return key ? candidate{base[b] + (double)top_value(key), b, key} : none;
   };
   // A first bound: the largest of the waves' n_best-th heads, in float; the heads that reach it are ranked.
   candidate mine[kHeadsAThread];
@@ -413,7 +428,7 @@ beam_join_kernel(beam_args a) {
 #pragma unroll
   for (int q = 0; q < kHeadsAThread; ++q) {
     const int i = tid + 256 * q;
-    mine[q] = i < heads ? made(i / deep, i % deep, keys[q]) : candidate{-INFINITY, 0};
+    mine[q] = i < heads ? made(i / deep, i % deep, keys[q]) : candidate{-INFINITY, 0, 0};
     order[q] = mine[q].worth > -INFINITY ? max(top_order((float)mine[q].worth), 1u) : 0u;
   }
   const uint32_t nth = wave_nth<32, kHeadsAThread>(order, a.n_best);
@@ -431,9 +446,7 @@ beam_join_kernel(beam_args a) {
   const int n_heads = kept;
   for (int i = tid; i < n_heads; i += 256) {
     const candidate c = head[i];
-    int rank = 0;
-#pragma unroll 4
-    for (int o = 0; o < n_heads; ++o) rank += before(head[o], c);
+    const int rank = rank_of(c, head, n_heads);
     if (rank >= a.n_best) continue;
     if (rank == a.n_best - 1) bound = c;
     gathered[atomicAdd(&count, 1)] = c;
@@ -451,14 +464,12 @@ beam_join_kernel(beam_args a) {
   const int n = count;
   for (int i = tid; i < n; i += 256) {
     const candidate c = gathered[i];
-    int rank = 0;
-#pragma unroll 4
-    for (int o = 0; o < n; ++o) rank += before(gathered[o], c);
+    const int rank = rank_of(c, gathered, n);
     if (rank < a.n_best) {
       const size_t to = (size_t)g * a.n_best + rank;
       a.best_score[to] = (float)c.worth;
-      a.best_row[to] = first + (int)(c.id >> 32);
-      a.best_token[to] = (int)(uint32_t)c.id;
+      a.best_row[to] = first + c.beam;
+      a.best_token[to] = (int)~(uint32_t)c.key;
     }
   }
   for (int j = n + tid; j < a.n_best; j += 256) {
