@@ -535,6 +535,7 @@ extern "C" a3_status a3_tree_accept(int dtype, const void *logits, int vocab, lo
                 count, path, next_token, src_slot, dst_slot, n_rows ? pick_slices(n_rows, vocab) : 1,
                 (unsigned long long *)ws};
   const int more = logits ? (int)(((long long)n_rows + 63) / 64) : 0;
+  if (n_groups + (long long)more == 0) return A3_OK;           // (no trees, and the picks are given)
   A3_REQUIRE((long long)n_rows * a.slices < (1LL << 31) && (long long)n_groups + more < (1LL << 31), A3_ERR_UNSUPPORTED, "a3_tree_accept: too many rows");
   if (logits && n_rows)
     with_dtype(dtype, [&](auto e) {
