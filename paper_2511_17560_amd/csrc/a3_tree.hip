@@ -717,7 +717,7 @@ tree_attention_kernel(tree_args a) {
   auto finish = [&](const place &p, bool begins, bool ends) {
     const bool whole = begins && ends;
     const int slot = 2 * w + (begins ? 1 : 0), some_odd = __any(odd);
-    if (lane == 0) odd_waves[wave] = some_odd;
+    if (WS > 1 && lane == 0) odd_waves[wave] = some_odd;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       l[nb] += __shfl_xor(l[nb], 16);
@@ -729,9 +729,11 @@ tree_attention_kernel(tree_args a) {
     }
     A3_LDS_BARRIER();
     float M[NB], L[NB];
-    int some[NB], odd_any = 0;
+    // (waves that all take the same slots have all seen the same values; with WS = 1 no barrier would keep a wave's next flag from these readers)
+    int some[NB], odd_any = some_odd;
 #pragma unroll
-    for (int x = 0; x < W; ++x) odd_any |= odd_waves[x];
+    for (int x = 0; x < W; ++x)
+      if (WS > 1) odd_any |= odd_waves[x];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       M[nb] = -INFINITY;
