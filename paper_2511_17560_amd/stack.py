@@ -328,7 +328,7 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     (row = beam = request of the pages), and the caches of the beams that go on in place of the others: beam j of a group takes over
     slots ``first_slot`` .. + ``n_slots`` (at most ``max_slots``) of row ``out.row[g, j]``, as many as that row has; in front of them the beams of
     a group have the same tokens, in pages of their own or shared.  ``first_slot`` (equal within a group), ``n_slots`` (of every row its own: beams
-    that have ended may hold fewer): device int32 [rows], the latter counting the new token.
+    that have ended may hold fewer; None: 1): device int32 [rows], the latter counting the new token.
     ``score`` of every row, ``done`` and ``end_token`` as for a3_beam_select; ``out`` has as many best ones as beams.  Returns decode_stack's
     dict."""
     if out.n_best != out.n_beams:
@@ -340,11 +340,13 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, row_slot, row_pos, row_len, bufs, w_vocab=w_vocab, stream=stream)
     api.a3_beam_select(r["logits"], score, done, end_token, out, stream=stream)
     # a move is as long as its source's run (where there is no source, -1, nothing moves, whatever the length)
-    n = layout.n_req
-    with torch.cuda.stream(api.torch_stream(stream)):
-        torch.clamp(out.row.view(-1)[:n], min=0, out=bufs.source[:n])
-        torch.index_select(n_slots.view(-1), 0, bufs.source[:n], out=bufs.runs[:n])
-    api.a3_paged_move(pages, out.row, first_slot, bufs.rows, first_slot, bufs.runs, max_slots, n // out.n_beams, out.n_beams, stream=stream)
+    n, runs = layout.n_req, None
+    if n_slots is not None:
+        runs = bufs.runs[:n]
+        with torch.cuda.stream(api.torch_stream(stream)):
+            torch.clamp(out.row.view(-1)[:n], min=0, out=bufs.source[:n])
+            torch.index_select(n_slots.view(-1), 0, bufs.source[:n], out=runs)
+    api.a3_paged_move(pages, out.row, first_slot, bufs.rows, first_slot, runs, max_slots, n // out.n_beams, out.n_beams, stream=stream)
     return r
 
 
