@@ -209,6 +209,21 @@ def prefill_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Te
     return dict(resid=resid, hidden=x, k=ks, v=vs)
 
 
+def _ready(dev: int, dtype: torch.dtype, elems: int, *tensors) -> None:
+    """Refuses what one of a step's last calls would refuse, after the others have changed the caches: tensors of another type or device,
+    of fewer elements, or apart."""
+    api._hold(dev, dtype, elems, *tensors)
+    if not all(t is None or t.is_contiguous() for t in tensors):
+        raise ValueError("the tensors of a step are contiguous")
+
+
+def _workspace(dev: int, need: int, what: str, *tensors) -> None:
+    """Refuses workspaces smaller than ``need`` (0: what they are for is not supported)."""
+    if need == 0:
+        raise ValueError(f"{what} of such sizes are not supported")
+    _ready(dev, torch.uint8, need, *tensors)
+
+
 class DecodeBuffers:
     """What one decoding step of up to ``layout.n_req`` rows writes, allocated once (a captured graph keeps using them).
     ``layout`` is an api.Layout.decode; ``pages`` one api.Pages per layer; ``vocab`` > 0 asks for logits too; ``tree`` (trees, most
@@ -249,6 +264,18 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
     if tree is not None and tree.n_rows != n:
         raise ValueError(f"trees of {tree.n_rows} rows for a step of {n}")
     _fit(pages, len(layers), n if row_req is None else 0, 0, layout, prompt=False)
+    dev = b.x.get_device()
+    if row_slot is None or (row_len is None and tree is None):
+        raise ValueError("a step needs every row's slot and length")
+    _ready(dev, api.torch_dtype(layout.dtype), n * layout.struct.hidden, resid, b.x)
+    _ready(dev, torch.int32, n, row_req, row_slot, row_pos, row_len)
+    if tree is None:
+        _workspace(dev, max(api.a3_paged_attention_ws_bytes(pages[0], n), 1), "rows", b.ws_attn)
+    else:
+        groups = tree.group_start.numel() - 1
+        _ready(dev, torch.int32, groups, tree.group_start, tree.group_req, tree.group_len)
+        _workspace(dev, api.a3_tree_attention_ws_bytes(pages[0], groups, tree.max_rows), "trees", b.ws_tree)
+    _workspace(dev, max(api.a3_block_tail_ws_bytes(layout, int(layers[0]["w_gate"].shape[0]), n), 1), "rows", b.ws_tail)
     api.a3_rms_norm(layout, resid, None, n, layers[0]["g_in"], eps, b.x, stream=stream)
     for l, lw in enumerate(layers):
         api.a3_selected_qkv_proj(layout, b.x, None, n, lw["wq"], lw["wk"], lw["wv"], q_out=b.q, k_out=b.k, v_out=b.v,
@@ -313,6 +340,13 @@ def verify_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
         raise ValueError("verify_stack: the picks are of the step's logits: w_vocab is needed")
     if out.max_path != tree.path_req.shape[1]:
         raise ValueError(f"verify_stack: paths of {out.max_path} for trees of paths of {tree.path_req.shape[1]}")
+    dev, groups = resid.get_device(), len(tree.path_req)
+    if groups > 65535:
+        raise ValueError(f"verify_stack: {groups} trees (65535 at most)")
+    _ready(dev, torch.int32, tree.n_rows, tree.tokens, tree.parent, out.picked)
+    _ready(dev, torch.int32, groups, tree.group_start, tree.group_len, out.count, out.next_token)
+    _ready(dev, torch.int32, groups * out.max_path, tree.path_req, out.path, out.src_slot, out.dst_slot)
+    _workspace(dev, int(api.lib().a3_tree_accept_ws_bytes(tree.n_rows, w_vocab.shape[0])), "picks", out.ws)
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, tree.row_slot, tree.row_pos, None, bufs, row_req=tree.row_req,
                      w_vocab=w_vocab, stream=stream, tree=tree)
     api.a3_tree_accept(r["logits"], tree.tokens, tree.parent, tree.group_start, tree.group_len, layout.n_req, tree.max_rows, out, stream=stream)
@@ -337,10 +371,16 @@ def beam_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Tenso
         raise ValueError(f"beam_stack: {layout.n_req} rows are no groups of {out.n_beams} beams")
     if w_vocab is None:
         raise ValueError("beam_stack: the choice is of the step's logits: w_vocab is needed")
+    dev, n, groups = resid.get_device(), layout.n_req, layout.n_req // out.n_beams
+    if score is None or first_slot is None or max_slots < 0 or (done is not None and end_token < 0) or groups > 65535:
+        raise ValueError(f"beam_stack: every beam's score and first slot are needed, max_slots {max_slots}, end_token {end_token}, {groups} groups")
+    _ready(dev, torch.float32, n, score, out.score)
+    _ready(dev, torch.int32, n, done, first_slot, n_slots, out.row, out.token)
+    _workspace(dev, int(api.lib().a3_beam_select_ws_bytes(groups, out.n_beams, w_vocab.shape[0], out.n_best)), "beams", out.ws)
     r = decode_stack(layout, shape, layers, g_final, resid, pages.pages, row_slot, row_pos, row_len, bufs, w_vocab=w_vocab, stream=stream)
     api.a3_beam_select(r["logits"], score, done, end_token, out, stream=stream)
     # a move is as long as its source's run (where there is no source, -1, nothing moves, whatever the length)
-    n, runs = layout.n_req, None
+    runs = None
     if n_slots is not None:
         runs = bufs.runs[:n]
         with torch.cuda.stream(api.torch_stream(stream)):
