@@ -304,6 +304,11 @@ class TreeRows:
         i32 = lambda a: torch.as_tensor(np.ascontiguousarray(a, dtype=np.int32), device=device)
         rows = [len(p) for p in parents]
         n, self.max_rows = sum(rows), max(rows + [1, max_rows])
+        if self.max_rows > 1024 or not 1 <= max_path <= 64:
+            raise ValueError(f"TreeRows: trees of {self.max_rows} rows (1024 at most), paths of {max_path} (1 to 64)")
+        for name, of, many in (("lens", lens, len(rows)), ("reqs", reqs, len(rows)), ("positions", positions, len(rows)), ("tokens", tokens, n)):
+            if of is not None and math.prod(np.shape(of)) != many:
+                raise ValueError(f"TreeRows: {many} {name} are needed for {len(rows)} trees of {n} rows, got {np.shape(of)}")
         words = -(-self.max_rows // 32)
         seen, depth = np.zeros((n, 32 * words), dtype=np.uint8), np.zeros(n, dtype=np.int64)
         start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int64)
