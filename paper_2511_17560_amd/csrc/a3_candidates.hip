@@ -31,7 +31,7 @@ __device__ __forceinline__ unsigned long long max_of_lanes(unsigned long long k,
 // The largest logit of a slice of a row.  A thread keeps the maximum of its values and the chunk of 32 that it came from: one instruction a
 // value, so that reading is all that counts.  The key of the largest is found in that chunk afterwards, by the threads that have it alone.  (A
 // maximum of -inf says nothing: all may be NaN.)  Bound by one trip to memory where there are few rows: 16 rows of 128256 floats (8.2 MB) 5.7 us,
-// 380 of 32003 bf16 (24 MB) 11.4 us, 2.1 TB/s.
+// 403 of 32003 bf16 (26 MB) 11.3 us, 2.3 TB/s (of 32000, whose rows are aligned, no less); 403 of 128256 floats (207 MB) 44 us the whole call.
 template <typename T>
 __global__ void __launch_bounds__(kLpThreads)
 pick_kernel(accept_args a) {
@@ -192,8 +192,8 @@ __device__ __forceinline__ long long place_of(const pages_args &p, int req, int 
 // A thread has 16 bytes of one KV head at one slot o of the runs, of all N moves of its set: it reads them all, then writes them all, and no
 // other thread touches what it does, so that a set needs neither a barrier nor a copy in between.  8-bit pages: then the scales, four bytes
 // a slot.  Where the slots are is the same in every pool and head: looked up once, for every gridDim.z-th of them.  Bound by memory (reading and
-// writing the rows that change their place): 24 rows' worth of 32 layers' caches among 32 beams, 1.56 GB, 276 us = 5.6 TB/s, what a large copy reaches
-// (looked up for each pool and head, by every thread, 426).
+// writing the rows that change their place): 24 rows' worth of 32 layers' caches among 32 beams, 1.56 GB, 277 us = 5.6 TB/s, where torch's copy of
+// 2 GiB reaches 4.9 (looked up for each pool and head, by every thread, 426); the same rows in 8-bit pages, 0.80 GB, 155 us.
 template <int N>
 __global__ void __launch_bounds__(256)
 move_kernel(move_args a) {
@@ -253,8 +253,8 @@ move_kernel(move_args a) {
 // A second kernel, one workgroup a group, makes worths of its lists (one of every slice of every beam, best first) in double and puts
 // them together: the n_best-th of the lists' heads (or of their first few, where there are fewer lists) bounds what can be among the best,
 // what reaches it is gathered, n_best^2 values at most, and ranked by counting.  It is a chain of latencies: three trips to
-// memory, and nothing that goes through all lists one by one.  1 x 4 beams of 128256 floats: 7.7 + 8.0 us; 64 x 8 of 152064 floats: 56 us (311 MB,
-// 5.6 TB/s) + 11 us.
+// memory, and nothing that goes through all lists one by one.  1 x 4 beams of 128256 floats: 7.6 + 6.8 us; 64 x 8 of 152064 floats: 56 us (311 MB,
+// 5.6 TB/s) + 6.8 us; of 152064 bf16 (156 MB) 45 us the whole call.
 struct beam_args {
   const void *x;
   long long ld;

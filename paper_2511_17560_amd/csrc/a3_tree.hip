@@ -37,8 +37,11 @@ struct tree_args {
 // The maximum that exponentials refer to moves only when a logit exceeds it by 8 (2^8 is far from any limit of a float), and to a whole
 // number: what moves sums, and weights that wait, is then a power of two.
 //
-// What bounds it: memory, as long as the cache is read once for all columns; with more columns the issue of instructions (a slab of 32 slots
-// costs a wave of 32 columns 48 matrix instructions and 180 others) and what of them does not overlap.
+// What bounds it: memory, as long as the cache is read once for all columns; with more columns the half steps below (a slab of 32 slots
+// costs a wave of 32 columns 48 matrix instructions and 180 others), in which the matrix unit is busy 38 % of the time and the vector unit 49 %: the
+// rest are waits between two barriers that two waves a SIMD do not fill.
+// Registers: every form keeps 62 to 136 scalars in lanes of vector registers; bf16 of 128 with two blocks a wave (17 .. 32 columns) has seven vector
+// registers too few, 32 bytes a lane in scratch.
 //
 // Up to 32 columns, up to 64 over 8-bit pages, and fp32 rows: K and V straight from memory to registers.  One slab of registers is enough to have the next one on its
 // way: K of the next is asked for as soon as the products with this one's have read it, V as soon as its operands are formed, so that each
@@ -51,7 +54,7 @@ struct tree_args {
 // one), the other forms weights on the vector unit.
 //
 // Measured (one MI355X, bf16, 8 KV heads of 128, the whole call): 4 requests of 64K, 32 rows of 128 columns 261 us (4.1 TB/s; four waves of 64
-// columns, PV of one step and QK of the next between the weights, 283; without the products 206, without the weights 210); 8 of 8K, 64 rows 126 us
+// columns, PV of one step and QK of the next between the weights, 283; without the products 206, without the weights 210); 8 of 8K, 64 rows 127 us
 // (0.49 PFLOP/s without the weights' second parts); 8 of 64K: 1 row 335 us (the single-token kernel 328), 4 rows 368, 8 rows 424, 16 rows 456.
 //
 // A lane's eight slots of a column are eight bits of the row's mask.  Only slabs that reach behind the committed slots look at it: a slot that
