@@ -353,11 +353,11 @@ class PageLayers:
         self.device, self.page_table = self.pages[0].device, self.pages[0].page_table
         if any(p.device != self.device or p.page_table.data_ptr() != self.page_table.data_ptr() for p in self.pages):
             raise ValueError("PageLayers: the layers share one page table")
-        like = ("format", "dtype", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "n_req", "max_pages")
-        for l, p in enumerate(self.pages):
-            for name in like:
-                if getattr(p.struct, name) != getattr(self.pages[0].struct, name):
-                    raise ValueError(f"PageLayers: the {name} of layer {l} is {getattr(p.struct, name)}, of layer 0 {getattr(self.pages[0].struct, name)}")
+        names = ("format", "dtype", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "n_req", "max_pages")
+        like = [tuple(getattr(p.struct, name) for name in names) for p in self.pages]
+        for l, mine in enumerate(like):
+            if mine != like[0]:
+                raise ValueError(f"PageLayers: layer {l} has ({', '.join(names)}) {mine}, layer 0 {like[0]}")
         self.structs = (a3_pages * len(self.pages))(*[p.struct for p in self.pages])
 
 
