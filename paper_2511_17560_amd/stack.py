@@ -269,6 +269,10 @@ def decode_stack(layout: api.Layout, shape, layers: Sequence[Dict[str, torch.Ten
         raise ValueError("a step needs every row's slot and length")
     _ready(dev, api.torch_dtype(layout.dtype), n * layout.struct.hidden, resid, b.x)
     _ready(dev, torch.int32, n, row_req, row_slot, row_pos, row_len)
+    if w_vocab is not None:
+        if w_vocab.dim() != 2 or w_vocab.shape[1] != layout.struct.hidden:
+            raise ValueError(f"w_vocab is [vocab, {layout.struct.hidden}], got {tuple(w_vocab.shape)}")
+        _ready(dev, api.torch_dtype(layout.dtype), w_vocab.numel(), w_vocab)
     if tree is None:
         _workspace(dev, max(api.a3_paged_attention_ws_bytes(pages[0], n), 1), "rows", b.ws_attn)
     else:

@@ -117,6 +117,17 @@ def test_beams_that_do_not_fit(ran, over):
     assert ran == []
 
 
+@pytest.mark.parametrize("what", ["width", "type", "strided", "flat"])
+def test_vocabularies_that_do_not_fit(ran, what):
+    for step, n in ((_verify, 5), (_beam, 6)):
+        s = Step(n)
+        s.w = dict(width=torch.zeros((VOCAB, 256), dtype=torch.bfloat16), type=s.w.float(), strided=torch.zeros((VOCAB, 1024), dtype=torch.bfloat16)[:, ::2],
+                   flat=torch.zeros((VOCAB,), dtype=torch.bfloat16))[what]
+        with pytest.raises(ValueError):
+            step(s)
+    assert ran == []
+
+
 def test_more_beams_than_there_can_be(ran):
     out = api.BeamChoice(1, 65, VOCAB, 65, device="cpu")
     s = Step(65)
